@@ -189,6 +189,59 @@ lowra_status lowra_linear_bwd_input(const lowra_layout* layout, const uint8_t* p
                                     const uint16_t* B, int r, float s, uint16_t* dX,
                                     void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- the linear with what stands around it in a layer: bias, activation, gate and residual in the epilogue.
+ * Activations: LOWRA_ACT_GELU is z Phi(z), LOWRA_ACT_GELU_TANH its tanh form, LOWRA_ACT_SILU z / (1 + exp(-z)).  Infinite z give
+ * the limits. */
+enum { LOWRA_ACT_NONE = 0, LOWRA_ACT_RELU = 1, LOWRA_ACT_GELU = 2, LOWRA_ACT_GELU_TANH = 3, LOWRA_ACT_SILU = 4 };
+
+/* Forward:  v = x What^T + s (x A^T) B^T + bias;  y = act(v) mul + residual;  z = v rounded to bf16, for the backward pass.  With
+ * mul a gated layer is two calls: u by lowra_linear_fwd, then act(gate) u by this one.  All operands bf16 dev, 16-byte aligned;
+ * null: not there.  v and y are computed in fp32 from the fp32 sums and rounded once.
+ *   residual may be y itself (the call adds to y); otherwise no operand overlaps y or z.
+ * Arguments, workspace and errors otherwise as in lowra_linear_fwd; INVALID_ARG also for a null or unknown epilogue and when the
+ * current device is not the layout's. */
+typedef struct lowra_fwd_epilogue {
+    int act;                    /* LOWRA_ACT_* */
+    const uint16_t* bias;       /* [N] */
+    const uint16_t* mul;        /* [M,N] */
+    const uint16_t* residual;   /* [M,N] */
+    uint16_t* z;                /* [M,N] (out) */
+} lowra_fwd_epilogue;
+lowra_status lowra_linear_fwd_act(const lowra_layout* layout, const uint8_t* packed, const float* absmax,
+                                  const float* mappings, const uint16_t* x, int M, const uint16_t* A,
+                                  const uint16_t* B, int r, float s, const lowra_fwd_epilogue* epilogue, uint16_t* y,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Input gradient, taken on through what produced the layer's input x = act(z) mul:
+ *   g = dY What + s (dY B) A + residual;   dX = g mul act'(z);   dmul = g act(z)
+ * so that dX is the gradient of z (the next layer's dY on the way back) and dmul that of mul; residual is a gradient that reaches
+ * x by another way.  z (with an activation, or when dmul is asked for), mul, residual: bf16 [M,K] dev | dX, dmul bf16 [M,K] dev (out);
+ * null: not there; dmul needs mul.  g stays in fp32; each output is rounded once.
+ *   residual may be dX itself; otherwise no operand overlaps an output.
+ * Arguments, workspace and errors otherwise as in lowra_linear_bwd_input; INVALID_ARG also as above, and for a missing z or mul. */
+typedef struct lowra_bwd_epilogue {
+    int act;
+    const uint16_t* z;
+    const uint16_t* mul;
+    const uint16_t* residual;
+    uint16_t* dmul;
+} lowra_bwd_epilogue;
+lowra_status lowra_linear_bwd_input_act(const lowra_layout* layout, const uint8_t* packed, const float* absmax,
+                                        const float* mappings, const uint16_t* dY, int M, const uint16_t* A,
+                                        const uint16_t* B, int r, float s, const lowra_bwd_epilogue* epilogue, uint16_t* dX,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same for a gradient that comes from outside, with the bias gradient: dY is the gradient of act(z) mul,
+ *   dZ = dY mul act'(z);   dmul = dY act(z);   db[n] = sum_m dZ[m,n], of dZ in fp32 before it is rounded
+ * dY [M,N] bf16 dev | z, mul [M,N] bf16 dev or null, as above | dZ, dmul [M,N] bf16 dev (out), db [N] fp32 dev (out), each or null
+ *   (with LOWRA_ACT_NONE and no mul dZ is dY: pass null for the bias gradient alone); dZ may be dY itself.
+ *   workspace: dev, >= lowra_act_bwd_workspace_bytes(M, N), 16-byte aligned; unused without db.
+ * The sums are added in a fixed order.  M == 0 writes zeros to db.  INVALID_ARG: a negative size, an unknown activation, a missing
+ * dY, z or mul, no output at all; UNSUPPORTED: N % 8 != 0; MISALIGNED; WORKSPACE_TOO_SMALL. */
+size_t lowra_act_bwd_workspace_bytes(int M, int N);
+lowra_status lowra_act_bwd(int M, int N, int act, const uint16_t* dY, const uint16_t* z, const uint16_t* mul, uint16_t* dZ,
+                           uint16_t* dmul, float* db, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Mapping/threshold learner (Sec. 5 "Weighted Lloyd's for LoRA Quantization", App. G): for every
  * output channel, `iterations` rounds of weighted Lloyd-Max on its normalised weights
  * u = w * (1/absmax) (the quantizer's normalisation), each element weighted by its block's absmax,

@@ -1,0 +1,87 @@
+// Activation's backward pass with the bias gradient (a gradient that reaches a linear layer's output from outside, Sec. 2.1):
+//   dZ = dY mul act'(z)      dmul = dY act(z)      db[n] = sum over the tokens of dZ[m,n], before it is rounded
+//
+// Memory bound: every operand is read or written once, 16 bytes per lane.  A thread keeps eight columns and walks down the
+// tokens, so that their sums stay in registers; the wavefronts of a workgroup meet in LDS, workgroups in the workspace, both
+// added in a fixed order.
+#include <algorithm>
+
+#include "epilogue.h"
+#include "gemm_common.h"
+
+namespace lowra {
+
+namespace {
+
+constexpr int ACT_COLS = 512;            // columns per workgroup: 64 lanes x 8
+constexpr int ACT_WAVES = 4;
+
+// token rows per workgroup: enough workgroups to fill the chip several times, at least four rows per wavefront
+int act_rows(int M, int N) {
+    const int strips = (N + ACT_COLS - 1) / ACT_COLS, want = 8 * device_compute_units();
+    const int chunks = std::max(1, std::min((M + 15) / 16, (want + strips - 1) / strips));
+    return (M + chunks - 1) / chunks;
+}
+int act_chunks(int M, int N) { const int rows = act_rows(M, N); return rows ? (M + rows - 1) / rows : 0; }
+
+__global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(int M, int N, int rows, BwdEpi e, const uint16_t* dY, uint16_t* dZ, float* sums) {
+    __shared__ float red[ACT_WAVES][8][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = blockIdx.x * ACT_COLS + lane * 8;
+    const int m0 = blockIdx.y * rows, m1 = min(m0 + rows, M);
+    float total[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (col < N) {                                                  // N is a multiple of 8
+        with_act(e.act, [&](auto A) {
+            constexpr int ACT = decltype(A)::value;
+            for (int m = m0 + wave; m < m1; m += ACT_WAVES) {
+                const size_t at = (size_t)m * N + col;
+                float v[8];
+                Bf16Run<8> g;
+                EpiRun<BwdEpi, 8> r;
+                load_run<8>(dY + at, g);
+                epi_load<8>(e, at, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = g[i];
+                epi_grads<ACT, 8>(e, at, v, r);
+                if (dZ) store_run<8>(dZ + at, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) total[i] += v[i];
+            }
+        });
+    }
+    if (!sums) return;                                              // uniform
+#pragma unroll
+    for (int i = 0; i < 8; ++i) red[wave][i][lane] = total[i];
+    __syncthreads();
+    for (int o = threadIdx.x; o < ACT_COLS; o += ACT_WAVES * 64) {
+        const int c = blockIdx.x * ACT_COLS + o;
+        if (c < N) sums[(size_t)blockIdx.y * N + c] = ((red[0][o & 7][o >> 3] + red[1][o & 7][o >> 3]) + red[2][o & 7][o >> 3]) + red[3][o & 7][o >> 3];
+    }
+}
+
+__global__ __launch_bounds__(256) void act_sum_kernel(const float* __restrict__ sums, int chunks, int N, float* __restrict__ db) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= N) return;
+    float v = 0.0f;
+    for (int q = 0; q < chunks; ++q) v += sums[(size_t)q * N + c];
+    db[c] = v;
+}
+
+}  // namespace
+
+size_t act_bwd_workspace_bytes(int M, int N) {
+    const int chunks = act_chunks(M, N);
+    return chunks > 1 ? (size_t)chunks * N * sizeof(float) : 0;
+}
+
+hipError_t launch_act_bwd(int M, int N, const BwdEpi& e, const uint16_t* dY, uint16_t* dZ, float* db, void* workspace, hipStream_t st) {
+    const int rows = act_rows(M, N), chunks = act_chunks(M, N);
+    float* sums = !db ? nullptr : chunks > 1 ? static_cast<float*>(workspace) : db;
+    act_bwd_kernel<<<dim3((unsigned)((N + ACT_COLS - 1) / ACT_COLS), (unsigned)chunks), dim3(ACT_WAVES * 64), 0, st>>>(M, N, rows, e, dY, dZ, sums);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess || !db || chunks == 1) return err;
+    act_sum_kernel<<<dim3((unsigned)((N + 255) / 256)), dim3(256), 0, st>>>(sums, chunks, N, db);
+    return hipGetLastError();
+}
+
+}  // namespace lowra

@@ -6,6 +6,7 @@
 #include <numeric>
 
 #include "../../include/lowra.h"
+#include "epilogue.h"
 #include "gemm_mid.h"
 
 namespace {
@@ -460,6 +461,72 @@ lowra_status lowra_linear_bwd_input(const lowra_layout* L, const uint8_t* packed
     lowra::LinearArgs a{packed, absmax, mappings, dY, M, A, B, r, s, dX, workspace, usable_bytes(workspace, workspace_bytes)};
     return lowra::launch_linear_bwd_input(*L, a, g_linear_path.load(), static_cast<hipStream_t>(stream)) == hipSuccess
                ? LOWRA_OK : LOWRA_HIP_ERROR;
+}
+
+// ---- the linear calls with an epilogue
+static_assert(LOWRA_ACT_NONE == lowra::kActNone && LOWRA_ACT_RELU == lowra::kActRelu && LOWRA_ACT_GELU == lowra::kActGelu &&
+              LOWRA_ACT_GELU_TANH == lowra::kActGeluTanh && LOWRA_ACT_SILU == lowra::kActSilu, "the header's numbers");
+static bool known_act(int act) { return act >= LOWRA_ACT_NONE && act <= LOWRA_ACT_SILU; }
+static bool on_current_device(const lowra_layout* L) {
+    int dev = -1;
+    return hipGetDevice(&dev) == hipSuccess && dev == L->device;
+}
+
+lowra_status lowra_linear_fwd_act(const lowra_layout* L, const uint8_t* packed, const float* absmax, const float* mappings,
+                                  const uint16_t* x, int M, const uint16_t* A, const uint16_t* B, int r, float s,
+                                  const lowra_fwd_epilogue* e, uint16_t* y, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!e || !known_act(e->act)) return LOWRA_INVALID_ARG;
+    const lowra_status st = check_linear(L, LOWRA_OP_LINEAR_FWD, packed, absmax, mappings, x, M, A, B, r, y, workspace, workspace_bytes);
+    if (st != LOWRA_OK || M == 0 || L->N == 0) return st;
+    if (!aligned16(e->bias) || !aligned16(e->mul) || !aligned16(e->residual) || !aligned16(e->z)) return LOWRA_MISALIGNED;
+    if (e->z && (e->z == y || e->z == e->residual || e->z == e->mul)) return LOWRA_INVALID_ARG;
+    if (!on_current_device(L)) return LOWRA_INVALID_ARG;
+    const lowra::FwdEpi epi{e->act, e->bias, e->mul, e->residual, e->z};
+    lowra::LinearArgs a{packed, absmax, mappings, x, M, A, B, r, s, y, workspace, usable_bytes(workspace, workspace_bytes)};
+    a.fwd_epi = &epi;
+    return lowra::launch_linear_fwd(*L, a, g_linear_path.load(), g_fwd_tiling.load(), static_cast<hipStream_t>(stream)) == hipSuccess
+               ? LOWRA_OK : LOWRA_HIP_ERROR;
+}
+
+lowra_status lowra_linear_bwd_input_act(const lowra_layout* L, const uint8_t* packed, const float* absmax, const float* mappings,
+                                        const uint16_t* dY, int M, const uint16_t* A, const uint16_t* B, int r, float s,
+                                        const lowra_bwd_epilogue* e, uint16_t* dX, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!e || !known_act(e->act) || (e->dmul && !e->mul)) return LOWRA_INVALID_ARG;
+    const lowra_status st = check_linear(L, LOWRA_OP_LINEAR_BWD_INPUT, packed, absmax, mappings, dY, M, A, B, r, dX, workspace, workspace_bytes);
+    if (st != LOWRA_OK || M == 0) return st;
+    if (L->N == 0) return LOWRA_UNSUPPORTED;                      // (an empty contraction is not worth an epilogue of its own)
+    if ((e->act != LOWRA_ACT_NONE || e->dmul) && !e->z) return LOWRA_INVALID_ARG;
+    if (!aligned16(e->z) || !aligned16(e->mul) || !aligned16(e->residual) || !aligned16(e->dmul)) return LOWRA_MISALIGNED;
+    if (e->dmul && (e->dmul == dX || e->dmul == e->residual || e->dmul == e->z || e->dmul == e->mul)) return LOWRA_INVALID_ARG;
+    if (!on_current_device(L)) return LOWRA_INVALID_ARG;
+    const lowra::BwdEpi epi{e->act, e->z, e->mul, e->residual, e->dmul};
+    lowra::LinearArgs a{packed, absmax, mappings, dY, M, A, B, r, s, dX, workspace, usable_bytes(workspace, workspace_bytes)};
+    a.bwd_epi = &epi;
+    return lowra::launch_linear_bwd_input(*L, a, g_linear_path.load(), static_cast<hipStream_t>(stream)) == hipSuccess
+               ? LOWRA_OK : LOWRA_HIP_ERROR;
+}
+
+size_t lowra_act_bwd_workspace_bytes(int M, int N) { return M > 0 && N > 0 ? lowra::act_bwd_workspace_bytes(M, N) : 0; }
+
+lowra_status lowra_act_bwd(int M, int N, int act, const uint16_t* dY, const uint16_t* z, const uint16_t* mul, uint16_t* dZ,
+                           uint16_t* dmul, float* db, void* workspace, size_t workspace_bytes, void* stream) {
+    if (M < 0 || N < 0 || !known_act(act) || (dmul && !mul) || (!dZ && !dmul && !db)) return LOWRA_INVALID_ARG;
+    if (N % 8 != 0) return LOWRA_UNSUPPORTED;
+    if (N == 0) return LOWRA_OK;
+    if (!aligned16(db)) return LOWRA_MISALIGNED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (M == 0) return !db || lowra::launch_zero_bf16(reinterpret_cast<uint16_t*>(db), (size_t)N * 2, st) == hipSuccess ? LOWRA_OK : LOWRA_HIP_ERROR;
+    if (!dY || ((act != LOWRA_ACT_NONE || dmul) && !z)) return LOWRA_INVALID_ARG;
+    if (!aligned16(dY) || !aligned16(z) || !aligned16(mul) || !aligned16(dZ) || !aligned16(dmul)) return LOWRA_MISALIGNED;
+    if (dmul && (dmul == dY || dmul == dZ || dmul == z || dmul == mul)) return LOWRA_INVALID_ARG;
+    const size_t need = db ? lowra::act_bwd_workspace_bytes(M, N) : 0;
+    if (need > 0) {
+        if (!workspace) return LOWRA_INVALID_ARG;
+        if (!aligned16(workspace)) return LOWRA_MISALIGNED;
+        if (workspace_bytes < need) return LOWRA_WORKSPACE_TOO_SMALL;
+    }
+    const lowra::BwdEpi epi{act, z, mul, nullptr, dmul};
+    return lowra::launch_act_bwd(M, N, epi, dY, dZ, db, workspace, st) == hipSuccess ? LOWRA_OK : LOWRA_HIP_ERROR;
 }
 
 // ---- several small-token forwards in one run

@@ -127,6 +127,134 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
 }
 
+// the operands of a linear call's epilogue, as include/lowra.h lays them out
+struct FwdEpilogue { int act; const void *bias, *mul, *residual; void* z; };
+struct BwdEpilogue { int act; const void *z, *mul, *residual; void* dmul; };
+typedef int (*linear_act_fn)(const void*, const void*, const void*, const void*, const void*, int, const void*, const void*, int, float, const void*,
+                             void*, void*, size_t, void*);
+typedef int (*act_bwd_fn)(int, int, int, const void*, const void*, const void*, void*, void*, void*, void*, size_t, void*);
+linear_act_fn lib_linear_act[2];
+act_bwd_fn lib_act_bwd;
+
+// (first, second or None)
+PyObject* pair_or_none(at::Tensor first, at::Tensor second, bool has_second) {
+    PyObject* x = THPVariable_Wrap(std::move(first));
+    PyObject* y = x && has_second ? THPVariable_Wrap(std::move(second)) : nullptr;
+    PyObject* t = x && (y || !has_second) ? PyTuple_Pack(2, x, y ? y : Py_None) : nullptr;
+    Py_XDECREF(x);
+    Py_XDECREF(y);
+    return t;
+}
+// an operand that may be None: false if it is neither that nor a plain bf16 tensor of this shape on `device`
+bool operand(PyObject* o, int64_t rows, int64_t cols, const at::Tensor& like, const void*& p) {
+    p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = plain(o, at::kBFloat16);
+    if (!t || t->device() != like.device() || !(rows < 0 ? t->dim() == 1 && t->size(0) == cols : shape2(*t, rows, cols))) return false;
+    p = t->data_ptr();
+    return true;
+}
+
+// linear_act(which, layout, packed, absmax, mappings, act, A, B, s, activation, bias or z, mul, residual, second, workspace) ->
+// (y, z or None) or (dX, dmul or None); `second`: whether z is kept (forward; the input gradient returns dmul where there is mul)
+PyObject* linear_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 15) return none();
+    try {
+        if (modes()) return none();
+        const long which = PyLong_AsLong(a[0]);
+        Lay l;
+        if ((which != 0 && which != 1) || !layout_of(a[1], l)) return none();
+        const at::Tensor* packed = plain(a[2], at::kByte);
+        const at::Tensor* absmax = plain(a[3], l.bf16_scales ? at::kBFloat16 : at::kFloat);
+        const at::Tensor* mappings = plain(a[4], at::kFloat);
+        const at::Tensor* act = plain(a[5], at::kBFloat16);
+        const int64_t in = which ? l.N : l.K, cols = which ? l.K : l.N;
+        if (!state_ok(l, packed, absmax, mappings) || !act || act->dim() != 2 || act->size(1) != in || !PyFloat_Check(a[8]) || !PyLong_CheckExact(a[9]) ||
+            !PyBool_Check(a[13])) return none();
+        const int64_t M = act->size(0);
+        if (M > INT32_MAX) return none();
+        const at::Tensor *A = nullptr, *B = nullptr;
+        int64_t r = 0;
+        if (a[6] != Py_None && a[7] != Py_None) {
+            A = plain(a[6], at::kBFloat16); B = plain(a[7], at::kBFloat16);
+            if (!A || !B || A->dim() != 2 || A->size(0) < 1) return none();
+            r = A->size(0);
+            if (r > INT32_MAX || A->size(1) != l.K || !shape2(*B, l.N, r)) return none();
+        }
+        const void *first, *mul, *residual;
+        if (!operand(a[10], which ? M : -1, cols, *act, first) || !operand(a[11], M, cols, *act, mul) || !operand(a[12], M, cols, *act, residual)) return none();
+        const long activation = PyLong_AsLong(a[9]);
+        if (PyErr_Occurred() || activation != (int)activation) return none();
+        const at::Tensor* ws = plain(a[14], at::kByte);
+        if (!ws || ws->device() != act->device() || packed->device() != act->device() || act->get_device() != c10::hip::current_device()) return none();
+        void* const wp = ws->data_ptr();
+        const size_t ws_bytes = (size_t)ws->numel();
+        const float s = (float)PyFloat_AS_DOUBLE(a[8]);
+        const bool two = which ? mul != nullptr : a[13] == Py_True;
+        at::Tensor out = empty({M, cols}, act->options()), second;
+        if (two) second = empty({M, cols}, act->options());
+        void *po = out.data_ptr(), *p2 = two ? second.data_ptr() : nullptr, *st = current_stream();
+        const void *pp = packed->data_ptr(), *pa = absmax->data_ptr(), *pm = mappings->data_ptr(), *px = act->data_ptr();
+        const void *pA = A ? A->data_ptr() : nullptr, *pB = B ? B->data_ptr() : nullptr;
+        const FwdEpilogue fe{(int)activation, first, mul, residual, p2};
+        const BwdEpilogue be{(int)activation, first, mul, residual, p2};
+        PyObject* res = pair_or_none(std::move(out), std::move(second), two);
+        if (!res) return none();
+        int status;
+        {
+            Unlocked u;
+            status = lib_linear_act[which](l.handle, pp, pa, pm, px, (int)M, pA, pB, (int)r, s, which ? (const void*)&be : (const void*)&fe, po, wp, ws_bytes, st);
+        }
+        return done(status, res);
+    } catch (...) {
+        return none();
+    }
+}
+
+// act_bwd(dY, activation, z, mul, bias_grad, workspace) -> (dZ or None, dmul or None, db or None)
+PyObject* act_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 6) return none();
+    try {
+        if (modes()) return none();
+        const at::Tensor* dY = plain(a[0], at::kBFloat16);
+        if (!dY || dY->dim() != 2 || !PyLong_CheckExact(a[1]) || !PyBool_Check(a[4])) return none();
+        const int64_t M = dY->size(0), N = dY->size(1);
+        const long activation = PyLong_AsLong(a[1]);
+        const void *z, *mul;
+        if (PyErr_Occurred() || activation != (int)activation || M > INT32_MAX || N > INT32_MAX || !operand(a[2], M, N, *dY, z) || !operand(a[3], M, N, *dY, mul))
+            return none();
+        const at::Tensor* ws = plain(a[5], at::kByte);
+        const bool want[3] = {activation != 0 || mul, mul != nullptr, a[4] == Py_True};
+        if (!ws || ws->device() != dY->device() || dY->get_device() != c10::hip::current_device() || !(want[0] || want[2])) return none();
+        at::Tensor out[3];
+        void* p[3] = {nullptr, nullptr, nullptr};
+        if (want[0]) out[0] = empty({M, N}, dY->options());
+        if (want[1]) out[1] = empty({M, N}, dY->options());
+        if (want[2]) out[2] = empty({N}, dY->options().dtype(at::kFloat));
+        for (int i = 0; i < 3; ++i) if (want[i]) p[i] = out[i].data_ptr();
+        const void* py = dY->data_ptr();
+        void *wp = ws->data_ptr(), *st = current_stream();
+        const size_t ws_bytes = (size_t)ws->numel();
+        PyObject* v[3] = {nullptr, nullptr, nullptr};
+        bool fine = true;
+        for (int i = 0; i < 3 && fine; ++i) {
+            if (want[i]) { v[i] = THPVariable_Wrap(std::move(out[i])); fine = v[i] != nullptr; }
+            else { Py_INCREF(Py_None); v[i] = Py_None; }
+        }
+        PyObject* res = fine ? PyTuple_Pack(3, v[0], v[1], v[2]) : nullptr;
+        for (PyObject* o : v) Py_XDECREF(o);
+        if (!res) return none();
+        int status;
+        {
+            Unlocked u;
+            status = lib_act_bwd((int)M, (int)N, (int)activation, py, z, mul, p[0], p[1], p[2], wp, ws_bytes, st);
+        }
+        return done(status, res);
+    } catch (...) {
+        return none();
+    }
+}
+
 // side_product(layout, op, M, r, workspace) -> (view,) or (None,)
 PyObject* side_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 5) return none();
@@ -261,7 +389,20 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// init_act(addresses): those of the calls with an activation
+PyObject* init_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 3) { PyErr_SetString(PyExc_TypeError, "init_act: three addresses"); return nullptr; }
+    void* f[3];
+    for (int i = 0; i < 3; ++i) f[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+    lib_linear_act[0] = (linear_act_fn)f[0]; lib_linear_act[1] = (linear_act_fn)f[1]; lib_act_bwd = (act_bwd_fn)f[2];
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)())init, METH_FASTCALL, nullptr},
+                         {"init_act", (PyCFunction)(void (*)())init_act, METH_FASTCALL, nullptr},
+                         {"linear_act", (PyCFunction)(void (*)())linear_act, METH_FASTCALL, nullptr},
+                         {"act_bwd", (PyCFunction)(void (*)())act_bwd, METH_FASTCALL, nullptr},
                          {"linear", (PyCFunction)(void (*)())linear, METH_FASTCALL, nullptr},
                          {"side_product", (PyCFunction)(void (*)())side_product, METH_FASTCALL, nullptr},
                          {"grads", (PyCFunction)(void (*)())grads, METH_FASTCALL, nullptr},

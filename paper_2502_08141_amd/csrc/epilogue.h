@@ -1,0 +1,245 @@
+// What the linear calls with an epilogue do to a result before it is stored, and the activation's backward pass.
+//
+//   forward         v = product + bias                 y = act(v) mul + residual     z = bf16(v), where it is kept
+//   input gradient  g = product + residual             dX = g mul act'(z)            dmul = g act(z)
+//
+// All arithmetic is fp32 on the fp32 accumulators; every output is rounded to bf16 once.  z is kept as bf16, the type of the
+// activations beside it: the gradient of an activation changes by its curvature times half a bf16 step of z, less than the
+// gradient's own rounding for |z| up to about one, and fp32 would double what the backward pass reads.
+//
+// What bounds it: plain-ALU issue where a GEMM's workgroup is alone on its compute unit (nothing overlaps its epilogue), so
+// the activations are a handful of instructions.  Quarter-rate instructions per value: silu 2 (exp2, reciprocal), gelu 1
+// (exp2 of a polynomial; 2 with its slope), tanh form 2.
+#pragma once
+#include <type_traits>
+
+#include "lowra_host.h"
+
+namespace lowra {
+
+enum : int { kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4 };
+
+// log2(e)
+constexpr float kLog2e = 1.44269504f;
+
+// The normal distribution function at -|z|, as 2 to the power of a polynomial in |z| (our own minimax fit of log2 Phi(-a) on
+// [0, 7]): within 4e-6 of it relatively up to |z| = 4, 7e-5 up to 7; beyond, the negative leading coefficient takes it to zero.
+// In this form the small tail keeps its relative accuracy, which 1 + erf loses, and one exp2 is the only slow instruction.
+__device__ __forceinline__ float normal_tail(float z) {
+    const float a = __builtin_fabsf(z);
+    float q = -0x1.df6e4cp-20f;
+    q = __builtin_fmaf(q, a, 0x1.fd25bcp-15f);
+    q = __builtin_fmaf(q, a, -0x1.e477p-11f);
+    q = __builtin_fmaf(q, a, 0x1.16095ep-7f);
+    q = __builtin_fmaf(q, a, -0x1.b9b316p-5f);
+    q = __builtin_fmaf(q, a, -0x1.d58178p-2f);
+    q = __builtin_fmaf(q, a, -0x1.26b778p+0f);
+    q = __builtin_fmaf(q, a, -0x1.ffff92p-1f);
+    return __builtin_amdgcn_exp2f(q);
+}
+
+// act(z) and, with SLOPE, act'(z).  Infinite z give the limits (a factor that has become zero is not multiplied with one).
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ void activation(float z, float& y, float& slope) {
+    slope = 1.0f;
+    if constexpr (ACT == kActNone) {
+        y = z;
+    } else if constexpr (ACT == kActRelu) {
+        y = z < 0.0f ? 0.0f : z;                                   // (a NaN stays one)
+        slope = z > 0.0f ? 1.0f : 0.0f;
+    } else if constexpr (ACT == kActGelu) {
+        const float e = normal_tail(z), p = z > 0.0f ? 1.0f - e : e;
+        y = p == 0.0f ? 0.0f : z * p;
+        if constexpr (SLOPE) {
+            const float d = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e)) * 0.398942280f;       // the density
+            slope = d == 0.0f ? p : __builtin_fmaf(z, d, p);
+        }
+    } else {
+        // z times the logistic function of w
+        float w = z, dw = 1.0f;
+        if constexpr (ACT == kActGeluTanh) {
+            constexpr float c = 1.59576912f, d = 0.044715f;        // 2 sqrt(2 / pi)
+            const float z2 = z * z;
+            w = c * z * __builtin_fmaf(d, z2, 1.0f);
+            dw = c * __builtin_fmaf(3.0f * d, z2, 1.0f);
+        }
+        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w * -kLog2e));
+        y = s == 0.0f ? 0.0f : z * s;
+        if constexpr (SLOPE) {
+            const float t = s - s * s;                             // s (1 - s)
+            slope = t == 0.0f ? s : __builtin_fmaf(z * dw, t, s);
+        }
+    }
+}
+
+// calls f(std::integral_constant<int, act>): a uniform branch around what follows
+template <class F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+    switch (act) {
+        case kActRelu: f(std::integral_constant<int, kActRelu>{}); break;
+        case kActGelu: f(std::integral_constant<int, kActGelu>{}); break;
+        case kActGeluTanh: f(std::integral_constant<int, kActGeluTanh>{}); break;
+        case kActSilu: f(std::integral_constant<int, kActSilu>{}); break;
+        default: f(std::integral_constant<int, kActNone>{}); break;
+    }
+}
+
+// W (1, 4 or 8) neighbouring bf16 values in one access, kept as they are until they are used (a conversion beside the load would
+// wait for it there)
+template <int W> struct Bf16Run {
+    uint32_t d[W == 1 ? 1 : W / 2];
+    __device__ __forceinline__ float operator[](int i) const {
+        return W == 1 || (i & 1) == 0 ? bf16_bits_to_float(d[i >> 1]) : __builtin_bit_cast(float, d[i >> 1] & 0xffff0000u);
+    }
+};
+template <int W>
+__device__ __forceinline__ void load_run(const uint16_t* p, Bf16Run<W>& r) {
+    static_assert(W == 1 || W == 4 || W == 8, "one access");
+    if constexpr (W == 8) { const uint4 t = *reinterpret_cast<const uint4*>(p); r.d[0] = t.x; r.d[1] = t.y; r.d[2] = t.z; r.d[3] = t.w; }
+    if constexpr (W == 4) { const uint2 t = *reinterpret_cast<const uint2*>(p); r.d[0] = t.x; r.d[1] = t.y; }
+    if constexpr (W == 1) r.d[0] = *p;
+}
+template <int W>
+__device__ __forceinline__ void store_run(uint16_t* p, const float (&v)[W]) {
+    if constexpr (W == 1) *p = (uint16_t)(pack_bf16x2(v[0], 0.0f) & 0xffffu);
+    if constexpr (W == 4) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    if constexpr (W == 8)
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+}
+
+// The operands of an epilogue; null: not there.  mul, residual, z, dmul: [M][columns] like the result.
+struct FwdEpi {
+    int act;
+    const uint16_t* bias;        // [columns]
+    const uint16_t* mul;
+    const uint16_t* residual;    // may be the result's own buffer: an element is read before it is written, by the same thread
+    uint16_t* z;                 // out
+};
+struct BwdEpi {
+    int act;
+    const uint16_t* z;
+    const uint16_t* mul;
+    const uint16_t* residual;    // as above
+    uint16_t* dmul;              // out
+};
+struct NoEpi {};
+
+// What an epilogue reads for W neighbouring results
+template <class E, int W> struct EpiRun;
+template <int W> struct EpiRun<FwdEpi, W> { Bf16Run<W> mul, residual; };
+template <int W> struct EpiRun<BwdEpi, W> { Bf16Run<W> z, mul, residual; };
+template <int W>
+__device__ __forceinline__ void epi_load(const FwdEpi& e, size_t at, EpiRun<FwdEpi, W>& r) {
+    if (e.mul) load_run<W>(e.mul + at, r.mul);
+    if (e.residual) load_run<W>(e.residual + at, r.residual);
+}
+template <int W>
+__device__ __forceinline__ void epi_load(const BwdEpi& e, size_t at, EpiRun<BwdEpi, W>& r) {
+    if (e.z) load_run<W>(e.z + at, r.z);
+    if (e.mul) load_run<W>(e.mul + at, r.mul);
+    if (e.residual) load_run<W>(e.residual + at, r.residual);
+}
+// the bias of W neighbouring columns; none in the input gradient
+template <int W>
+__device__ __forceinline__ void epi_bias(const FwdEpi& e, int col, float (&b)[W]) {
+    Bf16Run<W> r;
+    if (e.bias) load_run<W>(e.bias + col, r);
+#pragma unroll
+    for (int i = 0; i < W; ++i) b[i] = e.bias ? r[i] : 0.0f;
+}
+template <int W>
+__device__ __forceinline__ void epi_bias(const BwdEpi&, int, float (&)[W]) {}
+
+// v: the products; `at`: element of the result
+template <int ACT, int W>
+__device__ __forceinline__ void epi_store(const FwdEpi& e, size_t at, float (&v)[W], const float (&b)[W], const EpiRun<FwdEpi, W>& r, uint16_t* out) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] += b[i];
+    if (e.z) store_run<W>(e.z + at, v);
+    float slope;
+#pragma unroll
+    for (int i = 0; i < W; ++i) activation<ACT, false>(v[i], v[i], slope);
+    if (e.mul) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] *= r.mul[i];
+    }
+    if (e.residual) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] += r.residual[i];
+    }
+    store_run<W>(out + at, v);
+}
+// v: the products in, dX out (in fp32)
+template <int ACT, int W>
+__device__ __forceinline__ void epi_grads(const BwdEpi& e, size_t at, float (&v)[W], const EpiRun<BwdEpi, W>& r) {
+    if (e.residual) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] += r.residual[i];
+    }
+    float y[W], slope[W];
+    if (ACT != kActNone || e.dmul) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) activation<ACT, true>(r.z[i], y[i], slope[i]);
+    }
+    if (e.dmul) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) y[i] *= v[i];
+        store_run<W>(e.dmul + at, y);
+    }
+    if (e.mul) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] *= r.mul[i];
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if constexpr (ACT == kActRelu) v[i] = slope[i] != 0.0f ? v[i] : 0.0f;      // (an infinite gradient where nothing passes: zero)
+        else if constexpr (ACT != kActNone) v[i] *= slope[i];
+    }
+}
+template <int ACT, int W>
+__device__ __forceinline__ void epi_store(const BwdEpi& e, size_t at, float (&v)[W], const float (&)[W], const EpiRun<BwdEpi, W>& r, uint16_t* out) {
+    epi_grads<ACT, W>(e, at, v, r);
+    store_run<W>(out + at, v);
+}
+
+// Eight columns from `col` on of the token rows row, row + STEP, .. (ITS of them): read(i, v) gives the products of the i-th.  The
+// operands of U rows are asked for together: nothing else is there to cover their way while a workgroup is alone on its unit.
+template <int STEP, int ITS, class E, class Read>
+__device__ __forceinline__ void epi_rows(const E& e, uint16_t* out, int ld, int M, int row, int col, Read&& read) {
+    constexpr int U = ITS % 4 == 0 ? 4 : ITS % 2 == 0 ? 2 : 1;
+    float b[8];
+    epi_bias<8>(e, col, b);
+    with_act(e.act, [&](auto A) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int i = 0; i < ITS; i += U) {
+            EpiRun<E, 8> r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (row + (i + u) * STEP < M) epi_load<8>(e, (size_t)(row + (i + u) * STEP) * ld + col, r[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (row + (i + u) * STEP < M) {
+                    float v[8];
+                    read(i + u, v);
+                    epi_store<decltype(A)::value, 8>(e, (size_t)(row + (i + u) * STEP) * ld + col, v, b, r[u], out);
+                }
+        }
+    });
+}
+// The tile as fp32 in LDS, CHUNKS 16-byte chunks a row: chunk q (four columns) sits at half of the row by q's parity, place q / 2,
+// xored with the row.  The accumulators' writes (one chunk of neighbouring rows) and the reads of eight columns (neighbouring
+// even chunks, then odd ones, of one row) then both touch every bank.
+template <int CHUNKS>
+__device__ __forceinline__ int epi_chunk(int row, int q) { return row * (CHUNKS * 16) + ((((q >> 1) | ((q & 1) * (CHUNKS / 2))) ^ (row & (CHUNKS / 2 - 1))) << 4); }
+template <int CHUNKS>
+__device__ __forceinline__ void epi_read8(const uint8_t* smem, int row, int c8, float (&v)[8]) {
+    const float4 a = *reinterpret_cast<const float4*>(smem + epi_chunk<CHUNKS>(row, 2 * c8)), b = *reinterpret_cast<const float4*>(smem + epi_chunk<CHUNKS>(row, 2 * c8 + 1));
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+
+// ---- act.hip
+size_t act_bwd_workspace_bytes(int M, int N);
+// e.residual must be null; dZ null: only the sums (and dmul)
+hipError_t launch_act_bwd(int M, int N, const BwdEpi& e, const uint16_t* dY, uint16_t* dZ, float* db, void* workspace, hipStream_t st);
+
+}  // namespace lowra

@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "epilogue.h"
 #include "gemm_common.h"
 
 namespace lowra {
@@ -58,9 +59,40 @@ struct RowRegs {          // what a thread needs to decode its row's group for o
     int bits;
 };
 
+// The tile as it is, or through an epilogue (epilogue.h): the 128 token rows of two wavefronts at a time go through LDS as fp32, so
+// that every operand is read and every result written in 16 contiguous bytes, by a thread that keeps its columns.
+__device__ __forceinline__ void bwd_store(const floatx16_t (&acc)[4][4], const GemmParams& p, NoEpi, int m0, int k0, uint8_t*) {
+    store_out(acc, p.out, p.K, p.M, p.K, m0, k0);
+}
+__device__ __forceinline__ void bwd_store(const floatx16_t (&acc)[4][4], const GemmParams& p, const BwdEpi& epi, int m0, int k0, uint8_t* smem) {
+    static_assert(128 * 1024 <= kBwdSmem, "128 rows of 256 fp32");
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));                                  // (as in store_out_f32)
+    const int lane = tid & 63, wave = tid >> 6, wn = wave & 1, c = tid & 31, r0 = tid >> 5;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        __syncthreads();                                           // the last readers of what is overwritten are done
+        if ((wave >> 1) == half) {
+#pragma unroll
+            for (int tm = 0; tm < 4; ++tm)
+#pragma unroll
+                for (int tn = 0; tn < 4; ++tn) {
+                    const int col = wn * 128 + tn * 32 + (lane & 31);
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        *reinterpret_cast<float*>(smem + epi_chunk<64>(tm * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3), col >> 2) + (col & 3) * 4) = acc[tm][tn][v];
+                }
+        }
+        __syncthreads();
+        if (k0 + 8 * c < p.K)
+            epi_rows<8, 16>(epi, p.out, p.K, p.M, m0 + 128 * half + r0, k0 + 8 * c,
+                            [&](int i, float (&v)[8]) __attribute__((always_inline)) { epi_read8<64>(smem, i * 8 + r0, c, v); });
+    }
+}
+
 // LUT: the instantiation for matrices with 4-bit rows (every step a general step with the lookup decode)
-template <bool LUT>
-__global__ __launch_bounds__(NTHREADS) void linear_bwd_kernel(GemmParams p_in) {
+template <bool LUT, class E>
+__global__ __launch_bounds__(NTHREADS) void linear_bwd_kernel(GemmParams p_in, E epi) {
     extern __shared__ __align__(16) uint8_t smem[];
     const uint32_t smem_lds = (uint32_t)(uintptr_t)(lptr_t)smem;
     auto lds_of = [&](const uint8_t* q) -> uint32_t { return smem_lds + (uint32_t)(q - smem); };
@@ -684,7 +716,7 @@ __global__ __launch_bounds__(NTHREADS) void linear_bwd_kernel(GemmParams p_in) {
         }
         for (; kt < nt_all; ++kt) slow_step_lut(std::false_type{}, std::integral_constant<int, -1>{}, kt);
         if (nsplit > 1) store_out_f32(acc, p.split_out + ((size_t)split * (ntiles - p.split_first) + (tile - p.split_first)) * (BM * BN), BN, BM, BN, 0, 0);
-        else store_out(acc, p.out, p.K, p.M, p.K, m0, k0);
+        else bwd_store(acc, p, epi, m0, k0, smem);
         return;
     }
 
@@ -754,12 +786,13 @@ __global__ __launch_bounds__(NTHREADS) void linear_bwd_kernel(GemmParams p_in) {
     for (; kt < nt_all; ++kt) slow_step(kt);
 
     if (nsplit > 1) store_out_f32(acc, p.split_out + ((size_t)split * (ntiles - p.split_first) + (tile - p.split_first)) * (BM * BN), BN, BM, BN, 0, 0);
-        else store_out(acc, p.out, p.K, p.M, p.K, m0, k0);
+        else bwd_store(acc, p, epi, m0, k0, smem);
 }
 
 // dX tile = bf16(sum of its splits' partial tiles, in split order): eight workgroups per split tile, 8 outputs per thread
+template <class E>
 __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict__ part, int splits, int ntail, int first_tile,
-                                                        int tiles_k, int M, int K, uint16_t* __restrict__ out) {
+                                                        int tiles_k, int M, int K, uint16_t* out, E epi) {
     constexpr int PIECES = 8;                                      // workgroups per tile: 32 rows each
     const int tt = blockIdx.x / PIECES, piece = blockIdx.x % PIECES;
     const int tile = first_tile + tt;
@@ -773,30 +806,37 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict_
             const float4 u = src[0], v = src[1];
             a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w; b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
         }
-        *reinterpret_cast<uint4*>(out + (size_t)(m0 + r) * K + k0 + c) =
-            make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y), pack_bf16x2(b.z, b.w));
+        float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        const size_t at = (size_t)(m0 + r) * K + k0 + c;
+        if constexpr (std::is_same<E, BwdEpi>::value) {
+            EpiRun<BwdEpi, 8> run;
+            epi_load<8>(epi, at, run);
+            with_act(epi.act, [&](auto A) __attribute__((always_inline)) { epi_store<decltype(A)::value, 8>(epi, at, v, v, run, out); });
+        } else {
+            store_run<8>(out + at, v);
+        }
     }
 }
 
-hipError_t launch_gemm_bwd(const GemmParams& p, hipStream_t st) {
-    static const hipError_t attr0 = hipFuncSetAttribute(reinterpret_cast<const void*>(linear_bwd_kernel<false>),
-                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBwdSmem);
-    static const hipError_t attr1 = hipFuncSetAttribute(reinterpret_cast<const void*>(linear_bwd_kernel<true>),
-                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBwdSmem);
-    if (attr0 != hipSuccess) return attr0;
-    if (attr1 != hipSuccess) return attr1;
+template <bool LUT, class E>
+static hipError_t launch_bwd_kernel(const GemmParams& p, dim3 grid, const E& epi, hipStream_t st) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(linear_bwd_kernel<LUT, E>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBwdSmem);
+    if (attr != hipSuccess) return attr;
+    linear_bwd_kernel<LUT, E><<<grid, dim3(NTHREADS), kBwdSmem, st>>>(p, epi);
+    return hipGetLastError();
+}
+template <class E>
+static hipError_t launch_bwd(const GemmParams& p, const E& epi, hipStream_t st) {
     const int tiles_k = (p.K + BN - 1) / BN, ntiles = tiles_k * ((p.M + BM - 1) / BM);
     const int ntail = p.splits > 1 ? ntiles - p.split_first : 0;
     const dim3 grid(p.splits > 1 ? p.split_first + ntail * p.splits : ntiles);
-    if (p.any4)
-        linear_bwd_kernel<true><<<grid, dim3(NTHREADS), kBwdSmem, st>>>(p);
-    else
-        linear_bwd_kernel<false><<<grid, dim3(NTHREADS), kBwdSmem, st>>>(p);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = p.any4 ? launch_bwd_kernel<true>(p, grid, epi, st) : launch_bwd_kernel<false>(p, grid, epi, st);
     if (e != hipSuccess || p.splits <= 1) return e;
-    split_sum_kernel<<<dim3(ntail * 8), dim3(256), 0, st>>>(p.split_out, p.splits, ntail, p.split_first, tiles_k, p.M, p.K, p.out);
+    split_sum_kernel<E><<<dim3(ntail * 8), dim3(256), 0, st>>>(p.split_out, p.splits, ntail, p.split_first, tiles_k, p.M, p.K, p.out, epi);
     return hipGetLastError();
 }
+hipError_t launch_gemm_bwd(const GemmParams& p, const BwdEpi* epi, hipStream_t st) { return epi ? launch_bwd(p, *epi, st) : launch_bwd(p, NoEpi{}, st); }
 
 // Which output tiles of the input gradient share their contraction, and between how many workgroups: the tiles of the
 // last round of workgroups when that round would fill at most half of the compute units (all tiles when there is

@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "epilogue.h"
 #include "gemm_mid.h"
 
 namespace lowra {
@@ -93,8 +94,8 @@ __host__ __device__ constexpr PairInfo pair_info(int q) {
 }
 
 // One output tile: channels [n0, n0 + 256) x token rows [m0, m0 + 32 TM).
-template <int TM>
-__device__ __forceinline__ void fwd_tile(const GemmParams& p, const int n0, const int m0, uint8_t* smem) {
+template <int TM, class E>
+__device__ __forceinline__ void fwd_tile(const GemmParams& p, const E& epi, const int n0, const int m0, uint8_t* smem) {
     static_assert(TM == 8 || TM == 6 || TM == 4, "token tiles of 256, 192 or 128 rows");
     constexpr int kStepTransfers = step_transfers(TM);
     constexpr int WROWS = 8 * TM;            // token rows a wavefront moves per activation tile (8 per transfer)
@@ -637,6 +638,44 @@ __device__ __forceinline__ void fwd_tile(const GemmParams& p, const int n0, cons
             }
     }
 
+    // ---- an epilogue (epilogue.h): 128 token rows at a time go through LDS as fp32, so that every operand is read and every
+    // result written in 16 contiguous bytes, by a thread that keeps its columns
+    if constexpr (std::is_same<E, FwdEpi>::value) {
+        static_assert(128 * 1024 <= kFwdSmem, "128 rows of 256 fp32");
+        const int c = tid & 31, r0 = tid >> 5;
+        auto pass = [&](auto T0_) __attribute__((always_inline)) {
+            constexpr int t0 = decltype(T0_)::value, t1 = TM < t0 + 4 ? TM : t0 + 4;
+            __syncthreads();                                       // the last readers of what is overwritten are done
+#pragma unroll
+            for (int tn = 0; tn < 2; ++tn)
+#pragma unroll
+                for (int vq = 0; vq < 4; ++vq) {
+                    if (natural) {
+#pragma unroll
+                        for (int tm = t0; tm < t1; ++tm)
+                            *reinterpret_cast<float4*>(smem + epi_chunk<64>(32 * (tm - t0) + fi, wave * 16 + 8 * tn + 2 * vq + fkg)) =
+                                make_float4(acc[tn][tm][4 * vq], acc[tn][tm][4 * vq + 1], acc[tn][tm][4 * vq + 2], acc[tn][tm][4 * vq + 3]);
+                    } else {
+                        const uint2 o = *reinterpret_cast<const uint2*>(p.tile_order + n0 + wave * 64 + 32 * tn + 8 * vq + 4 * fkg);
+                        const int col[4] = {(int)(o.x & 0xffffu), (int)(o.x >> 16), (int)(o.y & 0xffffu), (int)(o.y >> 16)};
+#pragma unroll
+                        for (int tm = t0; tm < t1; ++tm)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                *reinterpret_cast<float*>(smem + epi_chunk<64>(32 * (tm - t0) + fi, col[e] >> 2) + (col[e] & 3) * 4) = acc[tn][tm][4 * vq + e];
+                    }
+                }
+            __syncthreads();
+            if (n0 + 8 * c < p.N) {                                // N is a multiple of 8: a chunk is in or out as a whole
+                auto read = [&](int i, float (&v)[8]) __attribute__((always_inline)) { epi_read8<64>(smem, i * 8 + r0, c, v); };
+                epi_rows<8, 4 * (t1 - t0)>(epi, p.out, p.N, p.M, m0 + 32 * t0 + r0, n0 + 8 * c, read);
+            }
+        };
+        pass(int_c<0>{});
+        if constexpr (TM > 4) pass(int_c<4>{});
+        return;
+    }
+
     // ---- epilogue: the tile goes through LDS so that every global store is 16 contiguous bytes.
     // Accumulator register v of tile (tn, tm): channel position 32 tn + 8 (v/4) + 4 fkg + v%4 of my
     // 64, token row 32 tm + fi.  In natural row order four registers are four adjacent columns.
@@ -692,16 +731,16 @@ struct FwdPlan {
     int tiles_a;              // workgroups of region A
 };
 
-template <int TMA, int TMB>
-__global__ __launch_bounds__(NTHREADS) void linear_fwd_kernel(GemmParams p, FwdPlan plan) {
+template <int TMA, int TMB, class E>
+__global__ __launch_bounds__(NTHREADS) void linear_fwd_kernel(GemmParams p, FwdPlan plan, E epi) {
     extern __shared__ __align__(16) uint8_t smem[];
     const int bid = blockIdx.x;
     if (TMA == TMB || bid < plan.tiles_a) {              // uniform
         const int tile = xcd_tile(bid, TMA == TMB ? (int)gridDim.x : plan.tiles_a);
-        fwd_tile<TMA>(p, (tile % plan.cols_a) * BN, (tile / plan.cols_a) * (32 * TMA), smem);
+        fwd_tile<TMA>(p, epi, (tile % plan.cols_a) * BN, (tile / plan.cols_a) * (32 * TMA), smem);
     } else if constexpr (TMA != TMB) {
         const int tile = xcd_tile(bid - plan.tiles_a, (int)gridDim.x - plan.tiles_a);
-        fwd_tile<TMB>(p, (plan.cols_a + tile % plan.cols_b) * BN, (tile / plan.cols_b) * (32 * TMB), smem);
+        fwd_tile<TMB>(p, epi, (plan.cols_a + tile % plan.cols_b) * BN, (tile / plan.cols_b) * (32 * TMB), smem);
     }
 }
 
@@ -759,9 +798,9 @@ double gemm_fwd_steps(int N, int K, int M, double enough) {
     return steps * cost;
 }
 
-template <int TMA, int TMB>
-static hipError_t launch_fwd_variant(const GemmParams& p, const FwdChoice& c, hipStream_t st) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(linear_fwd_kernel<TMA, TMB>),
+template <int TMA, int TMB, class E>
+static hipError_t launch_fwd_kernel(const GemmParams& p, const FwdChoice& c, const E& epi, hipStream_t st) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(linear_fwd_kernel<TMA, TMB, E>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)kFwdSmem);
     if (attr != hipSuccess) return attr;
     const int cols = (p.N + BN - 1) / BN;
@@ -770,8 +809,12 @@ static hipError_t launch_fwd_variant(const GemmParams& p, const FwdChoice& c, hi
     plan.cols_b = cols - plan.cols_a;
     plan.tiles_a = plan.cols_a * ((p.M + 32 * TMA - 1) / (32 * TMA));
     const int tiles_b = plan.cols_b * ((p.M + 32 * TMB - 1) / (32 * TMB));
-    linear_fwd_kernel<TMA, TMB><<<dim3(plan.tiles_a + tiles_b), dim3(NTHREADS), kFwdSmem, st>>>(p, plan);
+    linear_fwd_kernel<TMA, TMB, E><<<dim3(plan.tiles_a + tiles_b), dim3(NTHREADS), kFwdSmem, st>>>(p, plan, epi);
     return hipGetLastError();
+}
+template <int TMA, int TMB>
+static hipError_t launch_fwd_variant(const GemmParams& p, const FwdChoice& c, const FwdEpi* epi, hipStream_t st) {
+    return epi ? launch_fwd_kernel<TMA, TMB>(p, c, *epi, st) : launch_fwd_kernel<TMA, TMB>(p, c, NoEpi{}, st);
 }
 
 // the planner's choice for N channels, M tokens and `units` compute units, as token-tile heights and column count
@@ -782,20 +825,20 @@ void plan_fwd_tiling(int N, int M, int units, int* rows_a, int* rows_b, int* col
 }
 
 // `tiling`: -1 lets the planner choose; else TMA << 8 | TMB << 4 | cols_a << 12 (test and measurement hook)
-hipError_t launch_gemm_fwd(const GemmParams& p, int tiling, hipStream_t st) {
+hipError_t launch_gemm_fwd(const GemmParams& p, int tiling, const FwdEpi* epi, hipStream_t st) {
     const FwdChoice c = plan_fwd(p.N, p.M, tiling);
     const int key = c.tma * 10 + c.tmb;
     const bool split = c.tma != c.tmb && c.cols_a > 0 && c.cols_a < (p.N + BN - 1) / BN;
     if (!split) {
         const int tm = c.tma != c.tmb && c.cols_a == 0 ? c.tmb : c.tma;
-        if (tm == 8) return launch_fwd_variant<8, 8>(p, c, st);
-        if (tm == 6) return launch_fwd_variant<6, 6>(p, c, st);
-        if (tm == 4) return launch_fwd_variant<4, 4>(p, c, st);
+        if (tm == 8) return launch_fwd_variant<8, 8>(p, c, epi, st);
+        if (tm == 6) return launch_fwd_variant<6, 6>(p, c, epi, st);
+        if (tm == 4) return launch_fwd_variant<4, 4>(p, c, epi, st);
         return hipErrorInvalidValue;
     }
-    if (key == 86) return launch_fwd_variant<8, 6>(p, c, st);
-    if (key == 84) return launch_fwd_variant<8, 4>(p, c, st);
-    if (key == 64) return launch_fwd_variant<6, 4>(p, c, st);
+    if (key == 86) return launch_fwd_variant<8, 6>(p, c, epi, st);
+    if (key == 84) return launch_fwd_variant<8, 4>(p, c, epi, st);
+    if (key == 64) return launch_fwd_variant<6, 4>(p, c, epi, st);
     return hipErrorInvalidValue;
 }
 

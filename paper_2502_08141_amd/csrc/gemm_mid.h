@@ -46,6 +46,7 @@ inline int mid_pieces(const MidPlan& pl, size_t room) {
     return fit == 0 || (tiles + fit - 1) / fit > (size_t)kMidPieces ? 0 : (int)((tiles + fit - 1) / fit);
 }
 
-hipError_t launch_gemm_mid(const MidParams& p, int op, int TM, bool wide, hipStream_t st);
+// an epilogue of the forward's or of the input gradient's kind, or null
+hipError_t launch_gemm_mid(const MidParams& p, int op, int TM, bool wide, const FwdEpi* fwd, const BwdEpi* bwd, hipStream_t st);
 
 }  // namespace lowra

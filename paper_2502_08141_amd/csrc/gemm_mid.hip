@@ -13,6 +13,7 @@
 #include <atomic>
 #include <type_traits>
 
+#include "epilogue.h"
 #include "gemm_mid.h"
 
 namespace lowra {
@@ -73,10 +74,14 @@ __device__ __forceinline__ bf16x8_t narrow8(uint32_t cw, uint32_t SL, uint32_t S
     return frag_of(d[0], d[1], d[2], d[3]);
 }
 
+// tiles of 32 tokens that an epilogue stages at a time: a divisor of TM, 16 KB each in what the kernels hold (12 KB TM and more)
+constexpr int mid_epi_tiles(int TM) { return TM == 6 ? 3 : TM == 4 ? 2 : TM == 2 ? 2 : 1; }
+
 // What both kernels do at the end.  Accumulator register v of token tile t: column 32 wave + 8 (v/4) + 4 (lane/32) + v%4,
 // token 32 t + lane%32.
-template <int TM>
-__device__ __forceinline__ void mid_epilogue(const MidParams& p, const floatx16_t (&acc)[TM], uint8_t* smem, int wave, int lane,
+// With an epilogue (epilogue.h) PT tiles of 32 tokens at a time go through LDS as fp32 (16 KB each).
+template <int TM, class E>
+__device__ __forceinline__ void mid_epilogue(const MidParams& p, const E& epi, const floatx16_t (&acc)[TM], uint8_t* smem, int wave, int lane,
                                              int split, int tile, int c0, int m0, int cols) {
     const int fi = lane & 31, h = lane >> 5;
     if (p.splits > 1) {
@@ -87,6 +92,25 @@ __device__ __forceinline__ void mid_epilogue(const MidParams& p, const floatx16_
 #pragma unroll
             for (int vq = 0; vq < 4; ++vq)
                 dst[(t * 4 + vq) * 64] = make_float4(acc[t][4 * vq], acc[t][4 * vq + 1], acc[t][4 * vq + 2], acc[t][4 * vq + 3]);
+        return;
+    }
+    if constexpr (!std::is_same<E, NoEpi>::value) {
+        constexpr int PT = mid_epi_tiles(TM);
+        const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+#pragma unroll
+        for (int t0 = 0; t0 < TM; t0 += PT) {
+            __syncthreads();
+#pragma unroll
+            for (int t = t0; t < t0 + PT; ++t)
+#pragma unroll
+                for (int vq = 0; vq < 4; ++vq)
+                    *reinterpret_cast<float4*>(smem + epi_chunk<32>(32 * (t - t0) + fi, wave * 8 + 2 * vq + h)) =
+                        make_float4(acc[t][4 * vq], acc[t][4 * vq + 1], acc[t][4 * vq + 2], acc[t][4 * vq + 3]);
+            __syncthreads();
+            if (c0 + 8 * c < cols)                                    // cols is a multiple of 8
+                epi_rows<16, 2 * PT>(epi, p.out, cols, p.M, m0 + 32 * t0 + r0, c0 + 8 * c,
+                                     [&](int i, float (&v)[8]) __attribute__((always_inline)) { epi_read8<32>(smem, i * 16 + r0, c, v); });
+        }
         return;
     }
     __syncthreads();
@@ -138,10 +162,11 @@ struct FwdLds {
     static constexpr int BYTES = CODE0 + 4 * CODE;
 };
 
-template <int TM, bool WIDE, bool ODD>
-__global__ __launch_bounds__(MID_THREADS, 2) void mid_fwd_kernel(MidParams p) {
+template <int TM, bool WIDE, bool ODD, class E>
+__global__ __launch_bounds__(MID_THREADS, 2) void mid_fwd_kernel(MidParams p, E epi) {
     extern __shared__ __align__(16) uint8_t smem[];
     using L = FwdLds<TM, WIDE, ODD>;
+    static_assert(mid_epi_tiles(TM) * 16384 <= L::BYTES, "an epilogue's stage");
     constexpr int STAGE = L::STAGE, NP = L::NP;
     const uint32_t smem_lds = (uint32_t)(uintptr_t)(lptr_t)smem;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -406,7 +431,7 @@ __global__ __launch_bounds__(MID_THREADS, 2) void mid_fwd_kernel(MidParams p) {
             }
         }
     }
-    mid_epilogue<TM>(p, acc, smem, wave, lane, split, tile - p.tile0, n0, m0, p.N);
+    mid_epilogue<TM>(p, epi, acc, smem, wave, lane, split, tile - p.tile0, n0, m0, p.N);
 }
 
 // ---- input gradient.  The contraction runs over channels while codes are packed along k (gemm_bwd.hip): a step's
@@ -431,10 +456,11 @@ struct BwdLds {
 // tokens: VALU 30 % of a wavefront's life, LDS busy 40 % of the unit's, a quarter of that in conflicts).  So a step is one run
 // of instructions without branches (68.0 -> 64.2 us; 4096 x 1024, 777 tokens 30.3 -> 28.6), and tiles of 192 tokens halve the
 // decode of those of 96 (68.7 -> 63.2).
-template <int TM, bool WIDE, bool SHARED>
-__global__ __launch_bounds__(MID_THREADS, 2) void mid_bwd_kernel(MidParams p) {
+template <int TM, bool WIDE, bool SHARED, class E>
+__global__ __launch_bounds__(MID_THREADS, 2) void mid_bwd_kernel(MidParams p, E epi) {
     extern __shared__ __align__(16) uint8_t smem[];
     using L = BwdLds<TM, WIDE>;
+    static_assert(mid_epi_tiles(TM) * 16384 <= L::TAB0, "an epilogue's stage");
     constexpr int ROWTAB = WIDE ? 64 : 16;                            // bytes of a row's staged levels
     const uint32_t smem_lds = (uint32_t)(uintptr_t)(lptr_t)smem;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -684,12 +710,13 @@ __global__ __launch_bounds__(MID_THREADS, 2) void mid_bwd_kernel(MidParams p) {
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // transfers past the end: none may land in the output stage
-    mid_epilogue<TM>(p, acc, smem, wave, lane, split, tile - p.tile0, k0, m0, K);
+    mid_epilogue<TM>(p, epi, acc, smem, wave, lane, split, tile - p.tile0, k0, m0, K);
 }
 
 // out = bf16(sum of the splits' partial tiles, in split order).  A thread owns four columns of one token.
+template <class E>
 __global__ __launch_bounds__(256) void mid_sum_kernel(const float4* __restrict__ part, int splits, int ntiles, int tile0, int tiles_c, int TM,
-                                                      int M, int cols, uint16_t* __restrict__ out) {
+                                                      int M, int cols, uint16_t* out, E epi) {
     const size_t per = (size_t)ntiles * TM * 1024;                    // float4 per split
     const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (e >= per) return;
@@ -708,46 +735,57 @@ __global__ __launch_bounds__(256) void mid_sum_kernel(const float4* __restrict__
     const int q = (int)(e >> 8), t = q % TM, wt = q / TM, wave = wt & 3, tile = tile0 + (wt >> 2);
     const int col = (tile % tiles_c) * MID_COLS + 32 * wave + 8 * vq + 4 * (lane >> 5);
     const int m = (tile / tiles_c) * (32 * TM) + 32 * t + (lane & 31);
-    if (m < M && col < cols) *reinterpret_cast<uint2*>(out + (size_t)m * cols + col) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+    if (m >= M || col >= cols) return;
+    const size_t at = (size_t)m * cols + col;
+    float v[4] = {a.x, a.y, a.z, a.w};
+    if constexpr (std::is_same<E, NoEpi>::value) {
+        store_run<4>(out + at, v);
+    } else {
+        EpiRun<E, 4> run;
+        float b[4];
+        epi_load<4>(epi, at, run);
+        epi_bias<4>(epi, col, b);
+        with_act(epi.act, [&](auto A) __attribute__((always_inline)) { epi_store<decltype(A)::value, 4>(epi, at, v, b, run, out); });
+    }
 }
 
-template <int TM, bool WIDE, bool ODD>
-hipError_t launch_mid_fwd(const MidParams& p, unsigned grid, hipStream_t st) {
+template <int TM, bool WIDE, bool ODD, class E>
+hipError_t launch_mid_fwd(const MidParams& p, const E& epi, hipStream_t st) {
     constexpr int sh = FwdLds<TM, WIDE, ODD>::BYTES;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(mid_fwd_kernel<TM, WIDE, ODD>), hipFuncAttributeMaxDynamicSharedMemorySize, sh);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(mid_fwd_kernel<TM, WIDE, ODD, E>), hipFuncAttributeMaxDynamicSharedMemorySize, sh);
     if (attr != hipSuccess) return attr;
-    mid_fwd_kernel<TM, WIDE, ODD><<<dim3(grid), dim3(MID_THREADS), sh, st>>>(p);
+    mid_fwd_kernel<TM, WIDE, ODD, E><<<dim3((unsigned)(p.ntiles * p.splits)), dim3(MID_THREADS), sh, st>>>(p, epi);
     return hipGetLastError();
 }
 
-template <int TM, bool WIDE>
-hipError_t launch_mid_fwd_any(const MidParams& p, hipStream_t st) {
-    const unsigned grid = (unsigned)(p.ntiles * p.splits);
-    return (p.G & 1) ? launch_mid_fwd<TM, WIDE, true>(p, grid, st) : launch_mid_fwd<TM, WIDE, false>(p, grid, st);
-}
-
-template <int TM, bool WIDE, bool SHARED>
-hipError_t launch_mid_bwd(const MidParams& p, unsigned grid, hipStream_t st) {
+template <int TM, bool WIDE, bool SHARED, class E>
+hipError_t launch_mid_bwd(const MidParams& p, const E& epi, hipStream_t st) {
     using L = BwdLds<TM, WIDE>;
     constexpr int most = L::TAB0 + 2 * 64 * (WIDE ? 64 : 16);
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(mid_bwd_kernel<TM, WIDE, SHARED>), hipFuncAttributeMaxDynamicSharedMemorySize, most);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(mid_bwd_kernel<TM, WIDE, SHARED, E>), hipFuncAttributeMaxDynamicSharedMemorySize, most);
     if (attr != hipSuccess) return attr;
     const int sh = SHARED ? L::TAB0 + p.C * kTableStride * 4 : most;
     static_assert(kMidLutBooks * kTableStride * 4 <= 2 * 64 * 64, "either table scheme fits the region");
-    mid_bwd_kernel<TM, WIDE, SHARED><<<dim3(grid), dim3(MID_THREADS), sh, st>>>(p);
+    mid_bwd_kernel<TM, WIDE, SHARED, E><<<dim3((unsigned)(p.ntiles * p.splits)), dim3(MID_THREADS), sh, st>>>(p, epi);
     return hipGetLastError();
 }
 
+// op 0: the forward.  With an epilogue and splits the partial tiles' sum has it, and these kernels are the ones without.
 template <int TM, bool WIDE>
-hipError_t launch_mid_variant(const MidParams& p, int op, hipStream_t st) {
-    const unsigned grid = (unsigned)(p.ntiles * p.splits);
+hipError_t launch_mid_variant(const MidParams& p, int op, const FwdEpi* fwd, const BwdEpi* bwd, hipStream_t st) {
+    const bool has = (fwd || bwd) && p.splits <= 1;
     if (op == 0) {
-        return launch_mid_fwd_any<TM, WIDE>(p, st);
-    } else {
-        const bool shared = WIDE && p.C <= kMidLutBooks;
-        const hipError_t e = shared ? launch_mid_bwd<TM, WIDE, WIDE>(p, grid, st) : launch_mid_bwd<TM, WIDE, false>(p, grid, st);
-        if (e != hipSuccess) return e;
+        if (p.G & 1) return has ? launch_mid_fwd<TM, WIDE, true>(p, *fwd, st) : launch_mid_fwd<TM, WIDE, true>(p, NoEpi{}, st);
+        return has ? launch_mid_fwd<TM, WIDE, false>(p, *fwd, st) : launch_mid_fwd<TM, WIDE, false>(p, NoEpi{}, st);
     }
+    if (WIDE && p.C <= kMidLutBooks) return has ? launch_mid_bwd<TM, WIDE, WIDE>(p, *bwd, st) : launch_mid_bwd<TM, WIDE, WIDE>(p, NoEpi{}, st);
+    return has ? launch_mid_bwd<TM, WIDE, false>(p, *bwd, st) : launch_mid_bwd<TM, WIDE, false>(p, NoEpi{}, st);
+}
+
+template <class E>
+hipError_t launch_mid_sum(const MidParams& p, int TM, int cols, const E& epi, hipStream_t st) {
+    mid_sum_kernel<E><<<dim3((unsigned)((size_t)p.ntiles * TM * 4)), dim3(256), 0, st>>>(reinterpret_cast<const float4*>(p.part), p.splits, p.ntiles, p.tile0,
+                                                                                        p.tiles_c, TM, p.M, cols, p.out, epi);
     return hipGetLastError();
 }
 
@@ -843,7 +881,7 @@ MidPlan plan_mid(int op, int N, int K, int M, bool wide, int C, size_t part_byte
     return best;
 }
 
-hipError_t launch_gemm_mid(const MidParams& p_in, int op, int TM, bool wide, hipStream_t st) {
+hipError_t launch_gemm_mid(const MidParams& p_in, int op, int TM, bool wide, const FwdEpi* fwd, const BwdEpi* bwd, hipStream_t st) {
     MidParams p = p_in;
     const int tiles = p.tiles_c * p.tiles_m, cols = op == 0 ? p.N : p.K;
     const int fit = p.splits > 1 ? (int)std::min<size_t>(p.part_bytes / mid_tile_bytes(p.splits, TM), (size_t)tiles) : tiles;
@@ -852,16 +890,15 @@ hipError_t launch_gemm_mid(const MidParams& p_in, int op, int TM, bool wide, hip
     for (p.tile0 = 0; p.tile0 < tiles; p.tile0 += per) {
         p.ntiles = std::min(per, tiles - p.tile0);
         hipError_t e = hipErrorInvalidValue;
-        if (TM == 1) e = wide ? launch_mid_variant<1, true>(p, op, st) : launch_mid_variant<1, false>(p, op, st);
-        if (TM == 2) e = wide ? launch_mid_variant<2, true>(p, op, st) : launch_mid_variant<2, false>(p, op, st);
-        if (TM == 3) e = wide ? launch_mid_variant<3, true>(p, op, st) : launch_mid_variant<3, false>(p, op, st);
-        if (TM == 4) e = wide ? launch_mid_variant<4, true>(p, op, st) : launch_mid_variant<4, false>(p, op, st);
-        if (TM == 6) e = wide ? launch_mid_variant<6, true>(p, op, st) : launch_mid_variant<6, false>(p, op, st);
+        if (TM == 1) e = wide ? launch_mid_variant<1, true>(p, op, fwd, bwd, st) : launch_mid_variant<1, false>(p, op, fwd, bwd, st);
+        if (TM == 2) e = wide ? launch_mid_variant<2, true>(p, op, fwd, bwd, st) : launch_mid_variant<2, false>(p, op, fwd, bwd, st);
+        if (TM == 3) e = wide ? launch_mid_variant<3, true>(p, op, fwd, bwd, st) : launch_mid_variant<3, false>(p, op, fwd, bwd, st);
+        if (TM == 4) e = wide ? launch_mid_variant<4, true>(p, op, fwd, bwd, st) : launch_mid_variant<4, false>(p, op, fwd, bwd, st);
+        if (TM == 6) e = wide ? launch_mid_variant<6, true>(p, op, fwd, bwd, st) : launch_mid_variant<6, false>(p, op, fwd, bwd, st);
         if (e != hipSuccess) return e;
         if (p.splits <= 1) continue;
-        mid_sum_kernel<<<dim3((unsigned)((size_t)p.ntiles * TM * 4)), dim3(256), 0, st>>>(reinterpret_cast<const float4*>(p.part), p.splits, p.ntiles, p.tile0,
-                                                                                         p.tiles_c, TM, p.M, cols, p.out);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = fwd ? launch_mid_sum(p, TM, cols, *fwd, st) : bwd ? launch_mid_sum(p, TM, cols, *bwd, st) : launch_mid_sum(p, TM, cols, NoEpi{}, st);
+        if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }

@@ -38,6 +38,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "epilogue.h"
 #include "gemm_common.h"
 #include "gemv_t.h"
 
@@ -84,9 +85,22 @@ constexpr int GV_FIXED = 16 * GV_TABROW + 16 * GV_LEV * 4 + 64;      // LDS in f
 constexpr int gemv_t_parts(int W, int PER, int RT, bool fuse) { return RT == 0 ? 0 : fuse ? W : PER > 1 && 16 * RT < W * 64 ? W * 64 / (16 * RT) : 1; }
 constexpr int gemv_t_bytes(int W, int PER, int RT, bool fuse) { return gemv_t_parts(W, PER, RT, fuse) * 16 * RT * (PER > 1 || fuse ? 4 : 2); }
 
+// one output: token m, channel n
+__device__ __forceinline__ void gemv_store(const GemvParams& p, NoEpi, int m, int n, float v) {
+    p.y[(size_t)m * p.N + n] = (uint16_t)(pack_bf16x2(v, 0.0f) & 0xffffu);
+}
+__device__ __forceinline__ void gemv_store(const GemvParams& p, const FwdEpi& epi, int m, int n, float v) {
+    const size_t at = (size_t)m * p.N + n;
+    EpiRun<FwdEpi, 1> run;
+    float b[1], o[1] = {v};
+    epi_load<1>(epi, at, run);
+    epi_bias<1>(epi, n, b);
+    with_act(epi.act, [&](auto A) __attribute__((always_inline)) { epi_store<decltype(A)::value, 1>(epi, at, o, b, run, p.y); });
+}
+
 // FUSE: t comes from the workgroup itself (one round, r <= 16); else from the partial sums in p.tp
-template <int W, int PER, bool FUSE>
-__device__ __forceinline__ void gemv_body(const GemvParams& p, const int strip) {
+template <int W, int PER, bool FUSE, class E>
+__device__ __forceinline__ void gemv_body(const GemvParams& p, const E& epi, const int strip) {
     static_assert(!FUSE || PER == 1, "a wavefront forms t beside the products of its only block");
     extern __shared__ __align__(16) uint8_t gv_smem[];
     // LDS: pair tables [16 channels][GV_TABROW bytes] | levels [16][GV_LEV] | channel numbers [16] | t: sums [tparts][16 tokens][RT] or bf16 [16][RT] |
@@ -372,7 +386,7 @@ __device__ __forceinline__ void gemv_body(const GemvParams& p, const int strip) 
         if (row_ok) {
 #pragma unroll
             for (int v = 0; v < 4; ++v)
-                if (4 * kg + v < p.M) p.y[(size_t)(4 * kg + v) * p.N + nc] = (uint16_t)(pack_bf16x2(tot[v], 0.0f) & 0xffffu);
+                if (4 * kg + v < p.M) gemv_store(p, epi, 4 * kg + v, nc, tot[v]);
         }
         return;
     }
@@ -381,14 +395,14 @@ __device__ __forceinline__ void gemv_body(const GemvParams& p, const int strip) 
         if (m < p.M && n >= 0) {
             float v = 0.0f;
             for (int w = 0; w < waves; ++w) v += reinterpret_cast<const float*>(gv_smem + X0 + w * XPIECE)[o];
-            p.y[(size_t)m * p.N + n] = (uint16_t)(pack_bf16x2(v, 0.0f) & 0xffffu);
+            gemv_store(p, epi, m, n, v);
         }
     }
 }
 
-template <int W, int PER, bool FUSE>
-__global__ __launch_bounds__(W * 64) void gemv_fwd_kernel(GemvParams p) {
-    gemv_body<W, PER, FUSE>(p, blockIdx.x);
+template <int W, int PER, bool FUSE, class E>
+__global__ __launch_bounds__(W * 64) void gemv_fwd_kernel(GemvParams p, E epi) {
+    gemv_body<W, PER, FUSE>(p, epi, blockIdx.x);
 }
 // every matrix of a batch that takes this instantiation, in one launch: workgroup = one 16-channel strip of one matrix
 template <int W, int PER, bool FUSE>
@@ -396,7 +410,7 @@ __global__ __launch_bounds__(W * 64) void gemv_fwd_batch_kernel(const GemvParams
                                                                 const int* __restrict__ owner) {
     const int m = owner[blockIdx.x];
     const GemvParams p = descs[m];
-    gemv_body<W, PER, FUSE>(p, (int)blockIdx.x - strip0[m]);
+    gemv_body<W, PER, FUSE>(p, NoEpi{}, (int)blockIdx.x - strip0[m]);
 }
 
 struct GemvChoice { int W, PER, fuse; };
@@ -419,22 +433,15 @@ static size_t gemv_lds(GemvParams& p) {
     p.tparts = gemv_t_parts(W, PER, p.RT, FUSE);
     return gemv_lds(p, GemvChoice{W, PER, FUSE}, &p.xbufs);
 }
-template <int W, int PER, bool FUSE>
-static hipError_t gemv_attr() {
-    static hipError_t a0 = hipFuncSetAttribute(reinterpret_cast<const void*>(gemv_fwd_kernel<W, PER, FUSE>),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    static hipError_t a1 = hipFuncSetAttribute(reinterpret_cast<const void*>(gemv_fwd_batch_kernel<W, PER, FUSE>),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    return a0 != hipSuccess ? a0 : a1;
-}
-template <int W, int PER, bool FUSE>
-static hipError_t launch_one(GemvParams p, hipStream_t st) {
-    const hipError_t attr = gemv_attr<W, PER, FUSE>();
+static hipError_t gemv_attr(const void* kernel) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); }
+template <int W, int PER, bool FUSE, class E>
+static hipError_t launch_one(GemvParams p, const E& epi, hipStream_t st) {
+    static const hipError_t attr = gemv_attr(reinterpret_cast<const void*>(gemv_fwd_kernel<W, PER, FUSE, E>));
     if (attr != hipSuccess) return attr;
     const size_t sh = gemv_lds<W, PER, FUSE>(p);
     if (sh == 0) return hipErrorInvalidValue;
     const dim3 grid((p.N + 15) / 16);
-    gemv_fwd_kernel<W, PER, FUSE><<<grid, dim3(W * 64), sh, st>>>(p);
+    gemv_fwd_kernel<W, PER, FUSE, E><<<grid, dim3(W * 64), sh, st>>>(p, epi);
     return hipGetLastError();
 }
 
@@ -545,18 +552,20 @@ static hipError_t gemv_dispatch(GemvChoice c, F&& f) {
     return hipErrorInvalidValue;
 }
 struct LaunchSingle {
-    const GemvParams& p; hipStream_t st;
-    template <int W, int PER, bool FUSE> hipError_t operator()() const { return launch_one<W, PER, FUSE>(p, st); }
+    const GemvParams& p; const FwdEpi* epi; hipStream_t st;
+    template <int W, int PER, bool FUSE> hipError_t operator()() const {
+        return epi ? launch_one<W, PER, FUSE>(p, *epi, st) : launch_one<W, PER, FUSE>(p, NoEpi{}, st);
+    }
 };
 
-hipError_t launch_gemv_fwd(const GemvParams& p, hipStream_t st) {
+hipError_t launch_gemv_fwd(const GemvParams& p, const FwdEpi* epi, hipStream_t st) {
     const GemvChoice c = gemv_choose(p, (p.N + 15) / 16);
     if (p.RT > 0 && !c.fuse) {
         gemv_t_partial_kernel<<<dim3((p.G + 3) / 4), dim3(64), 0, st>>>(p.x, p.M, p.K, p.A, p.r, p.RT, p.tp);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    return gemv_dispatch(c, LaunchSingle{p, st});
+    return gemv_dispatch(c, LaunchSingle{p, epi, st});
 }
 
 // Which kernel a batch takes: estimated times, fits to 13824 batches (the projections of layers of nine sizes, 1024 x 2816 to
@@ -626,7 +635,7 @@ double gemv_stream_batch_us(const std::vector<GemvParams>& items, const std::vec
 struct PrepareDesc {
     GemvParams& p; size_t& sh;
     template <int W, int PER, bool FUSE> hipError_t operator()() const {
-        const hipError_t attr = gemv_attr<W, PER, FUSE>();
+        static const hipError_t attr = gemv_attr(reinterpret_cast<const void*>(gemv_fwd_batch_kernel<W, PER, FUSE>));
         if (attr != hipSuccess) return attr;
         sh = gemv_lds<W, PER, FUSE>(p);
         return sh ? hipSuccess : hipErrorInvalidValue;

@@ -23,6 +23,7 @@
 #include <cmath>
 #include <cstddef>
 
+#include "epilogue.h"
 #include "gemv_stream.h"
 
 namespace lowra {
@@ -509,7 +510,8 @@ __device__ __forceinline__ void gb_sum_flat_body(const GbItem* __restrict__ it, 
 // (64 consecutive columns of one token): thread (ql, sl) adds the slots sl, sl + 16, ... and the ranks sl, sl + 16
 // of quad ql; the 16 partial sums of a quad meet in LDS and are added in order (a fixed assignment: the result does
 // not depend on timing).
-__device__ __forceinline__ void gb_sum_body(const GbItem* __restrict__ it, const int blk, const int nblk) {
+template <class E>
+__device__ __forceinline__ void gb_sum_body(const GbItem* __restrict__ it, const E& epi, const int blk, const int nblk) {
     __shared__ float u[GS_TROW];
     __shared__ float4 red[16][16];
     const int M = it->M, K = it->K, r = it->r;
@@ -546,7 +548,15 @@ __device__ __forceinline__ void gb_sum_body(const GbItem* __restrict__ it, const
             float4 t = red[0][ql];
 #pragma unroll
             for (int w = 1; w < 16; ++w) { const float4 q = red[w][ql]; t.x += q.x; t.y += q.y; t.z += q.z; t.w += q.w; }
-            gstore_u2(dX + (size_t)m * K + k, make_uint2(pack_bf16x2(t.x, t.y), pack_bf16x2(t.z, t.w)));
+            if constexpr (std::is_same<E, BwdEpi>::value) {
+                float o[4] = {t.x, t.y, t.z, t.w};
+                const size_t at = (size_t)m * K + k;
+                EpiRun<BwdEpi, 4> run;
+                epi_load<4>(epi, at, run);
+                with_act(epi.act, [&](auto A) __attribute__((always_inline)) { epi_store<decltype(A)::value, 4>(epi, at, o, o, run, it->dX); });
+            } else {
+                gstore_u2(dX + (size_t)m * K + k, make_uint2(pack_bf16x2(t.x, t.y), pack_bf16x2(t.z, t.w)));
+            }
         }
     }
 }
@@ -555,8 +565,9 @@ __global__ __launch_bounds__(GB_PRE_WAVES * 64) void gemv_stream_bwd_pre_kernel(
     const GbPre it = items[blockIdx.x / P];                       // a copy: the body's stores cannot alias it
     gb_pre_body(it, blockIdx.x % P, P);
 }
-__global__ __launch_bounds__(256) void gemv_stream_bwd_sum_kernel(const GbItem* __restrict__ items, int per_item_blocks) {
-    gb_sum_body(items + blockIdx.x / per_item_blocks, blockIdx.x % per_item_blocks, per_item_blocks);
+template <class E>
+__global__ __launch_bounds__(256) void gemv_stream_bwd_sum_kernel(const GbItem* __restrict__ items, int per_item_blocks, E epi) {
+    gb_sum_body(items + blockIdx.x / per_item_blocks, epi, blockIdx.x % per_item_blocks, per_item_blocks);
 }
 template <int MT>
 __global__ __launch_bounds__(256) void gemv_stream_bwd_sum_flat_kernel(const GbItem* __restrict__ items, int per_item_blocks) {
@@ -714,7 +725,8 @@ hipError_t launch_gemv_stream_bwd(const lowra_layout& L, const LinearArgs& a, hi
                                                                                        a.mappings, tabs, part, a.M);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int blocks = std::max(1, std::min(2 * gs_compute_units(), a.M * L.K / 64));
-    gemv_stream_bwd_sum_kernel<<<dim3(blocks), dim3(256), 0, st>>>(sg.d_item, blocks);
+    if (a.bwd_epi) gemv_stream_bwd_sum_kernel<<<dim3(blocks), dim3(256), 0, st>>>(sg.d_item, blocks, *a.bwd_epi);
+    else gemv_stream_bwd_sum_kernel<<<dim3(blocks), dim3(256), 0, st>>>(sg.d_item, blocks, NoEpi{});
     return hipGetLastError();
 }
 
@@ -850,7 +862,7 @@ hipError_t gemv_stream_bwd_batch_run(const GbBatch& b, hipStream_t st) {
         else gemv_stream_bwd_sum_flat_kernel<16><<<dim3(b.nitems * blocks), dim3(256), 0, st>>>(items, blocks);
     } else {
         const int blocks = std::max(1, std::min(64, b.max_quads / 16));
-        gemv_stream_bwd_sum_kernel<<<dim3(b.nitems * blocks), dim3(256), 0, st>>>(static_cast<const GbItem*>(b.d_items), blocks);
+        gemv_stream_bwd_sum_kernel<<<dim3(b.nitems * blocks), dim3(256), 0, st>>>(static_cast<const GbItem*>(b.d_items), blocks, NoEpi{});
     }
     return hipGetLastError();
 }

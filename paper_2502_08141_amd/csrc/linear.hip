@@ -10,14 +10,15 @@
 #include <atomic>
 #include <new>
 
+#include "epilogue.h"
 #include "gemm_mid.h"
 
 namespace lowra {
 
-hipError_t launch_gemm_fwd(const GemmParams& p, int tiling, hipStream_t st);
-hipError_t launch_gemm_bwd(const GemmParams& p, hipStream_t st);
+hipError_t launch_gemm_fwd(const GemmParams& p, int tiling, const FwdEpi* epi, hipStream_t st);
+hipError_t launch_gemm_bwd(const GemmParams& p, const BwdEpi* epi, hipStream_t st);
 BwdSplitPlan gemm_bwd_split_plan(int N, int K, int M);
-hipError_t launch_gemv_fwd(const GemvParams& p, hipStream_t st);
+hipError_t launch_gemv_fwd(const GemvParams& p, const FwdEpi* epi, hipStream_t st);
 hipError_t launch_skinny_ws(const uint16_t* P, int ldp, int M, const uint16_t* Q, int ldq, int r, int Kc,
                             float s, uint16_t* out, int RP, float* scratch, bool split, float* few, hipStream_t st);
 size_t skinny_scratch_bytes(int M, int Kc, int RP);
@@ -177,15 +178,16 @@ static size_t gemv_workspace_bytes(const lowra_layout& L, int r) {
 hipError_t launch_linear_fwd(const lowra_layout& L, const LinearArgs& a_in, int path, int tiling, hipStream_t st) {
     if (a_in.M == 0 || L.N == 0) return hipSuccess;
     LinearArgs a;
+    const bool stream = path == 1 && !a_in.fwd_epi && gemv_stream_supported(L, a_in.M, a_in.r);      // (no epilogue there)
     // LOWRA_PATH_GEMM and a forced tiling keep the 256-column kernels
     const MidPlan mid = mid_plan_call(L, a_in, 0, path != 2 && tiling < 0);
-    hipError_t e_scales = with_fp32_scales(L, 0, a_in, a, mid.TM > 0 || (path == 1 && gemv_stream_supported(L, a_in.M, a_in.r)), st);
+    hipError_t e_scales = with_fp32_scales(L, 0, a_in, a, mid.TM > 0 || stream, st);
     if (e_scales != hipSuccess) return e_scales;
     const int RP = a.r > 0 ? round_up(a.r, BK) : 0;
     // A single matrix is too little work for the streaming kernel's set-up (descriptor kernel, tables, pipeline fill):
     // measured 20-50 us per call against 15-25 us for the general kernel.  It runs here only when asked for
     // (LOWRA_PATH_GEMV); the batched entry point is where it pays.
-    if (path == 1 && gemv_stream_supported(L, a.M, a.r)) {
+    if (stream) {
         KernelTimer timer(st);
         return launch_gemv_stream(L, a, st);
     }
@@ -196,7 +198,7 @@ hipError_t launch_linear_fwd(const lowra_layout& L, const LinearArgs& a_in, int 
         g.y = a.out; g.s = a.s;
         g.M = a.M; g.N = L.N; g.K = L.K; g.G = L.G; g.r = a.r; g.RT = a.r > 0 ? round_up(a.r, 16) : 0;
         KernelTimer timer(st);
-        return launch_gemv_fwd(g, st);
+        return launch_gemv_fwd(g, a.fwd_epi, st);
     }
     uint16_t* ws_t = static_cast<uint16_t*>(a.workspace);
     if (RP) {
@@ -207,7 +209,7 @@ hipError_t launch_linear_fwd(const lowra_layout& L, const LinearArgs& a_in, int 
     }
     if (mid.TM > 0) {
         KernelTimer timer(st);
-        return launch_gemm_mid(mid_params(L, a, 0, RP, ws_t, mid, linear_workspace_min(L, 0, a.M, a.r)), 0, mid.TM, L.n_by_bits[4] > 0, st);
+        return launch_gemm_mid(mid_params(L, a, 0, RP, ws_t, mid, linear_workspace_min(L, 0, a.M, a.r)), 0, mid.TM, L.n_by_bits[4] > 0, a.fwd_epi, nullptr, st);
     }
     GemmParams p;
     fill_params(p, L, a, RP);
@@ -222,7 +224,7 @@ hipError_t launch_linear_fwd(const lowra_layout& L, const LinearArgs& a_in, int 
         }
     }
     KernelTimer timer(st);
-    return launch_gemm_fwd(p, tiling, st);
+    return launch_gemm_fwd(p, tiling, a.fwd_epi, st);
 }
 
 hipError_t launch_linear_bwd_input(const lowra_layout& L, const LinearArgs& a_in, int path, hipStream_t st) {
@@ -265,8 +267,8 @@ hipError_t launch_linear_bwd_input(const lowra_layout& L, const LinearArgs& a_in
     }
     KernelTimer timer(st);
     if (mid.TM > 0)
-        return launch_gemm_mid(mid_params(L, a, 1, RP, p.ext_act, mid, linear_workspace_min(L, 1, a.M, a.r)), 1, mid.TM, L.n_by_bits[4] > 0, st);
-    return launch_gemm_bwd(p, st);
+        return launch_gemm_mid(mid_params(L, a, 1, RP, p.ext_act, mid, linear_workspace_min(L, 1, a.M, a.r)), 1, mid.TM, L.n_by_bits[4] > 0, nullptr, a.bwd_epi, st);
+    return launch_gemm_bwd(p, a.bwd_epi, st);
 }
 
 }  // namespace lowra

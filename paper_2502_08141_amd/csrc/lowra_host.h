@@ -149,6 +149,8 @@ hipError_t gemv_batch_build(std::vector<GemvParams>& items, lowra_fwd_batch& b);
 hipError_t gemv_batch_run(const lowra_fwd_batch& b, hipStream_t st);
 void gemv_batch_free(lowra_fwd_batch& b);
 
+struct FwdEpi;
+struct BwdEpi;
 struct LinearArgs {
     const uint8_t* packed;
     const float* absmax;
@@ -163,6 +165,8 @@ struct LinearArgs {
     void* workspace;
     size_t workspace_bytes;
     bool pieces = false;   // short of room for partial tiles: the whole plan in pieces, not one with fewer splits
+    const FwdEpi* fwd_epi = nullptr;       // the forward's epilogue (epilogue.h)
+    const BwdEpi* bwd_epi = nullptr;       // the input gradient's
 };
 // bf16 group scales -> fp32 (exact), for the kernels that read fp32 scales
 hipError_t launch_expand_scales(const uint16_t* src, size_t count, float* dst, hipStream_t st);

@@ -25,6 +25,8 @@ OP_LINEAR_FWD, OP_LINEAR_BWD_INPUT, OP_ADAPTER_GRADS, OP_LOFTQ_INIT = 0, 1, 2, 3
 OUT_BF16, OUT_FP32 = 0, 1
 PATH_AUTO, PATH_GEMV, PATH_GEMM, PATH_GEMV_GENERAL = 0, 1, 2, 3
 SCALE_FP32, SCALE_BF16 = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
 
 SYMBOLS = [
     "lowra_status_string", "lowra_plan_rows", "lowra_layout_create", "lowra_layout_destroy", "lowra_layout_set_scale_dtype",
@@ -35,6 +37,7 @@ SYMBOLS = [
     "lowra_adapter_grads", "lowra_linear_side_product", "lowra_adapter_grads_from_side", "lowra_loftq_init",
     "lowra_fwd_batch_workspace_bytes", "lowra_fwd_batch_create", "lowra_fwd_batch_run", "lowra_fwd_batch_destroy",
     "lowra_bwd_batch_workspace_bytes", "lowra_bwd_batch_create", "lowra_bwd_batch_run", "lowra_bwd_batch_destroy",
+    "lowra_linear_fwd_act", "lowra_linear_bwd_input_act", "lowra_act_bwd", "lowra_act_bwd_workspace_bytes",
     "lowra_measure_copy", "lowra_measure_read", "lowra_measure_mfma", "lowra_measure_mfma_random",
 ]
 
@@ -43,6 +46,16 @@ class FwdItem(C.Structure):
     """lowra_fwd_item: one matrix of a batched small-token forward (device pointers)."""
     _fields_ = [("layout", C.c_void_p), ("packed", C.c_void_p), ("absmax", C.c_void_p), ("x", C.c_void_p),
                 ("A", C.c_void_p), ("B", C.c_void_p), ("y", C.c_void_p)]
+
+
+class FwdEpilogue(C.Structure):
+    """lowra_fwd_epilogue (device pointers)."""
+    _fields_ = [("act", C.c_int), ("bias", C.c_void_p), ("mul", C.c_void_p), ("residual", C.c_void_p), ("z", C.c_void_p)]
+
+
+class BwdEpilogue(C.Structure):
+    """lowra_bwd_epilogue (device pointers)."""
+    _fields_ = [("act", C.c_int), ("z", C.c_void_p), ("mul", C.c_void_p), ("residual", C.c_void_p), ("dmul", C.c_void_p)]
 
 
 class LowraError(RuntimeError):
@@ -79,6 +92,11 @@ def lib() -> C.CDLL:
         L.lowra_linear_fwd.argtypes = lin
         L.lowra_linear_bwd_input.argtypes = lin
         L.lowra_linear_fwd_static.argtypes = lin[:11] + [vp]
+        L.lowra_linear_fwd_act.argtypes = lin[:10] + [vp] + lin[10:]
+        L.lowra_linear_bwd_input_act.argtypes = lin[:10] + [vp] + lin[10:]
+        L.lowra_act_bwd_workspace_bytes.restype = C.c_size_t
+        L.lowra_act_bwd_workspace_bytes.argtypes = [C.c_int, C.c_int]
+        L.lowra_act_bwd.argtypes = [C.c_int, C.c_int, C.c_int, u16p, u16p, u16p, u16p, u16p, f32p, vp, C.c_size_t, vp]
         L.lowra_learn_tables.argtypes = [vp, f32p, f32p, f32p, C.c_int, f32p, f32p, f32p, vp]
         L.lowra_average_thresholds.argtypes = [vp, f32p, vp]
         L.lowra_adapter_grads.argtypes = [vp, u16p, u16p, C.c_int, u16p, u16p, C.c_int, C.c_float, f32p, f32p, vp, C.c_size_t, vp]
@@ -116,6 +134,7 @@ def lib() -> C.CDLL:
         spec.loader.exec_module(call)
         call.init(*(C.cast(f, C.c_void_p).value for f in (L.lowra_linear_fwd, L.lowra_linear_bwd_input, L.lowra_linear_side_product,
                                                           L.lowra_adapter_grads, L.lowra_adapter_grads_from_side, L.lowra_dequantize)))
+        call.init_act(*(C.cast(f, C.c_void_p).value for f in (L.lowra_linear_fwd_act, L.lowra_linear_bwd_input_act, L.lowra_act_bwd)))
         _lib, _call = L, call
     return _lib
 
@@ -345,6 +364,118 @@ def lowra_linear_bwd_input(layout: Layout, packed, absmax, mappings, dY, A, B, s
             return _native(res, "lowra_linear_bwd_input")
     return _linear(lib().lowra_linear_bwd_input, "lowra_linear_bwd_input", OP_LINEAR_BWD_INPUT, layout, packed,
                    absmax, mappings, dY, layout.N, layout.K, A, B, s, dX, workspace)
+
+
+def _operand(t, shape, name: str, device):
+    """An optional bf16 operand of an epilogue."""
+    if t is not None:
+        _dev(t, torch.bfloat16, name)
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: shape mismatch")
+        if t.device != device:
+            raise ValueError(f"{name}: on another device")
+    return t
+
+
+def _linear_act(fn, name, op, layout, packed, absmax, mappings, act_in, cols_in, cols, A, B, s, epilogue, out, workspace):
+    """What the two linear calls with an epilogue share: `epilogue(M)` checks the operands and gives their record."""
+    _state(layout, packed, absmax, mappings)
+    _dev(act_in, torch.bfloat16, "activation")
+    if act_in.dim() != 2 or act_in.shape[1] != cols_in:
+        raise ValueError("activation shape mismatch")
+    if act_in.device.index != torch.cuda.current_device() or packed.device != act_in.device:
+        raise ValueError("tensors on another device than the current one")
+    M, r = int(act_in.shape[0]), 0
+    if A is not None and B is not None and A.shape[0] > 0:
+        _dev(A, torch.bfloat16, "A"); _dev(B, torch.bfloat16, "B")
+        r = int(A.shape[0])
+        if tuple(A.shape) != (r, layout.K) or tuple(B.shape) != (layout.N, r):
+            raise ValueError("LoRA operand shape mismatch")
+    else:
+        A = B = None
+    if out is None:
+        out = torch.empty((M, cols), dtype=torch.bfloat16, device=act_in.device)
+    _operand(out, (M, cols), "out", act_in.device)
+    record, second = epilogue(M)
+    if workspace is None:
+        workspace = torch.empty(layout.workspace_bytes(op, M, r), dtype=torch.uint8, device=act_in.device)
+    _dev(workspace, torch.uint8, "workspace")
+    _check(fn(layout.handle, _ptr(packed), _ptr(absmax), _ptr(mappings), _ptr(act_in), M, _ptr(A), _ptr(B), r, float(s), C.addressof(record),
+              _ptr(out), _ptr(workspace), workspace.numel(), _stream()), name)
+    return out, second
+
+
+def lowra_linear_fwd_act(layout: Layout, packed, absmax, mappings, x, A, B, s, act: int, bias=None, mul=None, residual=None, keep_z: bool = False,
+                         y=None, z=None, workspace=None):
+    """v = x What^T + s (x A^T) B^T + bias -> (y, z): y [M,N] bf16 = act(v) mul + residual, and z [M,N] bf16 = v with `keep_z` (or
+    where `z` is given), else None.  act: ACT_*; bias [N], mul and residual [M,N] bf16."""
+    if y is None and z is None and workspace is not None and layout.__class__ is Layout:
+        res = _call.linear_act(0, layout.native, packed, absmax, mappings, x, A, B, s, act, bias, mul, residual, keep_z, workspace)
+        if res is not None:
+            return _native(res, "lowra_linear_fwd_act")
+
+    def epilogue(M):
+        kept, shape = z, (M, layout.N)
+        _operand(bias, (layout.N,), "bias", x.device); _operand(mul, shape, "mul", x.device); _operand(residual, shape, "residual", x.device)
+        if kept is None and keep_z:
+            kept = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+        _operand(kept, shape, "z", x.device)
+        return FwdEpilogue(int(act), _ptr(bias), _ptr(mul), _ptr(residual), _ptr(kept)), kept
+
+    return _linear_act(lib().lowra_linear_fwd_act, "lowra_linear_fwd_act", OP_LINEAR_FWD, layout, packed, absmax, mappings, x, layout.K, layout.N,
+                       A, B, s, epilogue, y, workspace)
+
+
+def lowra_linear_bwd_input_act(layout: Layout, packed, absmax, mappings, dY, A, B, s, act: int, z=None, mul=None, residual=None, dX=None, dmul=None,
+                               workspace=None):
+    """g = dY What + s (dY B) A + residual -> (dX, dmul): dX [M,K] bf16 = g mul act'(z), and with `mul` dmul [M,K] bf16 = g act(z), else
+    None: the gradients of z and mul of the layer's input act(z) mul.  z, mul, residual: [M,K] bf16."""
+    if dX is None and dmul is None and workspace is not None and layout.__class__ is Layout:
+        res = _call.linear_act(1, layout.native, packed, absmax, mappings, dY, A, B, s, act, z, mul, residual, False, workspace)
+        if res is not None:
+            return _native(res, "lowra_linear_bwd_input_act")
+
+    def epilogue(M):
+        second, shape = dmul, (M, layout.K)
+        for t, n in ((z, "z"), (mul, "mul"), (residual, "residual")):
+            _operand(t, shape, n, dY.device)
+        if second is None and mul is not None:
+            second = torch.empty(shape, dtype=torch.bfloat16, device=dY.device)
+        _operand(second, shape, "dmul", dY.device)
+        return BwdEpilogue(int(act), _ptr(z), _ptr(mul), _ptr(residual), _ptr(second)), second
+
+    return _linear_act(lib().lowra_linear_bwd_input_act, "lowra_linear_bwd_input_act", OP_LINEAR_BWD_INPUT, layout, packed, absmax, mappings, dY,
+                       layout.N, layout.K, A, B, s, epilogue, dX, workspace)
+
+
+def lowra_act_bwd_workspace_bytes(M: int, N: int) -> int:
+    return int(lib().lowra_act_bwd_workspace_bytes(int(M), int(N)))
+
+
+def lowra_act_bwd(dY, act: int, z=None, mul=None, bias_grad: bool = False, workspace=None):
+    """dY [M,N] bf16, the gradient of act(z) mul -> (dZ, dmul, db): dZ bf16 = dY mul act'(z) (None where it would be dY), dmul bf16 =
+    dY act(z) (None without `mul`), db fp32 [N] = the sum of dZ over the tokens (None without `bias_grad`)."""
+    if workspace is not None and _lib is not None:
+        res = _call.act_bwd(dY, act, z, mul, bias_grad, workspace)
+        if res is not None:
+            return _native(res, "lowra_act_bwd")
+    _dev(dY, torch.bfloat16, "dY")
+    if dY.dim() != 2:
+        raise ValueError("dY: shape mismatch")
+    if dY.device.index != torch.cuda.current_device():
+        raise ValueError("tensors on another device than the current one")
+    shape, act = tuple(dY.shape), int(act)
+    M, N = shape
+    _operand(z, shape, "z", dY.device); _operand(mul, shape, "mul", dY.device)
+    dZ = torch.empty_like(dY) if act != ACT_NONE or mul is not None else None
+    dmul = torch.empty_like(dY) if mul is not None else None
+    db = torch.empty(N, dtype=torch.float32, device=dY.device) if bias_grad else None
+    if workspace is None:
+        workspace = torch.empty(lowra_act_bwd_workspace_bytes(M, N) if bias_grad else 0, dtype=torch.uint8, device=dY.device)
+    _dev(workspace, torch.uint8, "workspace")
+    _check(lib().lowra_act_bwd(M, N, act, _ptr(dY), _ptr(z), _ptr(mul), _ptr(dZ), _ptr(dmul), _ptr(db), _ptr(workspace), workspace.numel(), _stream()),
+           "lowra_act_bwd")
+    return dZ, dmul, db
 
 
 def lowra_learn_tables(layout: Layout, W, init_thresholds, init_mappings, iterations: int = 2):
