@@ -296,6 +296,49 @@ lowra_status lowra_adapter_grads_from_side(const lowra_layout* layout, const uin
                                            const uint16_t* st, const uint16_t* su, float* dA, float* dB,
                                            void* workspace, size_t workspace_bytes, void* stream);
 
+/* The optimiser step on the adapters with an orthogonalised update: for every matrix of a batch (A [r,K] and B [N,r] of any number
+ * of layers) with gradient g, momentum m and weight w
+ *   m' = momentum m + g;   u = g + momentum m' (nesterov) or m';   X = u / (|u| + eps), |u| the Frobenius norm;
+ *   `steps` times  X = a X + (b X X^T + c (X X^T)^2) X   (Newton-Schulz products: the singular values of X move towards one);
+ *   w' = w - lr (scale X + weight_decay w)
+ * The products run over the short side in 64 bits, whatever the gradient's spectrum; a zero gradient gives a zero update, and a
+ * NaN or an infinity stays in its own matrix.
+ * A batch fixes the matrices; a run takes the scalars, so that a schedule needs no new batch, and only launches (up to three
+ * kernels for each of the short-side classes 1..16, 17..32, 33..64 that the batch holds).  Results do not depend on what else the
+ * batch holds beyond the order of the sums.
+ *   items: host array of n entries (read during create only); device pointers, 16-byte aligned, that stay valid and in place for
+ *   the life of the batch; momentum_out may be momentum and weight_out weight (in place), nothing else overlaps an output.
+ *   workspace: dev, >= lowra_muon_batch_workspace_bytes(n, items), 16-byte aligned, owned by the caller, used by every run (runs
+ *   of one batch must not overlap).
+ * create: INVALID_ARG (null / n <= 0 / a non-positive size / a missing pointer: grad, momentum, momentum_out, and weight with
+ * weight_out or update are needed, weight_bf16 needs weight), UNSUPPORTED (a short side above 64), MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY,
+ * HIP_ERROR.  create allocates device memory for the descriptors and copies them synchronously; destroy frees.
+ * run: INVALID_ARG (null, steps outside 1..64, eps not above zero, another device than the one of create), HIP_ERROR. */
+typedef struct lowra_muon_item {
+    int rows, cols;              /* min(rows, cols) <= 64 */
+    float scale;                 /* of the update, e.g. sqrt(max(1, rows / cols)) */
+    const float* grad;           /* all [rows,cols], row-major */
+    const float* momentum;
+    float* momentum_out;
+    const float* weight;         /* null: no weights, only `update` */
+    float* weight_out;
+    uint16_t* weight_bf16;       /* w' rounded to bf16 (out), or null */
+    float* update;               /* scale X (out), or null */
+} lowra_muon_item;
+typedef struct lowra_muon_step {
+    float lr, momentum;
+    int nesterov;
+    float weight_decay;
+    int steps;
+    float a, b, c, eps;          /* e.g. 3.4445, -4.7750, 2.0315, 1e-7 */
+} lowra_muon_step;
+typedef struct lowra_muon_batch lowra_muon_batch;
+size_t lowra_muon_batch_workspace_bytes(int n, const lowra_muon_item* items);
+lowra_status lowra_muon_batch_create(int n, const lowra_muon_item* items, void* workspace, size_t workspace_bytes,
+                                     lowra_muon_batch** out);
+lowra_status lowra_muon_batch_run(const lowra_muon_batch* batch, const lowra_muon_step* step, void* stream);
+void lowra_muon_batch_destroy(lowra_muon_batch* batch);
+
 /* Alternating low-rank initialisation of the adapter (Sec. 4.1, "Using LoftQ as low-rank initializer";
  * App. D; the paper runs five steps): from B A = 0, each step quantizes W - B A with the layout's widths
  * and the given tables (step 1 therefore quantizes W itself), decodes it, and fits B A of rank r to what

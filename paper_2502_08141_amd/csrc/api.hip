@@ -8,6 +8,7 @@
 #include "../../include/lowra.h"
 #include "epilogue.h"
 #include "gemm_mid.h"
+#include "muon.h"
 
 namespace {
 
@@ -717,6 +718,81 @@ lowra_status lowra_bwd_batch_run(const lowra_bwd_batch* b, void* stream) {
 void lowra_bwd_batch_destroy(lowra_bwd_batch* b) {
     if (!b) return;
     lowra::gemv_stream_bwd_batch_free(b->gb);
+    delete b;
+}
+
+// ---- the orthogonalised adapter update
+static bool muon_sizes(const lowra_muon_item& it) { return it.rows > 0 && it.cols > 0 && std::min(it.rows, it.cols) <= lowra::kMuonMaxShort; }
+static lowra::MuonItem muon_item(const lowra_muon_item& it) {
+    lowra::MuonItem m{};
+    m.grad = it.grad; m.momentum = it.momentum; m.weight = it.weight;
+    m.momentum_out = it.momentum_out; m.weight_out = it.weight_out; m.update = it.update; m.weight_bf16 = it.weight_bf16;
+    m.wide = it.rows <= it.cols;
+    m.R = std::min(it.rows, it.cols); m.L = std::max(it.rows, it.cols);
+    m.scale = it.scale;
+    return m;
+}
+
+size_t lowra_muon_batch_workspace_bytes(int n, const lowra_muon_item* items) {
+    if (n <= 0 || !items) return 0;
+    try {
+        std::vector<lowra::MuonItem> v;
+        for (int i = 0; i < n; ++i) {
+            if (!muon_sizes(items[i])) return 0;
+            v.push_back(muon_item(items[i]));
+        }
+        return lowra::muon_workspace_bytes(n, v.data());
+    } catch (...) {
+        return 0;
+    }
+}
+
+lowra_status lowra_muon_batch_create(int n, const lowra_muon_item* items, void* workspace, size_t workspace_bytes, lowra_muon_batch** out) {
+    if (!out) return LOWRA_INVALID_ARG;
+    *out = nullptr;
+    if (n <= 0 || !items) return LOWRA_INVALID_ARG;
+    for (int i = 0; i < n; ++i) {
+        const lowra_muon_item& it = items[i];
+        if (it.rows <= 0 || it.cols <= 0) return LOWRA_INVALID_ARG;
+        if (!muon_sizes(it)) return LOWRA_UNSUPPORTED;
+        if (!it.grad || !it.momentum || !it.momentum_out || (!it.weight && !it.update)) return LOWRA_INVALID_ARG;
+        if ((it.weight != nullptr) != (it.weight_out != nullptr) || (it.weight_bf16 && !it.weight)) return LOWRA_INVALID_ARG;
+        if (!aligned16(it.grad) || !aligned16(it.momentum) || !aligned16(it.momentum_out) || !aligned16(it.weight) || !aligned16(it.weight_out) ||
+            !aligned16(it.weight_bf16) || !aligned16(it.update))
+            return LOWRA_MISALIGNED;
+    }
+    if (!workspace) return LOWRA_INVALID_ARG;
+    if (!aligned16(workspace)) return LOWRA_MISALIGNED;
+    lowra_muon_batch* b = nullptr;
+    lowra_status st = LOWRA_OK;
+    try {
+        std::vector<lowra::MuonItem> v;
+        for (int i = 0; i < n; ++i) v.push_back(muon_item(items[i]));
+        if (workspace_bytes < lowra::muon_workspace_bytes(n, v.data())) return LOWRA_WORKSPACE_TOO_SMALL;
+        b = new lowra_muon_batch;
+        if (hipGetDevice(&b->device) != hipSuccess || lowra::muon_build(v, workspace, b->groups) != hipSuccess) st = LOWRA_HIP_ERROR;
+    } catch (const std::bad_alloc&) {
+        st = LOWRA_OUT_OF_MEMORY;
+    } catch (...) {
+        st = LOWRA_INVALID_ARG;
+    }
+    if (st != LOWRA_OK) { (void)hipGetLastError(); lowra_muon_batch_destroy(b); return st; }
+    *out = b;
+    return LOWRA_OK;
+}
+
+lowra_status lowra_muon_batch_run(const lowra_muon_batch* b, const lowra_muon_step* s, void* stream) {
+    if (!b || !s || s->steps < 1 || s->steps > 64 || !(s->eps > 0.0f)) return LOWRA_INVALID_ARG;
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return LOWRA_HIP_ERROR;
+    if (dev != b->device) return LOWRA_INVALID_ARG;
+    const lowra::MuonStep m{s->lr, s->momentum, s->weight_decay, s->a, s->b, s->c, s->eps, s->nesterov != 0, s->steps};
+    return lowra::muon_run(b->groups, m, static_cast<hipStream_t>(stream)) == hipSuccess ? LOWRA_OK : LOWRA_HIP_ERROR;
+}
+
+void lowra_muon_batch_destroy(lowra_muon_batch* b) {
+    if (!b) return;
+    lowra::muon_free(b->groups);
     delete b;
 }
 

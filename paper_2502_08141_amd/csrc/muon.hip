@@ -1,0 +1,437 @@
+// The optimiser step on the adapters (Sec. 2.1: only A and B are trained) with an orthogonalised update:
+//   m' = beta m + g;  u = g + beta m' (Nesterov) or m';  X = u / (|u| + eps);  `steps` times X = a X + (b X X^T + c (X X^T)^2) X;
+//   w' = w - lr (scale X + decay w)
+//
+// An adapter has one short side R <= 64 (its rank) and one long side L.  The products never touch the long side twice: with
+// G = u u^T over the long side, R x R, every X is p(G) u for a polynomial p, and the Gram matrix of X is G p(G)^2.  So a step is
+//   1. one pass over g and m that writes m' and adds up G,
+//   2. the iteration on R x R matrices, one workgroup per adapter,
+//   3. one pass that multiplies p(G) with u and updates the weights.
+//
+// Precision.  A direction of u that is small beside the largest grows by a = 3.4 in every step, 485 in five, and an error of G
+// by a^2 in every step: in 32 bits X would be off by 1e-4 and more where the direct products are off by 1e-6 (R = 64, singular
+// values over three decades).  G, its polynomial and the products are in 64 bits (off by 3e-13), on v_mfma_f64_16x16x4: 32 multiply-adds
+// per element and 16 ranks in each pass are a quarter of what the memory takes at R = 16, half at R = 64.
+//
+// Layouts of v_mfma_f64_16x16x4: A[i][k] and B[k][i] in lane i + 16 k; D[row][column] in lane column + 16 q, register v, with row = q + 4 v.
+#include <algorithm>
+#include <new>
+
+#include "gemm_common.h"
+#include "muon.h"
+
+namespace lowra {
+
+namespace {
+
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f64x4_t mfma64(double a, double b, f64x4_t c) { return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0); }
+
+constexpr int MU_SPAN = 256;             // long-side elements that a workgroup of either pass takes at a time
+constexpr int MU_THREADS = 256;
+
+// NT: 16-wide tiles of the short side (1, 2 or 4).  Gram matrices are symmetric: tiles (t1, t2), t1 <= t2.
+constexpr int mu_tiles(int NT) { return NT * (NT + 1) / 2; }
+constexpr int mu_tile(int NT, int t1, int t2) { return t1 * NT - t1 * (t1 - 1) / 2 + (t2 - t1); }
+constexpr int mu_ld(int NT) { return 16 * NT + 2; }          // doubles per LDS row: 16 rows at one column lie 4 banks apart
+
+// four fp32 from element e on, of which the first n exist; vec: whole quads are 16-byte aligned and all there
+__device__ __forceinline__ float4 load4(const float* p, bool vec, int n) {
+    if (vec) return n > 0 ? *reinterpret_cast<const float4*>(p) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    return make_float4(n > 0 ? p[0] : 0.0f, n > 1 ? p[1] : 0.0f, n > 2 ? p[2] : 0.0f, n > 3 ? p[3] : 0.0f);
+}
+__device__ __forceinline__ void store4(float* p, bool vec, int n, float4 v) {
+    if (vec) { if (n > 0) *reinterpret_cast<float4*>(p) = v; return; }
+    if (n > 0) p[0] = v.x;
+    if (n > 1) p[1] = v.y;
+    if (n > 2) p[2] = v.z;
+    if (n > 3) p[3] = v.w;
+}
+__device__ __forceinline__ float at4(const float4& v, int e) { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; }
+
+struct Momentum { float beta; int nesterov; };
+// m' and u of one element
+__device__ __forceinline__ float momentum_of(const Momentum& mo, float g, float m) { return __builtin_fmaf(mo.beta, m, g); }
+__device__ __forceinline__ float update_of(const Momentum& mo, float g, float m1) { return mo.nesterov ? __builtin_fmaf(mo.beta, m1, g) : m1; }
+
+// ---- 1. momentum and Gram matrix.  A wavefront's step: operands of four products (k sets of four long-side elements) per tile.
+// Short side in rows (A): lane (i, q) loads row 16 t + i, columns c + 4 q .. + 3; product e contracts columns c + 4 q + e.
+// Short side in columns (B): lane (i, q) loads row c + q, NT columns from NT i on; tile e holds columns NT i + e: a permutation that
+// the second kernel undoes.
+template <int NT>
+__global__ __launch_bounds__(MU_THREADS) void muon_gram_kernel(const MuonItem* __restrict__ items, const MuonChunk* __restrict__ chunks, Momentum mo,
+                                                               double* __restrict__ part) {
+    constexpr int TILES = mu_tiles(NT);
+    __shared__ double red[3][TILES][256];
+    const MuonItem it = items[chunks[blockIdx.x].item];
+    const long long first = chunks[blockIdx.x].first, last = chunks[blockIdx.x].last;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    const int R = it.R;
+    f64x4_t acc[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) acc[t] = f64x4_t{0.0, 0.0, 0.0, 0.0};
+    auto multiply = [&](const double (&a)[NT]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t1 = 0; t1 < NT; ++t1)
+#pragma unroll
+            for (int t2 = t1; t2 < NT; ++t2) acc[mu_tile(NT, t1, t2)] = mfma64(a[t1], a[t2], acc[mu_tile(NT, t1, t2)]);
+    };
+    if (it.wide) {
+        const bool vec = (it.L & 3) == 0;
+        for (long long c = first + 16 * wave; c < last; c += 64) {
+            const long long col = c + 4 * q;
+            const int n = (int)min(max(last - col, 0ll), 4ll);
+            float4 u[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const bool ok = 16 * t + i < R;
+                const size_t e = (size_t)(ok ? 16 * t + i : 0) * it.L + col;
+                const int m = ok ? n : 0;
+                const float4 g = load4(it.grad + e, vec, m), o = load4(it.momentum + e, vec, m);
+                const float4 m1 = make_float4(momentum_of(mo, g.x, o.x), momentum_of(mo, g.y, o.y), momentum_of(mo, g.z, o.z), momentum_of(mo, g.w, o.w));
+                store4(it.momentum_out + e, vec, m, m1);
+                u[t] = make_float4(update_of(mo, g.x, m1.x), update_of(mo, g.y, m1.y), update_of(mo, g.z, m1.z), update_of(mo, g.w, m1.w));
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                double a[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) a[t] = (double)at4(u[t], e);
+                multiply(a);
+            }
+        }
+    } else {
+        for (long long c = first + 4 * wave; c < last; c += 16) {
+            const long long row = c + q;
+            double a[NT];
+#pragma unroll
+            for (int e = 0; e < NT; ++e) {
+                const bool ok = row < last && NT * i + e < R;
+                const size_t at = ok ? (size_t)row * R + NT * i + e : 0;
+                const float g = ok ? it.grad[at] : 0.0f, o = ok ? it.momentum[at] : 0.0f, m1 = momentum_of(mo, g, o);
+                if (ok) it.momentum_out[at] = m1;
+                a[e] = (double)update_of(mo, g, m1);
+            }
+            multiply(a);
+        }
+    }
+    // the wavefronts' sums, in order
+    if (wave > 0) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) red[wave - 1][t][v * 64 + lane] = acc[t][v];
+    }
+    __syncthreads();
+    if (wave == 0) {
+        double* dst = part + (size_t)blockIdx.x * (TILES * 256);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int o = v * 64 + lane;
+                dst[t * 256 + o] = ((acc[t][v] + red[0][t][o]) + red[1][t][o]) + red[2][t][o];
+            }
+    }
+}
+
+// ---- 2. the iteration.  Positions of a Gram matrix: tile t, place i is element 16 t + i of the short side (A) or NT i + t (B).
+// The polynomial is handed on in the order in which the third kernel's lanes want it: as it is (A), or with place p of a tile
+// holding element 4 (p % 4) + p / 4 (B).
+template <int NT>
+__global__ __launch_bounds__(NT == 4 ? 1024 : NT == 2 ? 512 : 256) void muon_iterate_kernel(const MuonItem* __restrict__ items, const double* __restrict__ part,
+                                                                                            double* __restrict__ poly, int steps, double ca, double cb,
+                                                                                            double cc, double eps) {
+    constexpr int TILES = mu_tiles(NT), LD = mu_ld(NT), RP = 16 * NT, WAVES = NT == 4 ? 16 : NT == 2 ? 8 : 4;
+    static_assert(TILES <= WAVES, "a wavefront has one tile of a product at most");
+    extern __shared__ __align__(16) uint8_t smem[];
+    double* G = reinterpret_cast<double*>(smem);
+    double *P = G + RP * LD, *Q = P + RP * LD, *T = Q + RP * LD;
+    const MuonItem it = items[blockIdx.x];
+    const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // tile (t1, t2) of a symmetric matrix from its accumulators, both halves
+    auto place = [&](double* M, int t1, int t2, int o, double x) __attribute__((always_inline)) {      // o: v * 64 + lane
+        const int r = 16 * t1 + ((o >> 4) & 3) + 4 * (o >> 6), c = 16 * t2 + (o & 15);
+        if (r <= c) { M[r * LD + c] = x; M[c * LD + r] = x; }        // (the two halves of a product differ by their rounding)
+    };
+    const double* src = part + (size_t)it.chunk0 * (TILES * 256);
+    for (int o = threadIdx.x; o < TILES * 256; o += WAVES * 64) {
+        double x = 0.0;
+        for (int k = 0; k < it.nchunks; ++k) x += src[(size_t)k * (TILES * 256) + o];
+        int t1 = 0, rest = o >> 8;
+        while (rest >= NT - t1) { rest -= NT - t1; ++t1; }
+        place(G, t1, t1 + rest, o & 255, x);
+    }
+    __syncthreads();
+    double trace = 0.0;
+#pragma unroll
+    for (int r = 0; r < RP; ++r) trace += G[r * LD + r];
+    const double norm = 1.0 / (sqrt(trace) + eps);
+    __syncthreads();
+    for (int o = threadIdx.x; o < RP * RP; o += WAVES * 64) G[(o / RP) * LD + o % RP] *= norm * norm;
+    __syncthreads();
+
+    // tile (t1, t2) of the product of two symmetric matrices that commute
+    auto product = [&](const double* X, const double* Y, int t1, int t2) __attribute__((always_inline)) {
+        f64x4_t c = {0.0, 0.0, 0.0, 0.0};
+        const double *x = X + (16 * t1 + i) * LD + q, *y = Y + (16 * t2 + i) * LD + q;
+#pragma unroll
+        for (int k = 0; k < RP; k += 4) c = mfma64(x[k], y[k], c);
+        return c;
+    };
+    auto tiles = [&](int job, int& t1, int& t2) __attribute__((always_inline)) {
+        t1 = 0;
+        while (job >= NT - t1) { job -= NT - t1; ++t1; }
+        t2 = t1 + job;
+    };
+    for (int s = 0; s < steps; ++s) {
+        const bool more = s + 1 < steps;
+        for (int job = wave; job < TILES; job += WAVES) {            // Q = a + b G + c G^2; P = Q in the first step
+            int t1, t2;
+            tiles(job, t1, t2);
+            const f64x4_t g2 = product(G, G, t1, t2);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int r = 16 * t1 + q + 4 * v, c = 16 * t2 + i;
+                const double x = cc * g2[v] + cb * G[r * LD + c] + (r == c ? ca : 0.0);
+                place(Q, t1, t2, v * 64 + lane, x);
+                if (s == 0) place(P, t1, t2, v * 64 + lane, x);
+            }
+        }
+        __syncthreads();
+        f64x4_t pn = {0.0, 0.0, 0.0, 0.0};                            // a tile of the new P: kept until everyone has read the old one
+        int p1 = -1, p2 = 0;
+        for (int job = wave; job < 2 * TILES; job += WAVES) {        // T = G Q, and P Q (at most one tile of it for a wavefront)
+            int t1, t2;
+            if (job < TILES) {
+                if (!more) continue;
+                tiles(job, t1, t2);
+                const f64x4_t x = product(G, Q, t1, t2);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) place(T, t1, t2, v * 64 + lane, x[v]);
+            } else if (s > 0) {
+                tiles(job - TILES, p1, p2);
+                pn = product(P, Q, p1, p2);
+            }
+        }
+        __syncthreads();
+        if (p1 >= 0) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) place(P, p1, p2, v * 64 + lane, pn[v]);
+        }
+        if (more) {
+            for (int job = wave; job < TILES; job += WAVES) {        // G = T Q
+                int t1, t2;
+                tiles(job, t1, t2);
+                const f64x4_t x = product(T, Q, t1, t2);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) place(G, t1, t2, v * 64 + lane, x[v]);
+            }
+        }
+        __syncthreads();
+    }
+    double* dst = poly + (size_t)blockIdx.x * (RP * RP);
+    auto position = [&](int p) {                                     // where the element that belongs at place p of the third kernel's order is
+        if (it.wide) return p;
+        const int e = (p & ~15) | (4 * (p & 3) + ((p >> 2) & 3));
+        return 16 * (e % NT) + e / NT;
+    };
+    for (int o = threadIdx.x; o < RP * RP; o += WAVES * 64) dst[o] = P[position(o / RP) * LD + position(o % RP)] * norm;
+}
+
+// ---- 3. X = p(G) u and the weights.  A wavefront takes 64 long-side elements: four operands o of 16, products k over the short side.
+// Short side in rows: lane (x, q) holds rows 16 t + q + 4 v, columns 4 x .. + 3; operand o is column 4 x + o, k set (t, v) the rows
+// 16 t + 4 v + q.  Results (row q + 4 v of a tile, column x) land where the lane's own elements are.
+// Short side in columns: lane (x, q) holds row 16 o + x, columns 16 t + 4 q .. + 3; k set (t, e) the columns 16 t + 4 q + e, and with the
+// rows of the polynomial in the same order (place p: element 4 (p % 4) + p / 4) the results again land there.
+struct MuonScalars { float lr, decay; };
+template <int NT>
+__global__ __launch_bounds__(MU_THREADS) void muon_apply_kernel(const MuonItem* __restrict__ items, const MuonChunk* __restrict__ chunks, Momentum mo,
+                                                                const double* __restrict__ poly, MuonScalars sc) {
+    constexpr int LD = mu_ld(NT), RP = 16 * NT;
+    __shared__ double P[RP * LD];
+    const int item = chunks[blockIdx.x].item;
+    const MuonItem it = items[item];
+    const long long first = chunks[blockIdx.x].first, last = chunks[blockIdx.x].last;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 15, q = lane >> 4;
+    const int R = it.R;
+    for (int o = threadIdx.x; o < RP * RP; o += MU_THREADS) P[(o / RP) * LD + o % RP] = poly[(size_t)item * (RP * RP) + o];
+    __syncthreads();
+    const bool vec = ((it.wide ? it.L : (long long)R) & 3) == 0;
+    for (long long c = first + 64 * wave; c < last; c += MU_SPAN) {
+        // quad (t, j): wide: row 16 t + q + 4 j, columns c + 4 x; else row c + 16 j + x, columns 16 t + 4 q
+        auto where = [&](int t, int j, size_t& e) __attribute__((always_inline)) -> int {              // elements there
+            if (it.wide) {
+                const int r = 16 * t + q + 4 * j;
+                const long long col = c + 4 * x;
+                const bool ok = r < R && col < last;
+                e = ok ? (size_t)r * it.L + col : 0;
+                return ok ? (int)min(last - col, 4ll) : 0;
+            }
+            const long long r = c + 16 * j + x;
+            const int col = 16 * t + 4 * q;
+            const bool ok = r < last && col < R;
+            e = ok ? (size_t)r * R + col : 0;
+            return ok ? min(R - col, 4) : 0;
+        };
+        float4 u[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                size_t e;
+                const int n = where(t, j, e);
+                const float4 m1 = load4(it.momentum_out + e, vec, n);
+                u[t][j] = m1;
+                if (mo.nesterov) {
+                    const float4 g = load4(it.grad + e, vec, n);
+                    u[t][j] = make_float4(update_of(mo, g.x, m1.x), update_of(mo, g.y, m1.y), update_of(mo, g.z, m1.z), update_of(mo, g.w, m1.w));
+                }
+            }
+#pragma unroll
+        for (int to = 0; to < NT; ++to) {
+            float4 w[4];
+            if (it.weight) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    size_t e;
+                    const int n = where(to, j, e);
+                    w[j] = load4(it.weight + e, vec, n);
+                }
+            }
+            f64x4_t acc[4];
+#pragma unroll
+            for (int o = 0; o < 4; ++o) acc[o] = f64x4_t{0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const double p = P[(16 * to + x) * LD + 16 * t + 4 * k + q];
+#pragma unroll
+                    for (int o = 0; o < 4; ++o) acc[o] = mfma64(p, (double)(it.wide ? at4(u[t][k], o) : at4(u[t][o], k)), acc[o]);
+                }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                size_t e;
+                const int n = where(to, j, e);
+                float4 y;
+                if (it.wide) y = make_float4((float)acc[0][j], (float)acc[1][j], (float)acc[2][j], (float)acc[3][j]);
+                else y = make_float4((float)acc[j][0], (float)acc[j][1], (float)acc[j][2], (float)acc[j][3]);
+                y.x *= it.scale; y.y *= it.scale; y.z *= it.scale; y.w *= it.scale;
+                if (it.update) store4(it.update + e, vec, n, y);
+                if (it.weight) {
+                    const float4 v = make_float4(w[j].x - sc.lr * __builtin_fmaf(sc.decay, w[j].x, y.x), w[j].y - sc.lr * __builtin_fmaf(sc.decay, w[j].y, y.y),
+                                                 w[j].z - sc.lr * __builtin_fmaf(sc.decay, w[j].z, y.z), w[j].w - sc.lr * __builtin_fmaf(sc.decay, w[j].w, y.w));
+                    store4(it.weight_out + e, vec, n, v);
+                    if (it.weight_bf16) {
+                        const uint2 b = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+                        if (vec) {
+                            if (n > 0) *reinterpret_cast<uint2*>(it.weight_bf16 + e) = b;
+                        } else {
+                            if (n > 0) it.weight_bf16[e] = (uint16_t)(b.x & 0xffffu);
+                            if (n > 1) it.weight_bf16[e + 1] = (uint16_t)(b.x >> 16);
+                            if (n > 2) it.weight_bf16[e + 2] = (uint16_t)(b.y & 0xffffu);
+                            if (n > 3) it.weight_bf16[e + 3] = (uint16_t)(b.y >> 16);
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+int mu_class(int R) { return R <= 16 ? 0 : R <= 32 ? 1 : 2; }
+constexpr int kMuNT[3] = {1, 2, 4};
+
+// long-side elements per workgroup: enough workgroups to fill the chip several times, few enough that a workgroup's partial Gram
+// matrix is little beside what it reads
+long long mu_chunk(long long total) {
+    const long long n = total / MU_SPAN / (4 * device_compute_units());
+    return MU_SPAN * std::max(1ll, std::min(n, 8ll));
+}
+
+struct MuonPlan { long long chunk[3]; size_t chunks[3], items[3], part0[3], poly0[3], bytes; };
+MuonPlan mu_plan(int n, const MuonItem* items) {
+    MuonPlan p{};
+    long long total[3] = {0, 0, 0};
+    for (int i = 0; i < n; ++i) total[mu_class(items[i].R)] += items[i].L;
+    for (int c = 0; c < 3; ++c) p.chunk[c] = mu_chunk(total[c]);
+    for (int i = 0; i < n; ++i) {
+        const int c = mu_class(items[i].R);
+        p.chunks[c] += (size_t)((items[i].L + p.chunk[c] - 1) / p.chunk[c]);
+        ++p.items[c];
+    }
+    for (int c = 0; c < 3; ++c) {
+        p.part0[c] = p.bytes; p.bytes += p.chunks[c] * mu_tiles(kMuNT[c]) * 256 * sizeof(double);
+        p.poly0[c] = p.bytes; p.bytes += p.items[c] * (size_t)(256 * kMuNT[c] * kMuNT[c]) * sizeof(double);
+    }
+    return p;
+}
+
+template <class T>
+hipError_t upload(const std::vector<T>& v, T*& d) {
+    hipError_t e = hipMalloc(reinterpret_cast<void**>(&d), v.size() * sizeof(T));
+    return e != hipSuccess ? e : hipMemcpy(d, v.data(), v.size() * sizeof(T), hipMemcpyHostToDevice);
+}
+
+template <int NT>
+hipError_t mu_run(const MuonGroup& g, const MuonStep& s, hipStream_t st) {
+    constexpr int threads = NT == 4 ? 1024 : NT == 2 ? 512 : 256, sh = 4 * 16 * NT * mu_ld(NT) * (int)sizeof(double);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(muon_iterate_kernel<NT>), hipFuncAttributeMaxDynamicSharedMemorySize, sh);
+    if (attr != hipSuccess) return attr;
+    const Momentum mo{s.momentum, s.nesterov};
+    hipError_t e;
+    muon_gram_kernel<NT><<<dim3((unsigned)g.nchunks), dim3(MU_THREADS), 0, st>>>(g.d_items, g.d_chunks, mo, g.part);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    muon_iterate_kernel<NT><<<dim3((unsigned)g.nitems), dim3(threads), sh, st>>>(g.d_items, g.part, g.poly, s.steps, (double)s.a, (double)s.b, (double)s.c,
+                                                                                 (double)s.eps);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    muon_apply_kernel<NT><<<dim3((unsigned)g.nchunks), dim3(MU_THREADS), 0, st>>>(g.d_items, g.d_chunks, mo, g.poly, MuonScalars{s.lr, s.decay});
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t muon_workspace_bytes(int n, const MuonItem* items) { return mu_plan(n, items).bytes; }
+
+hipError_t muon_build(const std::vector<MuonItem>& all, void* workspace, MuonGroup (&groups)[3]) {
+    const MuonPlan p = mu_plan((int)all.size(), all.data());
+    for (int c = 0; c < 3; ++c) {
+        std::vector<MuonItem> items;
+        std::vector<MuonChunk> chunks;
+        for (const MuonItem& a : all) {
+            if (mu_class(a.R) != c) continue;
+            MuonItem it = a;
+            it.chunk0 = (int)chunks.size();
+            for (long long l = 0; l < it.L; l += p.chunk[c]) chunks.push_back(MuonChunk{l, std::min(it.L, l + p.chunk[c]), (int)items.size()});
+            it.nchunks = (int)chunks.size() - it.chunk0;
+            items.push_back(it);
+        }
+        MuonGroup& g = groups[c];
+        g.nitems = (int)items.size(); g.nchunks = (int)chunks.size();
+        g.part = reinterpret_cast<double*>(static_cast<uint8_t*>(workspace) + p.part0[c]);
+        g.poly = reinterpret_cast<double*>(static_cast<uint8_t*>(workspace) + p.poly0[c]);
+        if (items.empty()) continue;
+        hipError_t e;
+        if ((e = upload(items, g.d_items)) != hipSuccess || (e = upload(chunks, g.d_chunks)) != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+hipError_t muon_run(const MuonGroup (&groups)[3], const MuonStep& s, hipStream_t st) {
+    hipError_t e = hipSuccess;
+    if (groups[0].nitems && (e = mu_run<1>(groups[0], s, st)) != hipSuccess) return e;
+    if (groups[1].nitems && (e = mu_run<2>(groups[1], s, st)) != hipSuccess) return e;
+    if (groups[2].nitems && (e = mu_run<4>(groups[2], s, st)) != hipSuccess) return e;
+    return e;
+}
+
+void muon_free(MuonGroup (&groups)[3]) {
+    for (MuonGroup& g : groups) {
+        (void)hipFree(g.d_items); (void)hipFree(g.d_chunks);
+        g = MuonGroup{};
+    }
+}
+
+}  // namespace lowra

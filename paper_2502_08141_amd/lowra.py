@@ -7,6 +7,7 @@ There is no CPU fallback: a missing library or a failing call raises.
 from __future__ import annotations
 
 import ctypes as C
+import dataclasses
 import importlib.util
 import os
 
@@ -38,6 +39,7 @@ SYMBOLS = [
     "lowra_fwd_batch_workspace_bytes", "lowra_fwd_batch_create", "lowra_fwd_batch_run", "lowra_fwd_batch_destroy",
     "lowra_bwd_batch_workspace_bytes", "lowra_bwd_batch_create", "lowra_bwd_batch_run", "lowra_bwd_batch_destroy",
     "lowra_linear_fwd_act", "lowra_linear_bwd_input_act", "lowra_act_bwd", "lowra_act_bwd_workspace_bytes",
+    "lowra_muon_batch_workspace_bytes", "lowra_muon_batch_create", "lowra_muon_batch_run", "lowra_muon_batch_destroy",
     "lowra_measure_copy", "lowra_measure_read", "lowra_measure_mfma", "lowra_measure_mfma_random",
 ]
 
@@ -56,6 +58,18 @@ class FwdEpilogue(C.Structure):
 class BwdEpilogue(C.Structure):
     """lowra_bwd_epilogue (device pointers)."""
     _fields_ = [("act", C.c_int), ("z", C.c_void_p), ("mul", C.c_void_p), ("residual", C.c_void_p), ("dmul", C.c_void_p)]
+
+
+class MuonItemRecord(C.Structure):
+    """lowra_muon_item (device pointers)."""
+    _fields_ = [("rows", C.c_int), ("cols", C.c_int), ("scale", C.c_float)] + [(n, C.c_void_p) for n in (
+        "grad", "momentum", "momentum_out", "weight", "weight_out", "weight_bf16", "update")]
+
+
+class MuonStep(C.Structure):
+    """lowra_muon_step."""
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("nesterov", C.c_int), ("weight_decay", C.c_float), ("steps", C.c_int),
+                ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("eps", C.c_float)]
 
 
 class LowraError(RuntimeError):
@@ -116,6 +130,12 @@ def lib() -> C.CDLL:
         L.lowra_bwd_batch_run.argtypes = [vp, vp]
         L.lowra_bwd_batch_destroy.restype = None
         L.lowra_bwd_batch_destroy.argtypes = [vp]
+        L.lowra_muon_batch_workspace_bytes.restype = C.c_size_t
+        L.lowra_muon_batch_workspace_bytes.argtypes = [C.c_int, C.c_void_p]
+        L.lowra_muon_batch_create.argtypes = [C.c_int, C.c_void_p, vp, C.c_size_t, C.c_void_p]
+        L.lowra_muon_batch_run.argtypes = [vp, vp, vp]
+        L.lowra_muon_batch_destroy.restype = None
+        L.lowra_muon_batch_destroy.argtypes = [vp]
         L.lowra_channel_mse.argtypes = [C.c_int, C.c_int, f32p, f32p, f32p, f32p, vp]
         L.lowra_assign_precisions.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_double, C.c_void_p]
         L.lowra_measure_copy.argtypes = [vp, vp, C.c_size_t, vp]
@@ -672,6 +692,72 @@ class BwdBatch:
     def close(self):
         if self.handle:
             lib().lowra_bwd_batch_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+@dataclasses.dataclass
+class MuonItem:
+    """One matrix of a MuonBatch: fp32 device tensors [rows, cols] (weight_bf16: bf16), the short side at most 64.  `momentum_out` and
+    `weight_out` are the tensors themselves where they are not given (in place); without `weight` the batch writes `update` only."""
+    grad: torch.Tensor
+    momentum: torch.Tensor
+    weight: torch.Tensor | None = None
+    weight_bf16: torch.Tensor | None = None
+    update: torch.Tensor | None = None
+    scale: float = 1.0
+    momentum_out: torch.Tensor | None = None
+    weight_out: torch.Tensor | None = None
+
+
+class MuonBatch:
+    """The optimiser step on a list of MuonItem with the update orthogonalised by Newton-Schulz products (lowra_muon_batch_*).  Every
+    tensor is kept alive by the object: the library holds their addresses."""
+
+    def __init__(self, items, workspace=None):
+        self.handle = C.c_void_p()
+        if not items:
+            raise ValueError("empty batch")
+        device = items[0].grad.device
+        arr = (MuonItemRecord * len(items))()
+        self._keep = []
+        for i, it in enumerate(items):
+            mo = it.momentum if it.momentum_out is None else it.momentum_out
+            wo = it.weight if it.weight_out is None else it.weight_out
+            fields = (("grad", it.grad, torch.float32), ("momentum", it.momentum, torch.float32), ("momentum_out", mo, torch.float32),
+                      ("weight", it.weight, torch.float32), ("weight_out", wo, torch.float32), ("weight_bf16", it.weight_bf16, torch.bfloat16),
+                      ("update", it.update, torch.float32))
+            for name, t, dtype in fields:
+                if t is None and name not in ("grad", "momentum"):
+                    continue
+                _dev(t, dtype, name)
+                if t.dim() != 2 or t.shape != it.grad.shape or t.device != device:
+                    raise ValueError(f"item {i}: {name}: shape or device mismatch")
+            arr[i] = MuonItemRecord(int(it.grad.shape[0]), int(it.grad.shape[1]), float(it.scale), *(_ptr(t) for _, t, _ in fields))
+            self._keep += [t for _, t, _ in fields]
+        if device.index != torch.cuda.current_device():
+            raise ValueError("tensors on another device than the current one")
+        need = int(lib().lowra_muon_batch_workspace_bytes(len(items), C.addressof(arr)))
+        if workspace is None:
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        _dev(workspace, torch.uint8, "workspace")
+        self._keep.append(workspace)
+        _check(lib().lowra_muon_batch_create(len(items), C.addressof(arr), _ptr(workspace), workspace.numel(), C.addressof(self.handle)),
+               "lowra_muon_batch_create")
+
+    def run(self, lr: float, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, steps: int = 5,
+            coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7):
+        step = MuonStep(lr, momentum, nesterov, weight_decay, steps, *coefficients, eps)
+        _check(lib().lowra_muon_batch_run(self.handle, C.addressof(step), _stream()), "lowra_muon_batch_run")
+
+    def close(self):
+        if self.handle:
+            lib().lowra_muon_batch_destroy(self.handle)
             self.handle = C.c_void_p()
 
     def __del__(self):
