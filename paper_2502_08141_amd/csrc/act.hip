@@ -33,19 +33,29 @@ __global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(int M, int N, i
     if (col < N) {                                                  // N is a multiple of 8
         with_act(e.act, [&](auto A) {
             constexpr int ACT = decltype(A)::value;
-            for (int m = m0 + wave; m < m1; m += ACT_WAVES) {
-                const size_t at = (size_t)m * N + col;
-                float v[8];
-                Bf16Run<8> g;
-                EpiRun<BwdEpi, 8> r;
-                load_run<8>(dY + at, g);
-                epi_load<8>(e, at, r);
+            constexpr int U = 4;                                    // rows whose operands are asked for together
+            for (int m = m0 + wave; m < m1; m += U * ACT_WAVES) {
+                Bf16Run<8> g[U];
+                EpiRun<BwdEpi, 8> r[U];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = g[i];
-                epi_grads<ACT, 8>(e, at, v, r);
-                if (dZ) store_run<8>(dZ + at, v);
+                for (int u = 0; u < U; ++u)
+                    if (m + u * ACT_WAVES < m1) {
+                        const size_t at = (size_t)(m + u * ACT_WAVES) * N + col;
+                        load_run<8>(dY + at, g[u]);
+                        epi_load<8>(e, at, r[u]);
+                    }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) total[i] += v[i];
+                for (int u = 0; u < U; ++u)
+                    if (m + u * ACT_WAVES < m1) {
+                        const size_t at = (size_t)(m + u * ACT_WAVES) * N + col;
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = g[u][i];
+                        epi_grads<ACT, 8>(e, at, v, r[u]);
+                        if (dZ) store_run<8>(dZ + at, v);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) total[i] += v[i];
+                    }
             }
         });
     }
@@ -59,12 +69,23 @@ __global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(int M, int N, i
     }
 }
 
+// 32 columns per workgroup, the chunks dealt to eight groups of threads, each with up to eight loads under way
 __global__ __launch_bounds__(256) void act_sum_kernel(const float* __restrict__ sums, int chunks, int N, float* __restrict__ db) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= N) return;
+    __shared__ float red[8][32];
+    const int c = threadIdx.x & 31, grp = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
     float v = 0.0f;
-    for (int q = 0; q < chunks; ++q) v += sums[(size_t)q * N + c];
-    db[c] = v;
+    for (int k = grp; k < chunks; k += 64) {
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = sums[(size_t)min(k + 8 * u, chunks - 1) * N + min(col, N - 1)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v += k + 8 * u < chunks ? x[u] : 0.0f;
+    }
+    red[grp][c] = v;
+    __syncthreads();
+    if (grp != 0 || col >= N) return;
+    for (int g = 1; g < 8; ++g) v += red[g][c];
+    db[col] = v;
 }
 
 }  // namespace
@@ -80,7 +101,7 @@ hipError_t launch_act_bwd(int M, int N, const BwdEpi& e, const uint16_t* dY, uin
     act_bwd_kernel<<<dim3((unsigned)((N + ACT_COLS - 1) / ACT_COLS), (unsigned)chunks), dim3(ACT_WAVES * 64), 0, st>>>(M, N, rows, e, dY, dZ, sums);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess || !db || chunks == 1) return err;
-    act_sum_kernel<<<dim3((unsigned)((N + 255) / 256)), dim3(256), 0, st>>>(sums, chunks, N, db);
+    act_sum_kernel<<<dim3((unsigned)((N + 31) / 32)), dim3(256), 0, st>>>(sums, chunks, N, db);
     return hipGetLastError();
 }
 

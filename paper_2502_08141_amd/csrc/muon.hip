@@ -54,18 +54,23 @@ struct Momentum { float beta; int nesterov; };
 __device__ __forceinline__ float momentum_of(const Momentum& mo, float g, float m) { return __builtin_fmaf(mo.beta, m, g); }
 __device__ __forceinline__ float update_of(const Momentum& mo, float g, float m1) { return mo.nesterov ? __builtin_fmaf(mo.beta, m1, g) : m1; }
 
-// ---- 1. momentum and Gram matrix.  A wavefront's step: operands of four products (k sets of four long-side elements) per tile.
-// Short side in rows (A): lane (i, q) loads row 16 t + i, columns c + 4 q .. + 3; product e contracts columns c + 4 q + e.
-// Short side in columns (B): lane (i, q) loads row c + q, NT columns from NT i on; tile e holds columns NT i + e: a permutation that
-// the second kernel undoes.
+// ---- 1. momentum and Gram matrix.  Products over four long-side elements at a time: lane (i, q) holds element 16 t + i of the
+// short side, k = q.
+// Short side in rows (A): a step of a wavefront is 16 columns; lane (i, q) loads row 16 t + i, columns c + 4 q .. + 3, and product e
+// contracts columns c + 4 q + e: any order of the long side will do, if both operands have it.
+// Short side in columns (B): a step is 16 rows, 16 R values on end whatever R is: loaded and stored as such, quads NT to a lane, and
+// brought into the operands' order through a piece of LDS of the wavefront's own.
+// The loads of the next step are under way while this one is multiplied.
+template <int NT> struct GramStep { float4 g[NT], m[NT]; };
 template <int NT>
 __global__ __launch_bounds__(MU_THREADS) void muon_gram_kernel(const MuonItem* __restrict__ items, const MuonChunk* __restrict__ chunks, Momentum mo,
                                                                double* __restrict__ part) {
     constexpr int TILES = mu_tiles(NT);
-    __shared__ double red[3][TILES][256];
+    __shared__ __align__(16) union { double red[3][TILES][256]; float u[4][256 * NT]; } sh;
     const MuonItem it = items[chunks[blockIdx.x].item];
     const long long first = chunks[blockIdx.x].first, last = chunks[blockIdx.x].last;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int R = it.R;
     f64x4_t acc[TILES];
 #pragma unroll
@@ -76,22 +81,45 @@ __global__ __launch_bounds__(MU_THREADS) void muon_gram_kernel(const MuonItem* _
 #pragma unroll
             for (int t2 = t1; t2 < NT; ++t2) acc[mu_tile(NT, t1, t2)] = mfma64(a[t1], a[t2], acc[mu_tile(NT, t1, t2)]);
     };
-    if (it.wide) {
-        const bool vec = (it.L & 3) == 0;
-        for (long long c = first + 16 * wave; c < last; c += 64) {
+    // quad k of a lane in the step at c: its first element, and how many there are
+    const bool wide = it.wide != 0;
+    auto quad = [&](long long c, int k, size_t& e) __attribute__((always_inline)) -> int {
+        if (wide) {
+            const bool ok = 16 * k + i < R;
             const long long col = c + 4 * q;
-            const int n = (int)min(max(last - col, 0ll), 4ll);
-            float4 u[NT];
+            e = (size_t)(ok ? 16 * k + i : 0) * it.L + col;
+            return ok ? (int)min(max(last - col, 0ll), 4ll) : 0;
+        }
+        const int f = 4 * (k * 64 + lane);
+        e = (size_t)c * R + f;
+        return min(max((int)min(last - c, 16ll) * R - f, 0), 4);
+    };
+    const bool rows4 = !wide || (it.L & 3) == 0;                      // whole quads are 16-byte aligned
+    auto load = [&](long long c, GramStep<NT>& s) __attribute__((always_inline)) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const bool ok = 16 * t + i < R;
-                const size_t e = (size_t)(ok ? 16 * t + i : 0) * it.L + col;
-                const int m = ok ? n : 0;
-                const float4 g = load4(it.grad + e, vec, m), o = load4(it.momentum + e, vec, m);
-                const float4 m1 = make_float4(momentum_of(mo, g.x, o.x), momentum_of(mo, g.y, o.y), momentum_of(mo, g.z, o.z), momentum_of(mo, g.w, o.w));
-                store4(it.momentum_out + e, vec, m, m1);
-                u[t] = make_float4(update_of(mo, g.x, m1.x), update_of(mo, g.y, m1.y), update_of(mo, g.z, m1.z), update_of(mo, g.w, m1.w));
-            }
+        for (int k = 0; k < NT; ++k) {
+            size_t e;
+            const int n = quad(c, k, e);
+            s.g[k] = load4(it.grad + e, rows4 && n == 4, n);
+            s.m[k] = load4(it.momentum + e, rows4 && n == 4, n);
+        }
+    };
+    GramStep<NT> cur, nxt;
+    const long long c0 = first + 16 * wave;
+    if (c0 < last) load(c0, cur);
+    for (long long c = c0; c < last; c += 64) {                       // uniform
+        if (c + 64 < last) load(c + 64, nxt);
+        float4 u[NT];
+#pragma unroll
+        for (int k = 0; k < NT; ++k) {
+            size_t e;
+            const int n = quad(c, k, e);
+            const float4 g = cur.g[k], o = cur.m[k];
+            const float4 m1 = make_float4(momentum_of(mo, g.x, o.x), momentum_of(mo, g.y, o.y), momentum_of(mo, g.z, o.z), momentum_of(mo, g.w, o.w));
+            store4(it.momentum_out + e, rows4 && n == 4, n, m1);
+            u[k] = make_float4(update_of(mo, g.x, m1.x), update_of(mo, g.y, m1.y), update_of(mo, g.z, m1.z), update_of(mo, g.w, m1.w));
+        }
+        if (wide) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 double a[NT];
@@ -99,28 +127,30 @@ __global__ __launch_bounds__(MU_THREADS) void muon_gram_kernel(const MuonItem* _
                 for (int t = 0; t < NT; ++t) a[t] = (double)at4(u[t], e);
                 multiply(a);
             }
-        }
-    } else {
-        for (long long c = first + 4 * wave; c < last; c += 16) {
-            const long long row = c + q;
-            double a[NT];
+        } else {
+            float* mine = sh.u[wave];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-            for (int e = 0; e < NT; ++e) {
-                const bool ok = row < last && NT * i + e < R;
-                const size_t at = ok ? (size_t)row * R + NT * i + e : 0;
-                const float g = ok ? it.grad[at] : 0.0f, o = ok ? it.momentum[at] : 0.0f, m1 = momentum_of(mo, g, o);
-                if (ok) it.momentum_out[at] = m1;
-                a[e] = (double)update_of(mo, g, m1);
+            for (int k = 0; k < NT; ++k)
+                if (4 * (k * 64 + lane) < 16 * R) *reinterpret_cast<float4*>(mine + 4 * (k * 64 + lane)) = u[k];     // (past the last row: zeros)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                double a[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) a[t] = 16 * t + i < R ? (double)mine[(4 * e + q) * R + 16 * t + i] : 0.0;
+                multiply(a);
             }
-            multiply(a);
         }
+        cur = nxt;
     }
+    __syncthreads();
     // the wavefronts' sums, in order
     if (wave > 0) {
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) red[wave - 1][t][v * 64 + lane] = acc[t][v];
+            for (int v = 0; v < 4; ++v) sh.red[wave - 1][t][v * 64 + lane] = acc[t][v];
     }
     __syncthreads();
     if (wave == 0) {
@@ -130,14 +160,13 @@ __global__ __launch_bounds__(MU_THREADS) void muon_gram_kernel(const MuonItem* _
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int o = v * 64 + lane;
-                dst[t * 256 + o] = ((acc[t][v] + red[0][t][o]) + red[1][t][o]) + red[2][t][o];
+                dst[t * 256 + o] = ((acc[t][v] + sh.red[0][t][o]) + sh.red[1][t][o]) + sh.red[2][t][o];
             }
     }
 }
 
-// ---- 2. the iteration.  Positions of a Gram matrix: tile t, place i is element 16 t + i of the short side (A) or NT i + t (B).
-// The polynomial is handed on in the order in which the third kernel's lanes want it: as it is (A), or with place p of a tile
-// holding element 4 (p % 4) + p / 4 (B).
+// ---- 2. the iteration.  The polynomial is handed on as the operands of the third kernel: operand (to, t, k) of it, 64 values for the
+// 64 lanes (x, q), row 16 to + x and column 16 t + 4 k + q; for B in another order of the short side, see there.
 template <int NT>
 __global__ __launch_bounds__(NT == 4 ? 1024 : NT == 2 ? 512 : 256) void muon_iterate_kernel(const MuonItem* __restrict__ items, const double* __restrict__ part,
                                                                                             double* __restrict__ poly, int steps, double ca, double cb,
@@ -156,12 +185,30 @@ __global__ __launch_bounds__(NT == 4 ? 1024 : NT == 2 ? 512 : 256) void muon_ite
         if (r <= c) { M[r * LD + c] = x; M[c * LD + r] = x; }        // (the two halves of a product differ by their rounding)
     };
     const double* src = part + (size_t)it.chunk0 * (TILES * 256);
-    for (int o = threadIdx.x; o < TILES * 256; o += WAVES * 64) {
-        double x = 0.0;
-        for (int k = 0; k < it.nchunks; ++k) x += src[(size_t)k * (TILES * 256) + o];
-        int t1 = 0, rest = o >> 8;
-        while (rest >= NT - t1) { rest -= NT - t1; ++t1; }
-        place(G, t1, t1 + rest, o & 255, x);
+    {   // the chunks' sums, in order; SLOTS of them for a thread, eight chunks' loads at a time
+        constexpr int SLOTS = (TILES * 256 + WAVES * 64 - 1) / (WAVES * 64);
+        double x[SLOTS];
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) x[j] = 0.0;
+        for (int k = 0; k < it.nchunks; k += 8) {
+            double v[SLOTS][8];
+#pragma unroll
+            for (int j = 0; j < SLOTS; ++j)
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    v[j][u] = src[(size_t)min(k + u, it.nchunks - 1) * (TILES * 256) + min((int)threadIdx.x + j * WAVES * 64, TILES * 256 - 1)];
+#pragma unroll
+            for (int j = 0; j < SLOTS; ++j)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[j] += k + u < it.nchunks ? v[j][u] : 0.0;
+        }
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) {
+            const int o = threadIdx.x + j * WAVES * 64;
+            int t1 = 0, rest = o >> 8;
+            while (rest >= NT - t1 && t1 < NT) { rest -= NT - t1; ++t1; }
+            if (o < TILES * 256) place(G, t1, t1 + rest, o & 255, x[j]);
+        }
     }
     __syncthreads();
     double trace = 0.0;
@@ -232,48 +279,34 @@ __global__ __launch_bounds__(NT == 4 ? 1024 : NT == 2 ? 512 : 256) void muon_ite
         __syncthreads();
     }
     double* dst = poly + (size_t)blockIdx.x * (RP * RP);
-    auto position = [&](int p) {                                     // where the element that belongs at place p of the third kernel's order is
-        if (it.wide) return p;
-        const int e = (p & ~15) | (4 * (p & 3) + ((p >> 2) & 3));
-        return 16 * (e % NT) + e / NT;
-    };
-    for (int o = threadIdx.x; o < RP * RP; o += WAVES * 64) dst[o] = P[position(o / RP) * LD + position(o % RP)] * norm;
+    auto element = [&](int p) { return it.wide ? p : (p & ~15) | (4 * (p & 3) + ((p >> 2) & 3)); };
+    for (int o = threadIdx.x; o < RP * RP; o += WAVES * 64) {
+        const int l = o & 63, k = (o >> 6) & 3, t = (o >> 8) % NT, to = (o >> 8) / NT;
+        dst[o] = P[element(16 * to + (l & 15)) * LD + element(16 * t + 4 * k + (l >> 4))] * norm;
+    }
 }
 
 // ---- 3. X = p(G) u and the weights.  A wavefront takes 64 long-side elements: four operands o of 16, products k over the short side.
 // Short side in rows: lane (x, q) holds rows 16 t + q + 4 v, columns 4 x .. + 3; operand o is column 4 x + o, k set (t, v) the rows
 // 16 t + 4 v + q.  Results (row q + 4 v of a tile, column x) land where the lane's own elements are.
-// Short side in columns: lane (x, q) holds row 16 o + x, columns 16 t + 4 q .. + 3; k set (t, e) the columns 16 t + 4 q + e, and with the
-// rows of the polynomial in the same order (place p: element 4 (p % 4) + p / 4) the results again land there.
+// Short side in columns: lane (x, q) holds row 16 o + x, columns 16 t + 4 q .. + 3; k set (t, e) the columns 16 t + 4 q + e.  With the
+// short side in the order in which place p of a tile is element 4 (p % 4) + p / 4, that is place 4 e + q of the tile, and the results
+// again land where the lane's own elements are.
 struct MuonScalars { float lr, decay; };
-template <int NT>
-__global__ __launch_bounds__(MU_THREADS) void muon_apply_kernel(const MuonItem* __restrict__ items, const MuonChunk* __restrict__ chunks, Momentum mo,
-                                                                const double* __restrict__ poly, MuonScalars sc) {
-    constexpr int LD = mu_ld(NT), RP = 16 * NT;
-    __shared__ double P[RP * LD];
-    const int item = chunks[blockIdx.x].item;
-    const MuonItem it = items[item];
-    const long long first = chunks[blockIdx.x].first, last = chunks[blockIdx.x].last;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 15, q = lane >> 4;
+template <int NT, bool WIDE>
+__device__ __forceinline__ void muon_apply(const MuonItem& it, long long first, long long last, const Momentum& mo, const double* P, const MuonScalars& sc) {
+    const int lane = threadIdx.x & 63, x = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int R = it.R;
-    for (int o = threadIdx.x; o < RP * RP; o += MU_THREADS) P[(o / RP) * LD + o % RP] = poly[(size_t)item * (RP * RP) + o];
-    __syncthreads();
-    const bool vec = ((it.wide ? it.L : (long long)R) & 3) == 0;
-    for (long long c = first + 64 * wave; c < last; c += MU_SPAN) {
+    const bool vec = ((WIDE ? it.L : (long long)R) & 3) == 0;
+    for (long long c = first + 64 * wave; c < last; c += MU_SPAN) {  // uniform
         // quad (t, j): wide: row 16 t + q + 4 j, columns c + 4 x; else row c + 16 j + x, columns 16 t + 4 q
         auto where = [&](int t, int j, size_t& e) __attribute__((always_inline)) -> int {              // elements there
-            if (it.wide) {
-                const int r = 16 * t + q + 4 * j;
-                const long long col = c + 4 * x;
-                const bool ok = r < R && col < last;
-                e = ok ? (size_t)r * it.L + col : 0;
-                return ok ? (int)min(last - col, 4ll) : 0;
-            }
-            const long long r = c + 16 * j + x;
-            const int col = 16 * t + 4 * q;
-            const bool ok = r < last && col < R;
-            e = ok ? (size_t)r * R + col : 0;
-            return ok ? min(R - col, 4) : 0;
+            const int s = WIDE ? 16 * t + q + 4 * j : 16 * t + 4 * q;
+            const long long l = WIDE ? c + 4 * x : c + 16 * j + x;
+            const bool ok = s < R && l < last;
+            e = !ok ? 0 : WIDE ? (size_t)s * it.L + l : (size_t)l * R + s;
+            return !ok ? 0 : WIDE ? (int)min(last - l, 4ll) : min(R - s, 4);
         };
         float4 u[NT][4];
 #pragma unroll
@@ -282,13 +315,19 @@ __global__ __launch_bounds__(MU_THREADS) void muon_apply_kernel(const MuonItem* 
             for (int j = 0; j < 4; ++j) {
                 size_t e;
                 const int n = where(t, j, e);
-                const float4 m1 = load4(it.momentum_out + e, vec, n);
-                u[t][j] = m1;
-                if (mo.nesterov) {
-                    const float4 g = load4(it.grad + e, vec, n);
+                u[t][j] = load4(it.momentum_out + e, vec, n);
+            }
+        if (mo.nesterov) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    size_t e;
+                    const int n = where(t, j, e);
+                    const float4 g = load4(it.grad + e, vec, n), m1 = u[t][j];
                     u[t][j] = make_float4(update_of(mo, g.x, m1.x), update_of(mo, g.y, m1.y), update_of(mo, g.z, m1.z), update_of(mo, g.w, m1.w));
                 }
-            }
+        }
 #pragma unroll
         for (int to = 0; to < NT; ++to) {
             float4 w[4];
@@ -307,16 +346,16 @@ __global__ __launch_bounds__(MU_THREADS) void muon_apply_kernel(const MuonItem* 
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const double p = P[(16 * to + x) * LD + 16 * t + 4 * k + q];
+                    const double p = P[((to * NT + t) * 4 + k) * 64 + lane];
 #pragma unroll
-                    for (int o = 0; o < 4; ++o) acc[o] = mfma64(p, (double)(it.wide ? at4(u[t][k], o) : at4(u[t][o], k)), acc[o]);
+                    for (int o = 0; o < 4; ++o) acc[o] = mfma64(p, (double)(WIDE ? at4(u[t][k], o) : at4(u[t][o], k)), acc[o]);
                 }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 size_t e;
                 const int n = where(to, j, e);
                 float4 y;
-                if (it.wide) y = make_float4((float)acc[0][j], (float)acc[1][j], (float)acc[2][j], (float)acc[3][j]);
+                if (WIDE) y = make_float4((float)acc[0][j], (float)acc[1][j], (float)acc[2][j], (float)acc[3][j]);
                 else y = make_float4((float)acc[j][0], (float)acc[j][1], (float)acc[j][2], (float)acc[j][3]);
                 y.x *= it.scale; y.y *= it.scale; y.z *= it.scale; y.w *= it.scale;
                 if (it.update) store4(it.update + e, vec, n, y);
@@ -339,6 +378,19 @@ __global__ __launch_bounds__(MU_THREADS) void muon_apply_kernel(const MuonItem* 
             }
         }
     }
+}
+template <int NT>
+__global__ __launch_bounds__(MU_THREADS, NT == 1 ? 4 : NT == 2 ? 3 : 2) void muon_apply_kernel(const MuonItem* __restrict__ items, const MuonChunk* __restrict__ chunks,
+                                                                                               Momentum mo, const double* __restrict__ poly, MuonScalars sc) {
+    __shared__ double P[256 * NT * NT];
+    const int item = chunks[blockIdx.x].item;
+    const MuonItem it = items[item];
+    const long long first = chunks[blockIdx.x].first, last = chunks[blockIdx.x].last;
+#pragma unroll
+    for (int o = 0; o < NT * NT; ++o) P[o * 256 + threadIdx.x] = poly[((size_t)item * (NT * NT) + o) * 256 + threadIdx.x];
+    __syncthreads();
+    if (it.wide) muon_apply<NT, true>(it, first, last, mo, P, sc);
+    else muon_apply<NT, false>(it, first, last, mo, P, sc);
 }
 
 int mu_class(int R) { return R <= 16 ? 0 : R <= 32 ? 1 : 2; }
