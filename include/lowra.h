@@ -311,7 +311,7 @@ lowra_status lowra_adapter_grads_from_side(const lowra_layout* layout, const uin
  *   workspace: dev, >= lowra_muon_batch_workspace_bytes(n, items), 16-byte aligned, owned by the caller, used by every run (runs
  *   of one batch must not overlap).
  * create: INVALID_ARG (null / n <= 0 / a non-positive size / a missing pointer: grad, momentum, momentum_out, and weight with
- * weight_out or update are needed, weight_bf16 needs weight), UNSUPPORTED (a short side above 64), MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY,
+ * weight_out or update are needed, weight_bf16 needs weight), UNSUPPORTED (a short side above 64, 2^29 elements or more), MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY,
  * HIP_ERROR.  create allocates device memory for the descriptors and copies them synchronously; destroy frees.
  * run: INVALID_ARG (null, steps outside 1..64, eps not above zero, another device than the one of create), HIP_ERROR. */
 typedef struct lowra_muon_item {

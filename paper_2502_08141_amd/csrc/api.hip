@@ -722,7 +722,7 @@ void lowra_bwd_batch_destroy(lowra_bwd_batch* b) {
 }
 
 // ---- the orthogonalised adapter update
-static bool muon_sizes(const lowra_muon_item& it) { return it.rows > 0 && it.cols > 0 && std::min(it.rows, it.cols) <= lowra::kMuonMaxShort; }
+static bool muon_sizes(const lowra_muon_item& it) { return it.rows > 0 && it.cols > 0 && std::min(it.rows, it.cols) <= lowra::kMuonMaxShort && (long long)it.rows * it.cols < lowra::kMuonMaxElements; }
 static lowra::MuonItem muon_item(const lowra_muon_item& it) {
     lowra::MuonItem m{};
     m.grad = it.grad; m.momentum = it.momentum; m.weight = it.weight;

@@ -4,17 +4,17 @@
 
 namespace lowra {
 
+constexpr long long kMuonMaxElements = 1ll << 29;    // 32-bit byte offsets
 constexpr int kMuonMaxShort = 64;        // the short side: the rank that the adapter gradients support
 
 struct MuonItem {
     const float* grad; const float* momentum; const float* weight;        // weight null: the update only
     float* momentum_out; float* weight_out; float* update; uint16_t* weight_bf16;
-    long long L;                         // the long side
-    int R, wide;                         // the short side; wide: it counts the rows
+    int L, R, wide;                      // the long side and the short one; wide: that counts the rows
     float scale;
     int chunk0, nchunks;                 // this matrix's chunks (muon_build)
 };
-struct MuonChunk { long long first, last; int item; };                    // long-side elements [first, last) of a matrix
+struct MuonChunk { int first, last, item; };                              // long-side elements [first, last) of a matrix
 struct MuonGroup {                       // the matrices of one short-side class
     MuonItem* d_items = nullptr; MuonChunk* d_chunks = nullptr;
     double *part = nullptr, *poly = nullptr;

@@ -35,17 +35,46 @@ constexpr int mu_tiles(int NT) { return NT * (NT + 1) / 2; }
 constexpr int mu_tile(int NT, int t1, int t2) { return t1 * NT - t1 * (t1 - 1) / 2 + (t2 - t1); }
 constexpr int mu_ld(int NT) { return 16 * NT + 2; }          // doubles per LDS row: 16 rows at one column lie 4 banks apart
 
-// four fp32 from element e on, of which the first n exist; vec: whole quads are 16-byte aligned and all there
-__device__ __forceinline__ float4 load4(const float* p, bool vec, int n) {
-    if (vec) return n > 0 ? *reinterpret_cast<const float4*>(p) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    return make_float4(n > 0 ? p[0] : 0.0f, n > 1 ? p[1] : 0.0f, n > 2 ? p[2] : 0.0f, n > 3 ? p[3] : 0.0f);
+// The matrices are accessed through buffer descriptors: a quad that is not there has an offset past the end, reads as zeros and
+// is not written, without a branch or a mask around the access (a load under a condition shares its registers with the zeros of the
+// other lanes and is waited for before they are written: the first kernel took 1.3 times as long).  A null pointer is an empty buffer.
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+__device__ __forceinline__ rsrc_t rsrc_of(const void* p, int elements, int size) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, p ? elements * size : 0, 0x00027000);
 }
-__device__ __forceinline__ void store4(float* p, bool vec, int n, float4 v) {
-    if (vec) { if (n > 0) *reinterpret_cast<float4*>(p) = v; return; }
-    if (n > 0) p[0] = v.x;
-    if (n > 1) p[1] = v.y;
-    if (n > 2) p[2] = v.z;
-    if (n > 3) p[3] = v.w;
+constexpr uint32_t MU_NONE = 0x80000000u;             // past every end: a matrix has less than 2^31 bytes
+// A quad of fp32 from element e on.  VEC: quads are 16-byte aligned and whole or not there; else n of them are.
+template <bool VEC>
+__device__ __forceinline__ float4 load4(rsrc_t r, bool ok, uint32_t e, int n) {
+    if constexpr (VEC) {
+        return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, ok ? e * 4 : MU_NONE, 0, 0));
+    } else {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, ok && i < n ? (e + i) * 4 : MU_NONE, 0, 0));
+        return make_float4(v[0], v[1], v[2], v[3]);
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store4(rsrc_t r, bool ok, uint32_t e, int n, float4 v) {
+    if constexpr (VEC) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(g_u32x4_t, v), r, ok ? e * 4 : MU_NONE, 0, 0);
+    } else {
+        const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x[i]), r, ok && i < n ? (e + i) * 4 : MU_NONE, 0, 0);
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store4_bf16(rsrc_t r, bool ok, uint32_t e, int n, float4 v) {
+    const uint32_t lo = pack_bf16x2(v.x, v.y), hi = pack_bf16x2(v.z, v.w);
+    if constexpr (VEC) {
+        __builtin_amdgcn_raw_buffer_store_b64(g_u32x2_t{lo, hi}, r, ok ? e * 2 : MU_NONE, 0, 0);
+    } else {
+        const uint32_t x[4] = {lo, lo >> 16, hi, hi >> 16};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(x[i] & 0xffffu), r, ok && i < n ? (e + i) * 2 : MU_NONE, 0, 0);
+    }
 }
 __device__ __forceinline__ float at4(const float4& v, int e) { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; }
 
@@ -55,94 +84,105 @@ __device__ __forceinline__ float momentum_of(const Momentum& mo, float g, float 
 __device__ __forceinline__ float update_of(const Momentum& mo, float g, float m1) { return mo.nesterov ? __builtin_fmaf(mo.beta, m1, g) : m1; }
 
 // ---- 1. momentum and Gram matrix.  Products over four long-side elements at a time: lane (i, q) holds element 16 t + i of the
-// short side, k = q.
-// Short side in rows (A): a step of a wavefront is 16 columns; lane (i, q) loads row 16 t + i, columns c + 4 q .. + 3, and product e
-// contracts columns c + 4 q + e: any order of the long side will do, if both operands have it.
-// Short side in columns (B): a step is 16 rows, 16 R values on end whatever R is: loaded and stored as such, quads NT to a lane, and
-// brought into the operands' order through a piece of LDS of the wavefront's own.
+// short side, k = q.  A step of a wavefront is 64 / NT long-side elements, four quads to a lane whatever NT is, brought into the
+// operands' order through a piece of LDS of the wavefront's own.
+// Short side in rows (A): 16 / NT lanes side by side load a row's 256 / NT bytes of the step, 4 NT rows at a time (with 64 bytes of
+// 16 rows per load the pass over A at rank 16 took 1.5 times as long).  LDS rows of 64 / NT + 4 values: the operands' reads, 16 rows at
+// one column and three more, touch every bank once.
+// Short side in columns (B): the step's rows are 64 R / NT values on end whatever R is, loaded, stored and kept in LDS as such.
 // The loads of the next step are under way while this one is multiplied.
-template <int NT> struct GramStep { float4 g[NT], m[NT]; };
-template <int NT>
-__global__ __launch_bounds__(MU_THREADS) void muon_gram_kernel(const MuonItem* __restrict__ items, const MuonChunk* __restrict__ chunks, Momentum mo,
-                                                               double* __restrict__ part) {
-    constexpr int TILES = mu_tiles(NT);
-    __shared__ __align__(16) union { double red[3][TILES][256]; float u[4][256 * NT]; } sh;
-    const MuonItem it = items[chunks[blockIdx.x].item];
-    const long long first = chunks[blockIdx.x].first, last = chunks[blockIdx.x].last;
+constexpr int mu_step(int NT) { return 64 / NT; }
+constexpr int mu_stage(int NT) { return 16 * NT * (mu_step(NT) + 4); }     // floats: more than the 1024 of the other form
+template <int NT> struct GramSums { f64x4_t acc[mu_tiles(NT)]; };
+template <int NT, bool WIDE, bool VEC>
+__device__ __forceinline__ void muon_gram(const MuonItem& it, int first, int last, const Momentum& mo, float* mine, GramSums<NT>& sums) {
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int R = it.R;
-    f64x4_t acc[TILES];
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) acc[t] = f64x4_t{0.0, 0.0, 0.0, 0.0};
-    auto multiply = [&](const double (&a)[NT]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int t1 = 0; t1 < NT; ++t1)
-#pragma unroll
-            for (int t2 = t1; t2 < NT; ++t2) acc[mu_tile(NT, t1, t2)] = mfma64(a[t1], a[t2], acc[mu_tile(NT, t1, t2)]);
-    };
-    // quad k of a lane in the step at c: its first element, and how many there are
-    const bool wide = it.wide != 0;
-    auto quad = [&](long long c, int k, size_t& e) __attribute__((always_inline)) -> int {
-        if (wide) {
-            const bool ok = 16 * k + i < R;
-            const long long col = c + 4 * q;
-            e = (size_t)(ok ? 16 * k + i : 0) * it.L + col;
-            return ok ? (int)min(max(last - col, 0ll), 4ll) : 0;
+    const int R = it.R, L = it.L;
+    const rsrc_t grad = rsrc_of(it.grad, R * L, 4), momentum = rsrc_of(it.momentum, R * L, 4), momentum_out = rsrc_of(it.momentum_out, R * L, 4);
+    constexpr int STEP = mu_step(NT), LDW = STEP + 4, PER = STEP / 4;  // PER: lanes of a row
+    // quad k of a lane in the step at c: its first element, whether it is there, and how many there are
+    auto quad = [&](int c, int k, bool& ok, uint32_t& e) __attribute__((always_inline)) -> int {
+        if (WIDE) {
+            const int row = k * (64 / PER) + lane / PER, col = c + 4 * (lane % PER);
+            ok = row < R && col < last;
+            e = (uint32_t)(row * L + col);
+            return last - col;
         }
-        const int f = 4 * (k * 64 + lane);
-        e = (size_t)c * R + f;
-        return min(max((int)min(last - c, 16ll) * R - f, 0), 4);
+        const int f = 4 * (k * 64 + lane), have = min(last - c, STEP) * R;
+        ok = f < have;
+        e = (uint32_t)(c * R + f);
+        return have - f;
     };
-    const bool rows4 = !wide || (it.L & 3) == 0;                      // whole quads are 16-byte aligned
-    auto load = [&](long long c, GramStep<NT>& s) __attribute__((always_inline)) {
+    struct Step { float4 g[4], m[4]; };
+    auto load = [&](int c, Step& s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = 0; k < NT; ++k) {
-            size_t e;
-            const int n = quad(c, k, e);
-            s.g[k] = load4(it.grad + e, rows4 && n == 4, n);
-            s.m[k] = load4(it.momentum + e, rows4 && n == 4, n);
+        for (int k = 0; k < 4; ++k) {
+            uint32_t e;
+            bool ok;
+            const int n = quad(c, k, ok, e);
+            s.g[k] = load4<VEC>(grad, ok, e, n);
+            s.m[k] = load4<VEC>(momentum, ok, e, n);
         }
     };
-    GramStep<NT> cur, nxt;
-    const long long c0 = first + 16 * wave;
-    if (c0 < last) load(c0, cur);
-    for (long long c = c0; c < last; c += 64) {                       // uniform
-        if (c + 64 < last) load(c + 64, nxt);
-        float4 u[NT];
+    // a wavefront's steps: 64 elements side by side, then the next 256
+    auto after = [](int c, int j) { return c + ((j + 1) % NT == 0 ? MU_SPAN - (NT - 1) * STEP : STEP); };
+    Step cur, nxt;
+    int c = first + 64 * wave;
+    if (c < last) load(c, cur);
+    for (int j = 0; c < last; ++j) {                                  // uniform
+        const int cn = after(c, j);
+        if (cn < last) load(cn, nxt);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-        for (int k = 0; k < NT; ++k) {
-            size_t e;
-            const int n = quad(c, k, e);
+        for (int k = 0; k < 4; ++k) {
+            uint32_t e;
+            bool ok;
+            const int n = quad(c, k, ok, e);
             const float4 g = cur.g[k], o = cur.m[k];
             const float4 m1 = make_float4(momentum_of(mo, g.x, o.x), momentum_of(mo, g.y, o.y), momentum_of(mo, g.z, o.z), momentum_of(mo, g.w, o.w));
-            store4(it.momentum_out + e, rows4 && n == 4, n, m1);
-            u[k] = make_float4(update_of(mo, g.x, m1.x), update_of(mo, g.y, m1.y), update_of(mo, g.z, m1.z), update_of(mo, g.w, m1.w));
+            store4<VEC>(momentum_out, ok, e, n, m1);
+            // (what is not there has come as zeros)
+            float* dst = mine + (WIDE ? (k * (64 / PER) + lane / PER) * LDW + 4 * (lane % PER) : 4 * (k * 64 + lane));
+            *reinterpret_cast<float4*>(dst) = make_float4(update_of(mo, g.x, m1.x), update_of(mo, g.y, m1.y), update_of(mo, g.z, m1.z), update_of(mo, g.w, m1.w));
         }
-        if (wide) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                double a[NT];
+        for (int e = 0; e < STEP / 4; ++e) {
+            double a[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) a[t] = (double)at4(u[t], e);
-                multiply(a);
+            for (int t = 0; t < NT; ++t) {
+                if (WIDE) a[t] = (double)mine[(16 * t + i) * LDW + 4 * e + q];
+                else a[t] = 16 * t + i < R ? (double)mine[(4 * e + q) * R + 16 * t + i] : 0.0;
             }
-        } else {
-            float* mine = sh.u[wave];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-            for (int k = 0; k < NT; ++k)
-                if (4 * (k * 64 + lane) < 16 * R) *reinterpret_cast<float4*>(mine + 4 * (k * 64 + lane)) = u[k];     // (past the last row: zeros)
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (int t1 = 0; t1 < NT; ++t1)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                double a[NT];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) a[t] = 16 * t + i < R ? (double)mine[(4 * e + q) * R + 16 * t + i] : 0.0;
-                multiply(a);
-            }
+                for (int t2 = t1; t2 < NT; ++t2) sums.acc[mu_tile(NT, t1, t2)] = mfma64(a[t1], a[t2], sums.acc[mu_tile(NT, t1, t2)]);
         }
         cur = nxt;
+        c = cn;
+    }
+}
+// (two workgroups to a unit at least, or the accumulators are kept in the other half of the registers and copied in every step)
+template <int NT>
+__global__ __launch_bounds__(MU_THREADS, NT == 4 ? 2 : 4) void muon_gram_kernel(const MuonItem* __restrict__ items, const MuonChunk* __restrict__ chunks, Momentum mo,
+                                                                                double* __restrict__ part) {
+    constexpr int TILES = mu_tiles(NT);
+    __shared__ __align__(16) union { double red[3][TILES][256]; float u[4][mu_stage(NT)]; } sh;
+    const MuonItem it = items[chunks[blockIdx.x].item];
+    const int first = chunks[blockIdx.x].first, last = chunks[blockIdx.x].last;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    GramSums<NT> s;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) s.acc[t] = f64x4_t{0.0, 0.0, 0.0, 0.0};
+    const bool vec = ((it.wide ? it.L : it.R * it.L) & 3) == 0;
+    if (it.wide) {
+        if (vec) muon_gram<NT, true, true>(it, first, last, mo, sh.u[wave], s);
+        else muon_gram<NT, true, false>(it, first, last, mo, sh.u[wave], s);
+    } else {
+        if (vec) muon_gram<NT, false, true>(it, first, last, mo, sh.u[wave], s);
+        else muon_gram<NT, false, false>(it, first, last, mo, sh.u[wave], s);
     }
     __syncthreads();
     // the wavefronts' sums, in order
@@ -150,7 +190,7 @@ __global__ __launch_bounds__(MU_THREADS) void muon_gram_kernel(const MuonItem* _
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) sh.red[wave - 1][t][v * 64 + lane] = acc[t][v];
+            for (int v = 0; v < 4; ++v) sh.red[wave - 1][t][v * 64 + lane] = s.acc[t][v];
     }
     __syncthreads();
     if (wave == 0) {
@@ -160,7 +200,7 @@ __global__ __launch_bounds__(MU_THREADS) void muon_gram_kernel(const MuonItem* _
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int o = v * 64 + lane;
-                dst[t * 256 + o] = ((acc[t][v] + sh.red[0][t][o]) + sh.red[1][t][o]) + sh.red[2][t][o];
+                dst[t * 256 + o] = ((s.acc[t][v] + sh.red[0][t][o]) + sh.red[1][t][o]) + sh.red[2][t][o];
             }
     }
 }
@@ -293,52 +333,49 @@ __global__ __launch_bounds__(NT == 4 ? 1024 : NT == 2 ? 512 : 256) void muon_ite
 // short side in the order in which place p of a tile is element 4 (p % 4) + p / 4, that is place 4 e + q of the tile, and the results
 // again land where the lane's own elements are.
 struct MuonScalars { float lr, decay; };
-template <int NT, bool WIDE>
-__device__ __forceinline__ void muon_apply(const MuonItem& it, long long first, long long last, const Momentum& mo, const double* P, const MuonScalars& sc) {
+template <int NT, bool WIDE, bool VEC>
+__device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int last, const Momentum& mo, const double* P, const MuonScalars& sc) {
     const int lane = threadIdx.x & 63, x = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int R = it.R;
-    const bool vec = ((WIDE ? it.L : (long long)R) & 3) == 0;
-    for (long long c = first + 64 * wave; c < last; c += MU_SPAN) {  // uniform
+    const int R = it.R, L = it.L, n_all = R * L;
+    const rsrc_t grad = rsrc_of(it.grad, n_all, 4), momentum = rsrc_of(it.momentum_out, n_all, 4), weight = rsrc_of(it.weight, n_all, 4),
+                 weight_out = rsrc_of(it.weight_out, n_all, 4), update = rsrc_of(it.update, n_all, 4), weight_bf16 = rsrc_of(it.weight_bf16, n_all, 2);
+    for (int c = first + 64 * wave; c < last; c += MU_SPAN) {        // uniform
         // quad (t, j): wide: row 16 t + q + 4 j, columns c + 4 x; else row c + 16 j + x, columns 16 t + 4 q
-        auto where = [&](int t, int j, size_t& e) __attribute__((always_inline)) -> int {              // elements there
-            const int s = WIDE ? 16 * t + q + 4 * j : 16 * t + 4 * q;
-            const long long l = WIDE ? c + 4 * x : c + 16 * j + x;
-            const bool ok = s < R && l < last;
-            e = !ok ? 0 : WIDE ? (size_t)s * it.L + l : (size_t)l * R + s;
-            return !ok ? 0 : WIDE ? (int)min(last - l, 4ll) : min(R - s, 4);
+        auto quad = [&](int t, int j, bool& ok, uint32_t& e) __attribute__((always_inline)) -> int {
+            int y = q;
+            if (!VEC) asm volatile("" : "+v"(y));                    // (taken afresh: the addresses of all elements at once do not fit)
+            const int s = WIDE ? 16 * t + y + 4 * j : 16 * t + 4 * y;
+            const int l = WIDE ? c + 4 * x : c + 16 * j + x;
+            ok = s < R && l < last;
+            e = (uint32_t)(WIDE ? s * L + l : l * R + s);
+            return WIDE ? last - l : R - s;
         };
         float4 u[NT][4];
+        auto load = [&](rsrc_t r, int t, int j) __attribute__((always_inline)) {
+            uint32_t e;
+            bool ok;
+            const int n = quad(t, j, ok, e);
+            return load4<VEC>(r, ok, e, n);
+        };
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                size_t e;
-                const int n = where(t, j, e);
-                u[t][j] = load4(it.momentum_out + e, vec, n);
-            }
+            for (int j = 0; j < 4; ++j) u[t][j] = load(momentum, t, j);
         if (mo.nesterov) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    size_t e;
-                    const int n = where(t, j, e);
-                    const float4 g = load4(it.grad + e, vec, n), m1 = u[t][j];
+                    const float4 g = load(grad, t, j), m1 = u[t][j];
                     u[t][j] = make_float4(update_of(mo, g.x, m1.x), update_of(mo, g.y, m1.y), update_of(mo, g.z, m1.z), update_of(mo, g.w, m1.w));
                 }
         }
-#pragma unroll
-        for (int to = 0; to < NT; ++to) {
+#pragma unroll 1
+        for (int to = 0; to < NT; ++to) {                             // (one body: u in 64 bits takes half of the registers as it is)
             float4 w[4];
-            if (it.weight) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    size_t e;
-                    const int n = where(to, j, e);
-                    w[j] = load4(it.weight + e, vec, n);
-                }
-            }
+            for (int j = 0; j < 4; ++j) w[j] = load(weight, to, j);
             f64x4_t acc[4];
 #pragma unroll
             for (int o = 0; o < 4; ++o) acc[o] = f64x4_t{0.0, 0.0, 0.0, 0.0};
@@ -352,29 +389,18 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, long long first, 
                 }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                size_t e;
-                const int n = where(to, j, e);
+                uint32_t e;
+                bool ok;
+                const int n = quad(to, j, ok, e);
                 float4 y;
                 if (WIDE) y = make_float4((float)acc[0][j], (float)acc[1][j], (float)acc[2][j], (float)acc[3][j]);
                 else y = make_float4((float)acc[j][0], (float)acc[j][1], (float)acc[j][2], (float)acc[j][3]);
                 y.x *= it.scale; y.y *= it.scale; y.z *= it.scale; y.w *= it.scale;
-                if (it.update) store4(it.update + e, vec, n, y);
-                if (it.weight) {
-                    const float4 v = make_float4(w[j].x - sc.lr * __builtin_fmaf(sc.decay, w[j].x, y.x), w[j].y - sc.lr * __builtin_fmaf(sc.decay, w[j].y, y.y),
-                                                 w[j].z - sc.lr * __builtin_fmaf(sc.decay, w[j].z, y.z), w[j].w - sc.lr * __builtin_fmaf(sc.decay, w[j].w, y.w));
-                    store4(it.weight_out + e, vec, n, v);
-                    if (it.weight_bf16) {
-                        const uint2 b = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-                        if (vec) {
-                            if (n > 0) *reinterpret_cast<uint2*>(it.weight_bf16 + e) = b;
-                        } else {
-                            if (n > 0) it.weight_bf16[e] = (uint16_t)(b.x & 0xffffu);
-                            if (n > 1) it.weight_bf16[e + 1] = (uint16_t)(b.x >> 16);
-                            if (n > 2) it.weight_bf16[e + 2] = (uint16_t)(b.y & 0xffffu);
-                            if (n > 3) it.weight_bf16[e + 3] = (uint16_t)(b.y >> 16);
-                        }
-                    }
-                }
+                const float4 v = make_float4(w[j].x - sc.lr * __builtin_fmaf(sc.decay, w[j].x, y.x), w[j].y - sc.lr * __builtin_fmaf(sc.decay, w[j].y, y.y),
+                                             w[j].z - sc.lr * __builtin_fmaf(sc.decay, w[j].z, y.z), w[j].w - sc.lr * __builtin_fmaf(sc.decay, w[j].w, y.w));
+                if (it.update) store4<VEC>(update, ok, e, n, y);              // uniform
+                store4<VEC>(weight_out, ok, e, n, v);
+                store4_bf16<VEC>(weight_bf16, ok, e, n, v);
             }
         }
     }
@@ -385,12 +411,18 @@ __global__ __launch_bounds__(MU_THREADS, NT == 1 ? 4 : NT == 2 ? 3 : 2) void muo
     __shared__ double P[256 * NT * NT];
     const int item = chunks[blockIdx.x].item;
     const MuonItem it = items[item];
-    const long long first = chunks[blockIdx.x].first, last = chunks[blockIdx.x].last;
+    const int first = chunks[blockIdx.x].first, last = chunks[blockIdx.x].last;
 #pragma unroll
     for (int o = 0; o < NT * NT; ++o) P[o * 256 + threadIdx.x] = poly[((size_t)item * (NT * NT) + o) * 256 + threadIdx.x];
     __syncthreads();
-    if (it.wide) muon_apply<NT, true>(it, first, last, mo, P, sc);
-    else muon_apply<NT, false>(it, first, last, mo, P, sc);
+    const bool vec = ((it.wide ? it.L : it.R) & 3) == 0;
+    if (it.wide) {
+        if (vec) muon_apply<NT, true, true>(it, first, last, mo, P, sc);
+        else muon_apply<NT, true, false>(it, first, last, mo, P, sc);
+    } else {
+        if (vec) muon_apply<NT, false, true>(it, first, last, mo, P, sc);
+        else muon_apply<NT, false, false>(it, first, last, mo, P, sc);
+    }
 }
 
 int mu_class(int R) { return R <= 16 ? 0 : R <= 32 ? 1 : 2; }
@@ -398,12 +430,12 @@ constexpr int kMuNT[3] = {1, 2, 4};
 
 // long-side elements per workgroup: enough workgroups to fill the chip several times, few enough that a workgroup's partial Gram
 // matrix is little beside what it reads
-long long mu_chunk(long long total) {
+int mu_chunk(long long total) {
     const long long n = total / MU_SPAN / (4 * device_compute_units());
-    return MU_SPAN * std::max(1ll, std::min(n, 8ll));
+    return MU_SPAN * (int)std::max(1ll, std::min(n, 8ll));
 }
 
-struct MuonPlan { long long chunk[3]; size_t chunks[3], items[3], part0[3], poly0[3], bytes; };
+struct MuonPlan { int chunk[3]; size_t chunks[3], items[3], part0[3], poly0[3], bytes; };
 MuonPlan mu_plan(int n, const MuonItem* items) {
     MuonPlan p{};
     long long total[3] = {0, 0, 0};
@@ -456,7 +488,7 @@ hipError_t muon_build(const std::vector<MuonItem>& all, void* workspace, MuonGro
             if (mu_class(a.R) != c) continue;
             MuonItem it = a;
             it.chunk0 = (int)chunks.size();
-            for (long long l = 0; l < it.L; l += p.chunk[c]) chunks.push_back(MuonChunk{l, std::min(it.L, l + p.chunk[c]), (int)items.size()});
+            for (int l = 0; l < it.L; l += p.chunk[c]) chunks.push_back(MuonChunk{l, std::min(it.L - l, p.chunk[c]) + l, (int)items.size()});
             it.nchunks = (int)chunks.size() - it.chunk0;
             items.push_back(it);
         }

@@ -18,6 +18,7 @@ def test_create_refusals():
                dict(weight_out=None), dict(weight=None, weight_out=None), dict(weight=None, weight_out=None, update=P, weight_bf16=P), dict(ws=None)):
         assert create(**kw) == lowra.INVALID_ARG, kw
     assert create(rows=65, cols=65) == lowra.UNSUPPORTED and create(rows=65, cols=1 << 20) == lowra.UNSUPPORTED
+    assert create(rows=64, cols=1 << 23) == lowra.UNSUPPORTED and create(rows=1 << 29, cols=1) == lowra.UNSUPPORTED
     for k in ("grad", "momentum", "momentum_out", "weight", "weight_out", "weight_bf16", "update"):
         assert create(**{k: P + 4}) == lowra.MISALIGNED, k
     assert create(ws=P + 8) == lowra.MISALIGNED
