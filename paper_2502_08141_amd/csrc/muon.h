@@ -18,7 +18,7 @@ struct MuonChunk { int first, last, item; };                              // lon
 struct MuonGroup {                       // the matrices of one short-side class
     MuonItem* d_items = nullptr; MuonChunk* d_chunks = nullptr;
     double *part = nullptr, *poly = nullptr;
-    int nitems = 0, nchunks = 0;
+    int nitems = 0, ngram = 0, napply = 0;                               // d_chunks: the first pass's, then the last's
 };
 struct MuonStep { float lr, momentum, decay, a, b, c, eps; int nesterov, steps; };
 

@@ -428,22 +428,23 @@ __global__ __launch_bounds__(MU_THREADS, NT == 1 ? 4 : NT == 2 ? 3 : 2) void muo
 int mu_class(int R) { return R <= 16 ? 0 : R <= 32 ? 1 : 2; }
 constexpr int kMuNT[3] = {1, 2, 4};
 
-// long-side elements per workgroup: enough workgroups to fill the chip several times, few enough that a workgroup's partial Gram
-// matrix is little beside what it reads
-int mu_chunk(long long total) {
+// Long-side elements per workgroup: enough workgroups to fill the chip several times, and no more than 2048.  The first pass takes at
+// least 512 at 64 ranks, where a workgroup's partial Gram matrix is 20 KB and one unit adds up all of a matrix's: with 256, one layer at
+// rank 64 spends 8 us more there, and a unit with two such workgroups is busy as long as one with one of 512.
+int mu_chunk(long long total, int least) {
     const long long n = total / MU_SPAN / (4 * device_compute_units());
-    return MU_SPAN * (int)std::max(1ll, std::min(n, 8ll));
+    return std::max(least, MU_SPAN * (int)std::max(1ll, std::min(n, 8ll)));
 }
 
-struct MuonPlan { int chunk[3]; size_t chunks[3], items[3], part0[3], poly0[3], bytes; };
+struct MuonPlan { int gram[3], apply[3]; size_t chunks[3], items[3], part0[3], poly0[3], bytes; };
 MuonPlan mu_plan(int n, const MuonItem* items) {
     MuonPlan p{};
     long long total[3] = {0, 0, 0};
     for (int i = 0; i < n; ++i) total[mu_class(items[i].R)] += items[i].L;
-    for (int c = 0; c < 3; ++c) p.chunk[c] = mu_chunk(total[c]);
+    for (int c = 0; c < 3; ++c) { p.gram[c] = mu_chunk(total[c], c == 2 ? 512 : MU_SPAN); p.apply[c] = mu_chunk(total[c], MU_SPAN); }
     for (int i = 0; i < n; ++i) {
         const int c = mu_class(items[i].R);
-        p.chunks[c] += (size_t)((items[i].L + p.chunk[c] - 1) / p.chunk[c]);
+        p.chunks[c] += (size_t)((items[i].L + p.gram[c] - 1) / p.gram[c]);
         ++p.items[c];
     }
     for (int c = 0; c < 3; ++c) {
@@ -466,12 +467,12 @@ hipError_t mu_run(const MuonGroup& g, const MuonStep& s, hipStream_t st) {
     if (attr != hipSuccess) return attr;
     const Momentum mo{s.momentum, s.nesterov};
     hipError_t e;
-    muon_gram_kernel<NT><<<dim3((unsigned)g.nchunks), dim3(MU_THREADS), 0, st>>>(g.d_items, g.d_chunks, mo, g.part);
+    muon_gram_kernel<NT><<<dim3((unsigned)g.ngram), dim3(MU_THREADS), 0, st>>>(g.d_items, g.d_chunks, mo, g.part);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     muon_iterate_kernel<NT><<<dim3((unsigned)g.nitems), dim3(threads), sh, st>>>(g.d_items, g.part, g.poly, s.steps, (double)s.a, (double)s.b, (double)s.c,
                                                                                  (double)s.eps);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    muon_apply_kernel<NT><<<dim3((unsigned)g.nchunks), dim3(MU_THREADS), 0, st>>>(g.d_items, g.d_chunks, mo, g.poly, MuonScalars{s.lr, s.decay});
+    muon_apply_kernel<NT><<<dim3((unsigned)g.napply), dim3(MU_THREADS), 0, st>>>(g.d_items, g.d_chunks + g.ngram, mo, g.poly, MuonScalars{s.lr, s.decay});
     return hipGetLastError();
 }
 
@@ -483,17 +484,22 @@ hipError_t muon_build(const std::vector<MuonItem>& all, void* workspace, MuonGro
     const MuonPlan p = mu_plan((int)all.size(), all.data());
     for (int c = 0; c < 3; ++c) {
         std::vector<MuonItem> items;
-        std::vector<MuonChunk> chunks;
+        std::vector<MuonChunk> chunks, apply;
+        auto cut = [](std::vector<MuonChunk>& to, int L, int by, int item) {
+            for (int l = 0; l < L; l += std::min(by, L - l)) to.push_back(MuonChunk{l, l + std::min(by, L - l), item});
+        };
         for (const MuonItem& a : all) {
             if (mu_class(a.R) != c) continue;
             MuonItem it = a;
             it.chunk0 = (int)chunks.size();
-            for (int l = 0; l < it.L; l += p.chunk[c]) chunks.push_back(MuonChunk{l, std::min(it.L - l, p.chunk[c]) + l, (int)items.size()});
+            cut(chunks, it.L, p.gram[c], (int)items.size());
             it.nchunks = (int)chunks.size() - it.chunk0;
+            cut(apply, it.L, p.apply[c], (int)items.size());
             items.push_back(it);
         }
         MuonGroup& g = groups[c];
-        g.nitems = (int)items.size(); g.nchunks = (int)chunks.size();
+        g.nitems = (int)items.size(); g.ngram = (int)chunks.size(); g.napply = (int)apply.size();
+        chunks.insert(chunks.end(), apply.begin(), apply.end());
         g.part = reinterpret_cast<double*>(static_cast<uint8_t*>(workspace) + p.part0[c]);
         g.poly = reinterpret_cast<double*>(static_cast<uint8_t*>(workspace) + p.poly0[c]);
         if (items.empty()) continue;
