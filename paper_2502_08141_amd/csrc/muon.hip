@@ -332,6 +332,10 @@ __global__ __launch_bounds__(NT == 4 ? 1024 : NT == 2 ? 512 : 256) void muon_ite
 // Short side in columns: lane (x, q) holds row 16 o + x, columns 16 t + 4 q .. + 3; k set (t, e) the columns 16 t + 4 q + e.  With the
 // short side in the order in which place p of a tile is element 4 (p % 4) + p / 4, that is place 4 e + q of the tile, and the results
 // again land where the lane's own elements are.
+// With 64 ranks two wavefronts share the four result tiles of their 64 elements (and load u twice, the second time from the cache): one
+// layer's adapters are 1220 such pieces of 16400 matrix cycles on 1024 SIMDs, as halves they lie more evenly (a step of one 7B layer
+// 100.8 -> 97.7 us; where all ranks are rows 91 -> 87, all columns, whose halves touch 64 bytes of a row at a time, 94.4 -> 95.5).
+constexpr int mu_parts(int NT) { return NT == 4 ? 2 : 1; }
 struct MuonScalars { float lr, decay; };
 template <int NT, bool WIDE, bool VEC>
 __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int last, const Momentum& mo, const double* P, const MuonScalars& sc) {
@@ -340,7 +344,9 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int la
     const int R = it.R, L = it.L, n_all = R * L;
     const rsrc_t grad = rsrc_of(it.grad, n_all, 4), momentum = rsrc_of(it.momentum_out, n_all, 4), weight = rsrc_of(it.weight, n_all, 4),
                  weight_out = rsrc_of(it.weight_out, n_all, 4), update = rsrc_of(it.update, n_all, 4), weight_bf16 = rsrc_of(it.weight_bf16, n_all, 2);
-    for (int c = first + 64 * wave; c < last; c += MU_SPAN) {        // uniform
+    constexpr int PARTS = mu_parts(NT), SPAN = MU_SPAN / PARTS;       // wavefronts that share the result tiles of 64 elements
+    const int part = wave % PARTS;
+    for (int c = first + 64 * (wave / PARTS); c < last; c += SPAN) { // uniform
         // quad (t, j): wide: row 16 t + q + 4 j, columns c + 4 x; else row c + 16 j + x, columns 16 t + 4 q
         auto quad = [&](int t, int j, bool& ok, uint32_t& e) __attribute__((always_inline)) -> int {
             int y = q;
@@ -372,7 +378,7 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int la
                 }
         }
 #pragma unroll 1
-        for (int to = 0; to < NT; ++to) {                             // (one body: u in 64 bits takes half of the registers as it is)
+        for (int to = part * (NT / PARTS); to < (part + 1) * (NT / PARTS); ++to) {      // (one body: u in 64 bits takes half of the registers as it is)
             float4 w[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = load(weight, to, j);
@@ -494,7 +500,7 @@ hipError_t muon_build(const std::vector<MuonItem>& all, void* workspace, MuonGro
             it.chunk0 = (int)chunks.size();
             cut(chunks, it.L, p.gram[c], (int)items.size());
             it.nchunks = (int)chunks.size() - it.chunk0;
-            cut(apply, it.L, p.apply[c], (int)items.size());
+            cut(apply, it.L, p.apply[c] / mu_parts(kMuNT[c]), (int)items.size());
             items.push_back(it);
         }
         MuonGroup& g = groups[c];
