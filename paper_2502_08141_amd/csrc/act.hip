@@ -51,7 +51,7 @@ __global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(int M, int N, i
                         float v[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) v[i] = g[u][i];
-                        epi_grads<ACT, 8>(e, at, v, r[u]);
+                        epi_apply<ACT, 8>(e, v, v, r[u], [&](const float (&w)[8]) __attribute__((always_inline)) { store_run<8>(e.dmul + at, w); });
                         if (dZ) store_run<8>(dZ + at, v);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) total[i] += v[i];

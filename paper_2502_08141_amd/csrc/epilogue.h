@@ -150,12 +150,12 @@ __device__ __forceinline__ void epi_bias(const FwdEpi& e, int col, float (&b)[W]
 template <int W>
 __device__ __forceinline__ void epi_bias(const BwdEpi&, int, float (&)[W]) {}
 
-// v: the products; `at`: element of the result
-template <int ACT, int W>
-__device__ __forceinline__ void epi_store(const FwdEpi& e, size_t at, float (&v)[W], const float (&b)[W], const EpiRun<FwdEpi, W>& r, uint16_t* out) {
+// v: the products in, y out; keep(z) stores z
+template <int ACT, int W, class Keep>
+__device__ __forceinline__ void epi_apply(const FwdEpi& e, float (&v)[W], const float (&b)[W], const EpiRun<FwdEpi, W>& r, Keep&& keep) {
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] += b[i];
-    if (e.z) store_run<W>(e.z + at, v);
+    if (e.z) keep(v);
     float slope;
 #pragma unroll
     for (int i = 0; i < W; ++i) activation<ACT, false>(v[i], v[i], slope);
@@ -167,11 +167,10 @@ __device__ __forceinline__ void epi_store(const FwdEpi& e, size_t at, float (&v)
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] += r.residual[i];
     }
-    store_run<W>(out + at, v);
 }
-// v: the products in, dX out (in fp32)
-template <int ACT, int W>
-__device__ __forceinline__ void epi_grads(const BwdEpi& e, size_t at, float (&v)[W], const EpiRun<BwdEpi, W>& r) {
+// v: the products in, dX out; keep(dmul) stores dmul
+template <int ACT, int W, class Keep>
+__device__ __forceinline__ void epi_apply(const BwdEpi& e, float (&v)[W], const float (&)[W], const EpiRun<BwdEpi, W>& r, Keep&& keep) {
     if (e.residual) {
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] += r.residual[i];
@@ -184,7 +183,7 @@ __device__ __forceinline__ void epi_grads(const BwdEpi& e, size_t at, float (&v)
     if (e.dmul) {
 #pragma unroll
         for (int i = 0; i < W; ++i) y[i] *= v[i];
-        store_run<W>(e.dmul + at, y);
+        keep(y);
     }
     if (e.mul) {
 #pragma unroll
@@ -196,33 +195,73 @@ __device__ __forceinline__ void epi_grads(const BwdEpi& e, size_t at, float (&v)
         else if constexpr (ACT != kActNone) v[i] *= slope[i];
     }
 }
-template <int ACT, int W>
-__device__ __forceinline__ void epi_store(const BwdEpi& e, size_t at, float (&v)[W], const float (&)[W], const EpiRun<BwdEpi, W>& r, uint16_t* out) {
-    epi_grads<ACT, W>(e, at, v, r);
+// one run by itself: element `at` of the result
+__device__ __forceinline__ uint16_t* epi_second(const FwdEpi& e) { return e.z; }
+__device__ __forceinline__ uint16_t* epi_second(const BwdEpi& e) { return e.dmul; }
+template <int W, class E>
+__device__ __forceinline__ void epi_run(const E& e, size_t at, int col, float (&v)[W], uint16_t* out) {
+    EpiRun<E, W> r;
+    float b[W];
+    epi_load<W>(e, at, r);
+    epi_bias<W>(e, col, b);
+    with_act(e.act, [&](auto A) __attribute__((always_inline)) {
+        epi_apply<decltype(A)::value, W>(e, v, b, r, [&](const float (&w)[W]) __attribute__((always_inline)) { store_run<W>(epi_second(e) + at, w); });
+    });
     store_run<W>(out + at, v);
 }
 
-// Eight columns from `col` on of the token rows row, row + STEP, .. (ITS of them): read(i, v) gives the products of the i-th.  The
-// operands of U rows are asked for together: nothing else is there to cover their way while a workgroup is alone on its unit.
-template <int STEP, int ITS, class E, class Read>
-__device__ __forceinline__ void epi_rows(const E& e, uint16_t* out, int ld, int M, int row, int col, Read&& read) {
-    constexpr int U = ITS % 4 == 0 ? 4 : ITS % 2 == 0 ? 2 : 1;
-    float b[8];
-    epi_bias<8>(e, col, b);
+// ---- the epilogue of a whole output tile: operands and results as buffers that start at the tile's first row (32-bit offsets; an
+// operand that is not there is an empty buffer, a row past the last token has an offset past the end)
+template <class E> struct EpiTile;
+template <> struct EpiTile<FwdEpi> { buffer_t mul, residual, second, out; };
+template <> struct EpiTile<BwdEpi> { buffer_t z, mul, residual, second, out; };
+__device__ __forceinline__ buffer_t epi_buffer(const uint16_t* p, size_t at) { return buffer_of(p ? p + at : nullptr, 0x7fffffffu); }
+__device__ __forceinline__ EpiTile<FwdEpi> epi_tile(const FwdEpi& e, uint16_t* out, size_t at) {
+    return EpiTile<FwdEpi>{epi_buffer(e.mul, at), epi_buffer(e.residual, at), epi_buffer(e.z, at), epi_buffer(out, at)};
+}
+__device__ __forceinline__ EpiTile<BwdEpi> epi_tile(const BwdEpi& e, uint16_t* out, size_t at) {
+    return EpiTile<BwdEpi>{epi_buffer(e.z, at), epi_buffer(e.mul, at), epi_buffer(e.residual, at), epi_buffer(e.dmul, at), epi_buffer(out, at)};
+}
+__device__ __forceinline__ void buffer_load8(buffer_t b, uint32_t off, Bf16Run<8>& r) {
+    const uint4 t = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0));
+    r.d[0] = t.x; r.d[1] = t.y; r.d[2] = t.z; r.d[3] = t.w;
+}
+__device__ __forceinline__ void buffer_store8(buffer_t b, uint32_t off, const float (&v)[8]) {
+    const u32x4_t t = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    __builtin_amdgcn_raw_buffer_store_b128(t, b, off, 0, 0);
+}
+__device__ __forceinline__ void epi_load(const EpiTile<FwdEpi>& t, uint32_t off, EpiRun<FwdEpi, 8>& r) {
+    buffer_load8(t.mul, off, r.mul);
+    buffer_load8(t.residual, off, r.residual);
+}
+__device__ __forceinline__ void epi_load(const EpiTile<BwdEpi>& t, uint32_t off, EpiRun<BwdEpi, 8>& r) {
+    buffer_load8(t.z, off, r.z);
+    buffer_load8(t.mul, off, r.mul);
+    buffer_load8(t.residual, off, r.residual);
+}
+// Eight columns (from `col` on) of a thread's token rows, numbers FROM .. TO - 1 of TOTAL here: offset(j) is where the j-th one's are and
+// read(j, v) gives its products.  run[j % U] holds its operands, asked for U rows ahead, over the passes through LDS: nothing else
+// covers their way where a workgroup is alone on its unit.
+template <int U, class E, class Offset>
+__device__ __forceinline__ void epi_fetch(const EpiTile<E>& t, EpiRun<E, 8> (&run)[U], Offset&& offset) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) epi_load(t, offset(u), run[u]);
+}
+template <int FROM, int TO, int TOTAL, int U, class E, class Offset, class Read>
+__device__ __forceinline__ void epi_rows(const E& e, const EpiTile<E>& t, const float (&b)[8], EpiRun<E, 8> (&run)[U], Offset&& offset, Read&& read) {
+    static_assert((TO - FROM) % U == 0 && FROM % U == 0, "");
     with_act(e.act, [&](auto A) __attribute__((always_inline)) {
 #pragma unroll 1
-        for (int i = 0; i < ITS; i += U) {
-            EpiRun<E, 8> r[U];
+        for (int j = FROM; j < TO; j += U) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (row + (i + u) * STEP < M) epi_load<8>(e, (size_t)(row + (i + u) * STEP) * ld + col, r[u]);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (row + (i + u) * STEP < M) {
-                    float v[8];
-                    read(i + u, v);
-                    epi_store<decltype(A)::value, 8>(e, (size_t)(row + (i + u) * STEP) * ld + col, v, b, r[u], out);
-                }
+            for (int u = 0; u < U; ++u) {
+                const uint32_t off = offset(j + u);
+                float v[8];
+                read(j + u, v);
+                epi_apply<decltype(A)::value, 8>(e, v, b, run[u], [&](const float (&w)[8]) __attribute__((always_inline)) { buffer_store8(t.second, off, w); });
+                buffer_store8(t.out, off, v);
+                if (j + U < TOTAL) epi_load(t, offset(j + u + U), run[u]);                       // uniform
+            }
         }
     });
 }

@@ -29,6 +29,7 @@ namespace lowra {
 typedef short v4i16_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16_t* lds_v4i16_ptr;
 
+constexpr int EPI_AHEAD = 4;   // token rows whose operands an epilogue asks for ahead
 constexpr int BROWB = 512;   // bytes per LDS row of the weight tile: 256 k x bf16
 constexpr int CSTAGE0 = 2 * STAGEB;            // staged codes: 2 buffers x 64 rows x 64 B
 constexpr int ASTAGE0 = CSTAGE0 + 2 * 4096;    // staged absmax: 2 buffers x 64 rows x 4 groups x 4 B
@@ -59,8 +60,8 @@ struct RowRegs {          // what a thread needs to decode its row's group for o
     int bits;
 };
 
-// The tile as it is, or through an epilogue (epilogue.h): the 128 token rows of two wavefronts at a time go through LDS as fp32, so
-// that every operand is read and every result written in 16 contiguous bytes, by a thread that keeps its columns.
+// The tile as it is, or through an epilogue (epilogue.h): 128 token rows at a time, 64 of either wavefront row, go through LDS as
+// fp32, so that every operand is read and every result written in 16 contiguous bytes, by a thread that keeps its columns.
 __device__ __forceinline__ void bwd_store(const floatx16_t (&acc)[4][4], const GemmParams& p, NoEpi, int m0, int k0, uint8_t*) {
     store_out(acc, p.out, p.K, p.M, p.K, m0, k0);
 }
@@ -68,26 +69,35 @@ __device__ __forceinline__ void bwd_store(const floatx16_t (&acc)[4][4], const G
     static_assert(128 * 1024 <= kBwdSmem, "128 rows of 256 fp32");
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                                  // (as in store_out_f32)
-    const int lane = tid & 63, wave = tid >> 6, wn = wave & 1, c = tid & 31, r0 = tid >> 5;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
+    const int lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1, c = tid & 31, r0 = tid >> 5;
+    const EpiTile<BwdEpi> tile = epi_tile(epi, p.out, (size_t)m0 * p.K + k0);
+    const bool col_ok = k0 + 8 * c < p.K;
+    auto offset = [&](int j) __attribute__((always_inline)) -> uint32_t {
+        const int r = 128 * ((j >> 3) & 1) + 64 * (j >> 4) + 8 * (j & 7) + r0;
+        return col_ok && m0 + r < p.M ? (uint32_t)r * (uint32_t)p.K * 2u + (uint32_t)c * 16u : kNowhere;
+    };
+    EpiRun<BwdEpi, 8> run[EPI_AHEAD];
+    epi_fetch(tile, run, offset);
+    const float none[8] = {};
+    auto pass = [&](auto P_) __attribute__((always_inline)) {
+        constexpr int P = decltype(P_)::value;
         __syncthreads();                                           // the last readers of what is overwritten are done
-        if ((wave >> 1) == half) {
 #pragma unroll
-            for (int tm = 0; tm < 4; ++tm)
+        for (int tm = 2 * P; tm < 2 * P + 2; ++tm)
 #pragma unroll
-                for (int tn = 0; tn < 4; ++tn) {
-                    const int col = wn * 128 + tn * 32 + (lane & 31);
+            for (int tn = 0; tn < 4; ++tn) {
+                const int col = wn * 128 + tn * 32 + (lane & 31);
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        *reinterpret_cast<float*>(smem + epi_chunk<64>(tm * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3), col >> 2) + (col & 3) * 4) = acc[tm][tn][v];
-                }
-        }
+                for (int v = 0; v < 16; ++v)
+                    *reinterpret_cast<float*>(smem + epi_chunk<64>(wm * 64 + (tm & 1) * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3), col >> 2) + (col & 3) * 4) =
+                        acc[tm][tn][v];
+            }
         __syncthreads();
-        if (k0 + 8 * c < p.K)
-            epi_rows<8, 16>(epi, p.out, p.K, p.M, m0 + 128 * half + r0, k0 + 8 * c,
-                            [&](int i, float (&v)[8]) __attribute__((always_inline)) { epi_read8<64>(smem, i * 8 + r0, c, v); });
-    }
+        epi_rows<16 * P, 16 * P + 16, 32>(epi, tile, none, run, offset,
+                                          [&](int j, float (&v)[8]) __attribute__((always_inline)) { epi_read8<64>(smem, (j & 15) * 8 + r0, c, v); });
+    };
+    pass(std::integral_constant<int, 0>{});
+    pass(std::integral_constant<int, 1>{});
 }
 
 // LUT: the instantiation for matrices with 4-bit rows (every step a general step with the lookup decode)
@@ -809,9 +819,7 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict_
         float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         const size_t at = (size_t)(m0 + r) * K + k0 + c;
         if constexpr (std::is_same<E, BwdEpi>::value) {
-            EpiRun<BwdEpi, 8> run;
-            epi_load<8>(epi, at, run);
-            with_act(epi.act, [&](auto A) __attribute__((always_inline)) { epi_store<decltype(A)::value, 8>(epi, at, v, v, run, out); });
+            epi_run<8>(epi, at, k0 + c, v, out);
         } else {
             store_run<8>(out + at, v);
         }

@@ -66,6 +66,7 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 #define LOWRA_FWD_COST4 0.62
 #endif
 
+constexpr int EPI_AHEAD = 4;               // token rows whose operands an epilogue asks for ahead
 constexpr int KS = 64;                     // contraction depth per step: one absmax group
 constexpr int AROWB = 128;                 // bytes per LDS activation row: 64 bf16 = 8 chunks of 16 B
 constexpr int ASTAGEB = 256 * AROWB;       // 32 KB per stage
@@ -643,6 +644,15 @@ __device__ __forceinline__ void fwd_tile(const GemmParams& p, const E& epi, cons
     if constexpr (std::is_same<E, FwdEpi>::value) {
         static_assert(128 * 1024 <= kFwdSmem, "128 rows of 256 fp32");
         const int c = tid & 31, r0 = tid >> 5;
+        const EpiTile<FwdEpi> tile = epi_tile(epi, p.out, (size_t)m0 * p.N + n0);
+        const bool col_ok = n0 + 8 * c < p.N;                      // N is a multiple of 8: a chunk is in or out as a whole
+        auto offset = [&](int j) __attribute__((always_inline)) -> uint32_t {
+            return col_ok && m0 + 8 * j + r0 < p.M ? (uint32_t)(8 * j + r0) * (uint32_t)p.N * 2u + (uint32_t)c * 16u : kNowhere;
+        };
+        EpiRun<FwdEpi, 8> run[EPI_AHEAD];
+        epi_fetch(tile, run, offset);
+        float b[8];
+        epi_bias<8>(epi, col_ok ? n0 + 8 * c : 0, b);
         auto pass = [&](auto T0_) __attribute__((always_inline)) {
             constexpr int t0 = decltype(T0_)::value, t1 = TM < t0 + 4 ? TM : t0 + 4;
             __syncthreads();                                       // the last readers of what is overwritten are done
@@ -666,10 +676,9 @@ __device__ __forceinline__ void fwd_tile(const GemmParams& p, const E& epi, cons
                     }
                 }
             __syncthreads();
-            if (n0 + 8 * c < p.N) {                                // N is a multiple of 8: a chunk is in or out as a whole
-                auto read = [&](int i, float (&v)[8]) __attribute__((always_inline)) { epi_read8<64>(smem, i * 8 + r0, c, v); };
-                epi_rows<8, 4 * (t1 - t0)>(epi, p.out, p.N, p.M, m0 + 32 * t0 + r0, n0 + 8 * c, read);
-            }
+            epi_rows<4 * t0, 4 * t1, 4 * TM>(epi, tile, b, run, offset, [&](int j, float (&v)[8]) __attribute__((always_inline)) {
+                epi_read8<64>(smem, (j - 4 * t0) * 8 + r0, c, v);
+            });
         };
         pass(int_c<0>{});
         if constexpr (TM > 4) pass(int_c<4>{});

@@ -95,10 +95,19 @@ __device__ __forceinline__ void mid_epilogue(const MidParams& p, const E& epi, c
         return;
     }
     if constexpr (!std::is_same<E, NoEpi>::value) {
-        constexpr int PT = mid_epi_tiles(TM);
+        constexpr int PT = mid_epi_tiles(TM), U = PT == 2 ? 4 : PT == 3 ? 3 : 2;
         const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
-#pragma unroll
-        for (int t0 = 0; t0 < TM; t0 += PT) {
+        const EpiTile<E> out = epi_tile(epi, p.out, (size_t)m0 * cols + c0);
+        const bool col_ok = c0 + 8 * c < cols;                        // cols is a multiple of 8
+        auto offset = [&](int j) __attribute__((always_inline)) -> uint32_t {
+            return col_ok && m0 + 16 * j + r0 < p.M ? (uint32_t)(16 * j + r0) * (uint32_t)cols * 2u + (uint32_t)c * 16u : kNowhere;
+        };
+        EpiRun<E, 8> run[U];
+        epi_fetch(out, run, offset);
+        float b[8];
+        epi_bias<8>(epi, col_ok ? c0 + 8 * c : 0, b);
+        auto pass = [&](auto T0_) __attribute__((always_inline)) {
+            constexpr int t0 = decltype(T0_)::value;
             __syncthreads();
 #pragma unroll
             for (int t = t0; t < t0 + PT; ++t)
@@ -107,10 +116,14 @@ __device__ __forceinline__ void mid_epilogue(const MidParams& p, const E& epi, c
                     *reinterpret_cast<float4*>(smem + epi_chunk<32>(32 * (t - t0) + fi, wave * 8 + 2 * vq + h)) =
                         make_float4(acc[t][4 * vq], acc[t][4 * vq + 1], acc[t][4 * vq + 2], acc[t][4 * vq + 3]);
             __syncthreads();
-            if (c0 + 8 * c < cols)                                    // cols is a multiple of 8
-                epi_rows<16, 2 * PT>(epi, p.out, cols, p.M, m0 + 32 * t0 + r0, c0 + 8 * c,
-                                     [&](int i, float (&v)[8]) __attribute__((always_inline)) { epi_read8<32>(smem, i * 16 + r0, c, v); });
-        }
+            epi_rows<2 * t0, 2 * (t0 + PT), 2 * TM>(epi, out, b, run, offset, [&](int j, float (&v)[8]) __attribute__((always_inline)) {
+                epi_read8<32>(smem, (j - 2 * t0) * 16 + r0, c, v);
+            });
+        };
+        pass(std::integral_constant<int, 0>{});
+        if constexpr (TM > PT) pass(std::integral_constant<int, PT>{});
+        if constexpr (TM > 2 * PT) pass(std::integral_constant<int, 2 * PT>{});
+        static_assert(TM <= 3 * PT, "");
         return;
     }
     __syncthreads();
@@ -741,11 +754,7 @@ __global__ __launch_bounds__(256) void mid_sum_kernel(const float4* __restrict__
     if constexpr (std::is_same<E, NoEpi>::value) {
         store_run<4>(out + at, v);
     } else {
-        EpiRun<E, 4> run;
-        float b[4];
-        epi_load<4>(epi, at, run);
-        epi_bias<4>(epi, col, b);
-        with_act(epi.act, [&](auto A) __attribute__((always_inline)) { epi_store<decltype(A)::value, 4>(epi, at, v, b, run, out); });
+        epi_run<4>(epi, at, col, v, out);
     }
 }
 

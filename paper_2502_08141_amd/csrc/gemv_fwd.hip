@@ -91,11 +91,8 @@ __device__ __forceinline__ void gemv_store(const GemvParams& p, NoEpi, int m, in
 }
 __device__ __forceinline__ void gemv_store(const GemvParams& p, const FwdEpi& epi, int m, int n, float v) {
     const size_t at = (size_t)m * p.N + n;
-    EpiRun<FwdEpi, 1> run;
-    float b[1], o[1] = {v};
-    epi_load<1>(epi, at, run);
-    epi_bias<1>(epi, n, b);
-    with_act(epi.act, [&](auto A) __attribute__((always_inline)) { epi_store<decltype(A)::value, 1>(epi, at, o, b, run, p.y); });
+    float o[1] = {v};
+    epi_run<1>(epi, at, n, o, p.y);
 }
 
 // FUSE: t comes from the workgroup itself (one round, r <= 16); else from the partial sums in p.tp

@@ -551,9 +551,7 @@ __device__ __forceinline__ void gb_sum_body(const GbItem* __restrict__ it, const
             if constexpr (std::is_same<E, BwdEpi>::value) {
                 float o[4] = {t.x, t.y, t.z, t.w};
                 const size_t at = (size_t)m * K + k;
-                EpiRun<BwdEpi, 4> run;
-                epi_load<4>(epi, at, run);
-                with_act(epi.act, [&](auto A) __attribute__((always_inline)) { epi_store<decltype(A)::value, 4>(epi, at, o, o, run, it->dX); });
+                epi_run<4>(epi, at, k, o, it->dX);
             } else {
                 gstore_u2(dX + (size_t)m * K + k, make_uint2(pack_bf16x2(t.x, t.y), pack_bf16x2(t.z, t.w)));
             }

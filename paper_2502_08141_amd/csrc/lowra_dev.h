@@ -82,6 +82,15 @@ __device__ __forceinline__ float4 load16_stream(const float4* p) {
     return make_float4(v.x, v.y, v.z, v.w);
 }
 
+// A buffer of `bytes` bytes for accesses with 32-bit byte offsets: past its end loads give zeros and stores do nothing, without a branch
+// or a mask around the access (a load under a condition shares its registers with the other side's values, and is waited for
+// before those are written).  A null pointer is an empty buffer.
+typedef __amdgpu_buffer_rsrc_t buffer_t;
+__device__ __forceinline__ buffer_t buffer_of(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, p ? bytes : 0u, 0x00027000);
+}
+constexpr uint32_t kNowhere = 0x80000000u;             // past the end of a buffer of less than 2^31 bytes, whatever small offset is added
+
 // Load the 8*bits bits of codes that cover elements [8u, 8u+8) of a packed row.
 __device__ __forceinline__ uint32_t load_codes8(const uint8_t* row, int u, int bits) {
     if (bits == 1) return row[u];

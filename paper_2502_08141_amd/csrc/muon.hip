@@ -35,45 +35,39 @@ constexpr int mu_tiles(int NT) { return NT * (NT + 1) / 2; }
 constexpr int mu_tile(int NT, int t1, int t2) { return t1 * NT - t1 * (t1 - 1) / 2 + (t2 - t1); }
 constexpr int mu_ld(int NT) { return 16 * NT + 2; }          // doubles per LDS row: 16 rows at one column lie 4 banks apart
 
-// The matrices are accessed through buffer descriptors: a quad that is not there has an offset past the end, reads as zeros and
-// is not written, without a branch or a mask around the access (a load under a condition shares its registers with the zeros of the
-// other lanes and is waited for before they are written: the first kernel took 1.3 times as long).  A null pointer is an empty buffer.
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
-__device__ __forceinline__ rsrc_t rsrc_of(const void* p, int elements, int size) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, p ? elements * size : 0, 0x00027000);
-}
-constexpr uint32_t MU_NONE = 0x80000000u;             // past every end: a matrix has less than 2^31 bytes
+// The matrices are accessed as buffers (lowra_dev.h): a quad that is not there has an offset past the end (with loads under masks the
+// first pass took 1.3 times as long).
 // A quad of fp32 from element e on.  VEC: quads are 16-byte aligned and whole or not there; else n of them are.
 template <bool VEC>
-__device__ __forceinline__ float4 load4(rsrc_t r, bool ok, uint32_t e, int n) {
+__device__ __forceinline__ float4 load4(buffer_t r, bool ok, uint32_t e, int n) {
     if constexpr (VEC) {
-        return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, ok ? e * 4 : MU_NONE, 0, 0));
+        return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, ok ? e * 4 : kNowhere, 0, 0));
     } else {
         float v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, ok && i < n ? (e + i) * 4 : MU_NONE, 0, 0));
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, ok && i < n ? (e + i) * 4 : kNowhere, 0, 0));
         return make_float4(v[0], v[1], v[2], v[3]);
     }
 }
 template <bool VEC>
-__device__ __forceinline__ void store4(rsrc_t r, bool ok, uint32_t e, int n, float4 v) {
+__device__ __forceinline__ void store4(buffer_t r, bool ok, uint32_t e, int n, float4 v) {
     if constexpr (VEC) {
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(g_u32x4_t, v), r, ok ? e * 4 : MU_NONE, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(g_u32x4_t, v), r, ok ? e * 4 : kNowhere, 0, 0);
     } else {
         const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x[i]), r, ok && i < n ? (e + i) * 4 : MU_NONE, 0, 0);
+        for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x[i]), r, ok && i < n ? (e + i) * 4 : kNowhere, 0, 0);
     }
 }
 template <bool VEC>
-__device__ __forceinline__ void store4_bf16(rsrc_t r, bool ok, uint32_t e, int n, float4 v) {
+__device__ __forceinline__ void store4_bf16(buffer_t r, bool ok, uint32_t e, int n, float4 v) {
     const uint32_t lo = pack_bf16x2(v.x, v.y), hi = pack_bf16x2(v.z, v.w);
     if constexpr (VEC) {
-        __builtin_amdgcn_raw_buffer_store_b64(g_u32x2_t{lo, hi}, r, ok ? e * 2 : MU_NONE, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b64(g_u32x2_t{lo, hi}, r, ok ? e * 2 : kNowhere, 0, 0);
     } else {
         const uint32_t x[4] = {lo, lo >> 16, hi, hi >> 16};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(x[i] & 0xffffu), r, ok && i < n ? (e + i) * 2 : MU_NONE, 0, 0);
+        for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(x[i] & 0xffffu), r, ok && i < n ? (e + i) * 2 : kNowhere, 0, 0);
     }
 }
 __device__ __forceinline__ float at4(const float4& v, int e) { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; }
@@ -99,7 +93,7 @@ __device__ __forceinline__ void muon_gram(const MuonItem& it, int first, int las
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int R = it.R, L = it.L;
-    const rsrc_t grad = rsrc_of(it.grad, R * L, 4), momentum = rsrc_of(it.momentum, R * L, 4), momentum_out = rsrc_of(it.momentum_out, R * L, 4);
+    const buffer_t grad = buffer_of(it.grad, (uint32_t)(R * L) * 4u), momentum = buffer_of(it.momentum, (uint32_t)(R * L) * 4u), momentum_out = buffer_of(it.momentum_out, (uint32_t)(R * L) * 4u);
     constexpr int STEP = mu_step(NT), LDW = STEP + 4, PER = STEP / 4;  // PER: lanes of a row
     // quad k of a lane in the step at c: its first element, whether it is there, and how many there are
     auto quad = [&](int c, int k, bool& ok, uint32_t& e) __attribute__((always_inline)) -> int {
@@ -342,8 +336,8 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int la
     const int lane = threadIdx.x & 63, x = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int R = it.R, L = it.L, n_all = R * L;
-    const rsrc_t grad = rsrc_of(it.grad, n_all, 4), momentum = rsrc_of(it.momentum_out, n_all, 4), weight = rsrc_of(it.weight, n_all, 4),
-                 weight_out = rsrc_of(it.weight_out, n_all, 4), update = rsrc_of(it.update, n_all, 4), weight_bf16 = rsrc_of(it.weight_bf16, n_all, 2);
+    const buffer_t grad = buffer_of(it.grad, (uint32_t)(n_all) * 4u), momentum = buffer_of(it.momentum_out, (uint32_t)(n_all) * 4u), weight = buffer_of(it.weight, (uint32_t)(n_all) * 4u),
+                 weight_out = buffer_of(it.weight_out, (uint32_t)(n_all) * 4u), update = buffer_of(it.update, (uint32_t)(n_all) * 4u), weight_bf16 = buffer_of(it.weight_bf16, (uint32_t)(n_all) * 2u);
     constexpr int PARTS = mu_parts(NT), SPAN = MU_SPAN / PARTS;       // wavefronts that share the result tiles of 64 elements
     const int part = wave % PARTS;
     for (int c = first + 64 * (wave / PARTS); c < last; c += SPAN) { // uniform
@@ -358,7 +352,7 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int la
             return WIDE ? last - l : R - s;
         };
         float4 u[NT][4];
-        auto load = [&](rsrc_t r, int t, int j) __attribute__((always_inline)) {
+        auto load = [&](buffer_t r, int t, int j) __attribute__((always_inline)) {
             uint32_t e;
             bool ok;
             const int n = quad(t, j, ok, e);
