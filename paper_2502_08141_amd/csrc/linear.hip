@@ -83,12 +83,22 @@ static size_t gemv_workspace_bytes(const lowra_layout& L, int r);
 static size_t linear_workspace_bytes_fp32(const lowra_layout& L, int op, int M, int r);
 static size_t bwd_split_bytes(const lowra_layout& L, int M);
 
+// Whether an input gradient with an epilogue is the streaming small-token kernel's.  Its three launches take 20 us and up and grow with
+// every token's partial results; the mid-token kernel takes 13 and as long for one token as for 32, but reads the codes slower.  Both
+// in one call each, rank 16: 4096 x 4096, 1 and 4 tokens 23.4 and 25.9 us against 21.0; 11008 x 4096 30.6 and 32.6 against 28.3;
+// 4096 x 11008 26.5 and 31.9 against 26.5; 5120 x 13824, 1, 4 and 8 tokens 28.5, 33.8 and 41.4 against 33.7.  (Calls without an epilogue
+// stay with the streaming kernel and its bits.)
+static bool bwd_epilogue_streams(const lowra_layout& L, int M) {
+    const double weights = 1e-6 * L.N * L.K;
+    return weights * (0.21 - 0.0195 * M) > 8.5 + 0.2 * M;
+}
+
 // The mid-token GEMM's plan for a call under LOWRA_PATH_AUTO (TM == 0: another kernel takes it).  `gemm`: no small-token
-// kernel takes the call.  `part_bytes`: workspace left for partial tiles.
-static MidPlan mid_plan_of(const lowra_layout& L, int op, int M, int r, int gemm, size_t part_bytes) {
+// kernel takes the call.  `part_bytes`: workspace left for partial tiles.  `few`: small-token calls are asked for too.
+static MidPlan mid_plan_of(const lowra_layout& L, int op, int M, int r, int gemm, size_t part_bytes, bool few = false) {
     MidPlan none{0, 0, 0, 0, 0};
     if (!gemm || L.G < 2 || M < 1) return none;
-    if (M <= 16 && (op == 0 ? gemv_fwd_supported(L, M) : gemv_stream_bwd_supported(L, M, r))) return none;
+    if (!few && M <= 16 && (op == 0 ? gemv_fwd_supported(L, M) : gemv_stream_bwd_supported(L, M, r))) return none;
     return plan_mid(op, L.N, L.K, M, L.n_by_bits[4] > 0, L.C, part_bytes);
 }
 static MidParams mid_params(const lowra_layout& L, const LinearArgs& a, int op, int RP, const uint16_t* side, const MidPlan& pl, size_t least) {
@@ -101,14 +111,14 @@ static MidParams mid_params(const lowra_layout& L, const LinearArgs& a, int op, 
     p.tiles_c = pl.tiles_c; p.tiles_m = pl.tiles_m; p.tile0 = 0; p.ntiles = 0; p.splits = pl.splits; p.per_split = pl.per_split;
     return p;
 }
-static MidPlan mid_plan_call(const lowra_layout& L, const LinearArgs& a, int op, bool gemm) {
+static MidPlan mid_plan_call(const lowra_layout& L, const LinearArgs& a, int op, bool gemm, bool few = false) {
     const size_t least = align256(linear_workspace_min(L, op, a.M, a.r));
     const size_t room = a.workspace_bytes > least ? a.workspace_bytes - least : 0;
     if (a.pieces) {
         const MidPlan whole = mid_plan_of(L, op, a.M, a.r, gemm, ~(size_t)0);
         if (whole.splits <= 1 || mid_pieces(whole, room) > 0) return whole;
     }
-    return mid_plan_of(L, op, a.M, a.r, gemm, room);
+    return mid_plan_of(L, op, a.M, a.r, gemm, room, few);
 }
 size_t linear_workspace_min(const lowra_layout& L, int op, int M, int r) {
     return align256(linear_workspace_bytes_fp32(L, op, M, r)) + expanded_scale_bytes(L);
@@ -120,7 +130,7 @@ static size_t few_bytes(const lowra_layout& L, int op, int M, int r) {
 // that product is done, for the partial tiles of a mid-token GEMM's splits
 size_t linear_workspace_bytes(const lowra_layout& L, int op, int M, int r) {
     const size_t least = linear_workspace_min(L, op, M, r);
-    const MidPlan pl = mid_plan_of(L, op, M, r, 1, ~(size_t)0);
+    const MidPlan pl = mid_plan_of(L, op, M, r, 1, ~(size_t)0, op == 1 && M <= 16 && !bwd_epilogue_streams(L, M));
     const size_t more = std::max(pl.splits > 1 ? mid_part_bytes(pl) : 0, few_bytes(L, op, M, r));   // (with few tokens too: LOWRA_PATH_GEMM)
     return more ? align256(least) + more : least;
 }
@@ -230,12 +240,14 @@ hipError_t launch_linear_fwd(const lowra_layout& L, const LinearArgs& a_in, int 
 hipError_t launch_linear_bwd_input(const lowra_layout& L, const LinearArgs& a_in, int path, hipStream_t st) {
     if (a_in.M == 0) return hipSuccess;
     LinearArgs a;
-    const MidPlan mid = mid_plan_call(L, a_in, 1, path != 2);
-    hipError_t e_scales = with_fp32_scales(L, 1, a_in, a, mid.TM > 0 || (path != 2 && gemv_stream_bwd_supported(L, a_in.M, a_in.r)), st);
+    const bool few = a_in.bwd_epi && path == 0 && a_in.M <= 16 && !bwd_epilogue_streams(L, a_in.M);
+    const MidPlan mid = mid_plan_call(L, a_in, 1, path != 2, few);
+    const bool stream = path != 2 && !(few && mid.TM > 0) && gemv_stream_bwd_supported(L, a_in.M, a_in.r);
+    hipError_t e_scales = with_fp32_scales(L, 1, a_in, a, mid.TM > 0 || stream, st);
     if (e_scales != hipSuccess) return e_scales;
     // Few tokens: the streaming kernel reads the codes once at the memory's pace (the GEMM below would pad the tokens
     // to a 256-row tile).  LOWRA_PATH_GEMM keeps the GEMM.
-    if (path != 2 && gemv_stream_bwd_supported(L, a.M, a.r)) {
+    if (stream) {
         KernelTimer timer(st);
         return launch_gemv_stream_bwd(L, a, st);
     }

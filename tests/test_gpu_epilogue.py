@@ -75,6 +75,29 @@ def test_256_column_kernels(size, mix, act):
         lowra.lowra_set_linear_path(lowra.PATH_AUTO)
 
 
+@pytest.mark.parametrize("path", [lowra.PATH_AUTO, lowra.PATH_GEMV])
+@pytest.mark.parametrize("M", [1, 5, 16])
+def test_few_tokens_back_in_either_kernel(M, path):
+    """The mid-token kernel under LOWRA_PATH_AUTO, the streaming one under LOWRA_PATH_GEMV, with a whole workspace and a small one."""
+    L = ExactLayer(520, 1024, M, 16, seed=15, bf16_scales=M == 5)
+    z, mul, res = normal((M, L.K), 1, 2.0), normal((M, L.K), 2), normal((M, L.K), 3)
+    lowra.lowra_set_linear_path(path)
+    try:
+        for act in ("none", "gelu", "silu"):
+            dX, dmul = bwd(L, act, z=z, mul=mul, residual=res, workspace=L.workspace(lowra.OP_LINEAR_BWD_INPUT))
+            check_bwd(dX, dmul, L.g, act, z=z, mul=mul, residual=res)
+    finally:
+        lowra.lowra_set_linear_path(lowra.PATH_AUTO)
+
+
+def test_few_tokens_of_a_large_matrix_stream():
+    """Where the streaming kernel is the faster one for one token (weights past 46 million)."""
+    L = ExactLayer(4104, 11776, 1, 8, seed=16, mix=(0.5, 0.5, 0.0))
+    z = normal((1, L.K), 1, 2.0)
+    dX, _ = bwd(L, "gelu", z=z, workspace=L.workspace(lowra.OP_LINEAR_BWD_INPUT))
+    check_bwd(dX, None, L.g, "gelu", z=z)
+
+
 @pytest.mark.parametrize("tiling", [(256, 256, 0), (192, 192, 0), (128, 128, 0), (256, 192, 1), (256, 128, 2), (192, 128, 1)])
 def test_forward_tilings(tiling):
     L = ExactLayer(776, 256, 530, 16, seed=4)
