@@ -199,7 +199,7 @@ enum { LOWRA_ACT_NONE = 0, LOWRA_ACT_RELU = 1, LOWRA_ACT_GELU = 2, LOWRA_ACT_GEL
  * null: not there.  v and y are computed in fp32 from the fp32 sums and rounded once.
  *   residual may be y itself (the call adds to y); otherwise no operand overlaps y or z.
  * Arguments, workspace and errors otherwise as in lowra_linear_fwd; INVALID_ARG also for a null or unknown epilogue and when the
- * current device is not the layout's. */
+ * current device is not the layout's; UNSUPPORTED also from N = 2^22 on. */
 typedef struct lowra_fwd_epilogue {
     int act;                    /* LOWRA_ACT_* */
     const uint16_t* bias;       /* [N] */
@@ -218,7 +218,8 @@ lowra_status lowra_linear_fwd_act(const lowra_layout* layout, const uint8_t* pac
  * x by another way.  z (with an activation, or when dmul is asked for), mul, residual: bf16 [M,K] dev | dX, dmul bf16 [M,K] dev (out);
  * null: not there; dmul needs mul.  g stays in fp32; each output is rounded once.
  *   residual may be dX itself; otherwise no operand overlaps an output.
- * Arguments, workspace and errors otherwise as in lowra_linear_bwd_input; INVALID_ARG also as above, and for a missing z or mul. */
+ * Arguments, workspace and errors otherwise as in lowra_linear_bwd_input; INVALID_ARG also as above, and for a missing z or mul;
+ * UNSUPPORTED also for N == 0 (with tokens) and from K = 2^22 on. */
 typedef struct lowra_bwd_epilogue {
     int act;
     const uint16_t* z;
@@ -234,10 +235,10 @@ lowra_status lowra_linear_bwd_input_act(const lowra_layout* layout, const uint8_
 /* The same for a gradient that comes from outside, with the bias gradient: dY is the gradient of act(z) mul,
  *   dZ = dY mul act'(z);   dmul = dY act(z);   db[n] = sum_m dZ[m,n], of dZ in fp32 before it is rounded
  * dY [M,N] bf16 dev | z, mul [M,N] bf16 dev or null, as above | dZ, dmul [M,N] bf16 dev (out), db [N] fp32 dev (out), each or null
- *   (with LOWRA_ACT_NONE and no mul dZ is dY: pass null for the bias gradient alone); dZ may be dY itself.
+ *   (with LOWRA_ACT_NONE and no mul dZ is dY: pass null for the bias gradient alone); dZ may be dY itself; otherwise nothing overlaps an output.
  *   workspace: dev, >= lowra_act_bwd_workspace_bytes(M, N), 16-byte aligned; unused without db.
  * The sums are added in a fixed order.  M == 0 writes zeros to db.  INVALID_ARG: a negative size, an unknown activation, a missing
- * dY, z or mul, no output at all; UNSUPPORTED: N % 8 != 0; MISALIGNED; WORKSPACE_TOO_SMALL. */
+ * dY, z or mul, no output at all; UNSUPPORTED: N % 8 != 0, M or N above 2^30; MISALIGNED; WORKSPACE_TOO_SMALL. */
 size_t lowra_act_bwd_workspace_bytes(int M, int N);
 lowra_status lowra_act_bwd(int M, int N, int act, const uint16_t* dY, const uint16_t* z, const uint16_t* mul, uint16_t* dZ,
                            uint16_t* dmul, float* db, void* workspace, size_t workspace_bytes, void* stream);
@@ -311,8 +312,9 @@ lowra_status lowra_adapter_grads_from_side(const lowra_layout* layout, const uin
  *   workspace: dev, >= lowra_muon_batch_workspace_bytes(n, items), 16-byte aligned, owned by the caller, used by every run (runs
  *   of one batch must not overlap).
  * create: INVALID_ARG (null / n <= 0 / a non-positive size / a missing pointer: grad, momentum, momentum_out, and weight with
- * weight_out or update are needed, weight_bf16 needs weight), UNSUPPORTED (a short side above 64, 2^29 elements or more), MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY,
- * HIP_ERROR.  create allocates device memory for the descriptors and copies them synchronously; destroy frees.
+ * weight_out or update are needed, weight_bf16 needs weight; an output or the workspace that overlaps anything else of the batch,
+ * so no tensor is in it twice), UNSUPPORTED (a short side above 64, 2^29 elements or more), MISALIGNED, WORKSPACE_TOO_SMALL,
+ * OUT_OF_MEMORY, HIP_ERROR.  create allocates device memory for the descriptors and copies them synchronously; destroy frees.
  * run: INVALID_ARG (null, steps outside 1..64, eps not above zero, another device than the one of create), HIP_ERROR. */
 typedef struct lowra_muon_item {
     int rows, cols;              /* min(rows, cols) <= 64 */

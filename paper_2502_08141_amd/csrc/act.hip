@@ -3,7 +3,8 @@
 //
 // Memory bound: every operand is read or written once, 16 bytes per lane.  A thread keeps eight columns and walks down the
 // tokens, so that their sums stay in registers; the wavefronts of a workgroup meet in LDS, workgroups in the workspace, both
-// added in a fixed order.
+// added in a fixed order.  Bias gradient alone of 4096 x 11008 (a read of 90 MB): 17.2 us, 5.2 TB/s, and 2.3 to add up the
+// chunks; gelu of 777 x 4096 (19 MB): 7.4 us and 2.3, between launch latency and bandwidth.
 #include <algorithm>
 
 #include "epilogue.h"
@@ -15,6 +16,7 @@ namespace {
 
 constexpr int ACT_COLS = 512;            // columns per workgroup: 64 lanes x 8
 constexpr int ACT_WAVES = 4;
+static_assert(kActMaxSize <= 1 << 30, "rows and columns are rounded up in int");
 
 // Token rows per workgroup: enough workgroups to fill the chip several times, about sixteen rows each (777 x 4096, gelu: 9.5 us; eight
 // 9.55, thirty-two 10.4).  Few tokens are one workgroup's, which saves the launch that adds up the chunks: 24 x 4096, gelu, 9.4 -> 6.2;

@@ -479,6 +479,7 @@ lowra_status lowra_linear_fwd_act(const lowra_layout* L, const uint8_t* packed, 
     if (!e || !known_act(e->act)) return LOWRA_INVALID_ARG;
     const lowra_status st = check_linear(L, LOWRA_OP_LINEAR_FWD, packed, absmax, mappings, x, M, A, B, r, y, workspace, workspace_bytes);
     if (st != LOWRA_OK || M == 0 || L->N == 0) return st;
+    if (L->N > lowra::kEpiMaxColumns) return LOWRA_UNSUPPORTED;
     if (!aligned16(e->bias) || !aligned16(e->mul) || !aligned16(e->residual) || !aligned16(e->z)) return LOWRA_MISALIGNED;
     if (e->z && (e->z == y || e->z == e->residual || e->z == e->mul)) return LOWRA_INVALID_ARG;
     if (!on_current_device(L)) return LOWRA_INVALID_ARG;
@@ -495,6 +496,7 @@ lowra_status lowra_linear_bwd_input_act(const lowra_layout* L, const uint8_t* pa
     if (!e || !known_act(e->act) || (e->dmul && !e->mul)) return LOWRA_INVALID_ARG;
     const lowra_status st = check_linear(L, LOWRA_OP_LINEAR_BWD_INPUT, packed, absmax, mappings, dY, M, A, B, r, dX, workspace, workspace_bytes);
     if (st != LOWRA_OK || M == 0) return st;
+    if (L->K > lowra::kEpiMaxColumns) return LOWRA_UNSUPPORTED;
     if (L->N == 0) return LOWRA_UNSUPPORTED;                      // (an empty contraction is not worth an epilogue of its own)
     if ((e->act != LOWRA_ACT_NONE || e->dmul) && !e->z) return LOWRA_INVALID_ARG;
     if (!aligned16(e->z) || !aligned16(e->mul) || !aligned16(e->residual) || !aligned16(e->dmul)) return LOWRA_MISALIGNED;
@@ -507,12 +509,13 @@ lowra_status lowra_linear_bwd_input_act(const lowra_layout* L, const uint8_t* pa
                ? LOWRA_OK : LOWRA_HIP_ERROR;
 }
 
-size_t lowra_act_bwd_workspace_bytes(int M, int N) { return M > 0 && N > 0 ? lowra::act_bwd_workspace_bytes(M, N) : 0; }
+static bool act_sizes(int M, int N) { return N % 8 == 0 && M <= lowra::kActMaxSize && N <= lowra::kActMaxSize; }
+size_t lowra_act_bwd_workspace_bytes(int M, int N) { return M > 0 && N > 0 && act_sizes(M, N) ? lowra::act_bwd_workspace_bytes(M, N) : 0; }
 
 lowra_status lowra_act_bwd(int M, int N, int act, const uint16_t* dY, const uint16_t* z, const uint16_t* mul, uint16_t* dZ,
                            uint16_t* dmul, float* db, void* workspace, size_t workspace_bytes, void* stream) {
     if (M < 0 || N < 0 || !known_act(act) || (dmul && !mul) || (!dZ && !dmul && !db)) return LOWRA_INVALID_ARG;
-    if (N % 8 != 0) return LOWRA_UNSUPPORTED;
+    if (!act_sizes(M, N)) return LOWRA_UNSUPPORTED;
     if (N == 0) return LOWRA_OK;
     if (!aligned16(db)) return LOWRA_MISALIGNED;
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -733,6 +736,29 @@ static lowra::MuonItem muon_item(const lowra_muon_item& it) {
     return m;
 }
 
+// whether an output of a batch overlaps anything but the input that it replaces
+static bool muon_overlaps(const std::vector<lowra::MuonItem>& items, const void* workspace, size_t workspace_bytes) {
+    struct Range { uintptr_t from, to; bool out; };
+    std::vector<Range> v{{reinterpret_cast<uintptr_t>(workspace), reinterpret_cast<uintptr_t>(workspace) + workspace_bytes, true}};
+    for (const lowra::MuonItem& it : items) {
+        auto add = [&](const void* p, size_t bytes, bool out) {
+            if (p) v.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (size_t)it.R * it.L * bytes, out});
+        };
+        add(it.grad, 4, false);
+        if (it.momentum != it.momentum_out) add(it.momentum, 4, false);
+        if (it.weight != it.weight_out) add(it.weight, 4, false);
+        add(it.momentum_out, 4, true); add(it.weight_out, 4, true); add(it.update, 4, true); add(it.weight_bf16, 2, true);
+    }
+    std::sort(v.begin(), v.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t any = 0, out = 0;                                   // how far what came before reaches
+    for (const Range& r : v) {
+        if (r.from < out || (r.out && r.from < any)) return true;
+        any = std::max(any, r.to);
+        if (r.out) out = std::max(out, r.to);
+    }
+    return false;
+}
+
 size_t lowra_muon_batch_workspace_bytes(int n, const lowra_muon_item* items) {
     if (n <= 0 || !items) return 0;
     try {
@@ -768,7 +794,9 @@ lowra_status lowra_muon_batch_create(int n, const lowra_muon_item* items, void* 
     try {
         std::vector<lowra::MuonItem> v;
         for (int i = 0; i < n; ++i) v.push_back(muon_item(items[i]));
-        if (workspace_bytes < lowra::muon_workspace_bytes(n, v.data())) return LOWRA_WORKSPACE_TOO_SMALL;
+        const size_t need = lowra::muon_workspace_bytes(n, v.data());
+        if (workspace_bytes < need) return LOWRA_WORKSPACE_TOO_SMALL;
+        if (muon_overlaps(v, workspace, need)) return LOWRA_INVALID_ARG;
         b = new lowra_muon_batch;
         if (hipGetDevice(&b->device) != hipSuccess || lowra::muon_build(v, workspace, b->groups) != hipSuccess) st = LOWRA_HIP_ERROR;
     } catch (const std::bad_alloc&) {

@@ -212,6 +212,7 @@ __device__ __forceinline__ void epi_run(const E& e, size_t at, int col, float (&
 
 // ---- the epilogue of a whole output tile: operands and results as buffers that start at the tile's first row (32-bit offsets; an
 // operand that is not there is an empty buffer, a row past the last token has an offset past the end)
+constexpr int kEpiMaxColumns = (1 << 22) - 8;          // 256 rows of a tile stay below 2^31 bytes
 template <class E> struct EpiTile;
 template <> struct EpiTile<FwdEpi> { buffer_t mul, residual, second, out; };
 template <> struct EpiTile<BwdEpi> { buffer_t z, mul, residual, second, out; };
@@ -241,7 +242,8 @@ __device__ __forceinline__ void epi_load(const EpiTile<BwdEpi>& t, uint32_t off,
 }
 // Eight columns (from `col` on) of a thread's token rows, numbers FROM .. TO - 1 of TOTAL here: offset(j) is where the j-th one's are and
 // read(j, v) gives its products.  run[j % U] holds its operands, asked for U rows ahead, over the passes through LDS: nothing else
-// covers their way where a workgroup is alone on its unit.
+// covers their way where a workgroup is alone on its unit.  (Input gradient of 4096 x 11008, 4096 tokens, through
+// a silu gate: eight rows' loads together from pointers within a pass 519 us, so 401, with two rows ahead 417; without an epilogue 353.)
 template <int U, class E, class Offset>
 __device__ __forceinline__ void epi_fetch(const EpiTile<E>& t, EpiRun<E, 8> (&run)[U], Offset&& offset) {
 #pragma unroll
@@ -277,6 +279,7 @@ __device__ __forceinline__ void epi_read8(const uint8_t* smem, int row, int c8, 
 }
 
 // ---- act.hip
+constexpr int kActMaxSize = 1 << 30;                   // of M and of N
 size_t act_bwd_workspace_bytes(int M, int N);
 // e.residual must be null; dZ null: only the sums (and dmul)
 hipError_t launch_act_bwd(int M, int N, const BwdEpi& e, const uint16_t* dY, uint16_t* dZ, float* db, void* workspace, hipStream_t st);

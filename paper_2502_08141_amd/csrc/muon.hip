@@ -10,8 +10,9 @@
 //
 // Precision.  A direction of u that is small beside the largest grows by a = 3.4 in every step, 485 in five, and an error of G
 // by a^2 in every step: in 32 bits X would be off by 1e-4 and more where the direct products are off by 1e-6 (R = 64, singular
-// values over three decades).  G, its polynomial and the products are in 64 bits (off by 3e-13), on v_mfma_f64_16x16x4: 32 multiply-adds
-// per element and 16 ranks in each pass are a quarter of what the memory takes at R = 16, half at R = 64.
+// values over three decades).  G, its polynomial and the products are in 64 bits (off by 3e-13), on v_mfma_f64_16x16x4, at
+// 68 TFLOP/s here, a library product's rate: per element the first pass takes 0.5 ps of
+// them at R = 16 and 1.2 at R = 64 beside 2.4 ps of the memory (12 bytes), the last 0.5 and 1.9 beside 3.5 (18 bytes).
 //
 // Layouts of v_mfma_f64_16x16x4: A[i][k] and B[k][i] in lane i + 16 k; D[row][column] in lane column + 16 q, register v, with row = q + 4 v.
 #include <algorithm>
@@ -100,7 +101,7 @@ __device__ __forceinline__ void muon_gram(const MuonItem& it, int first, int las
         if (WIDE) {
             const int row = k * (64 / PER) + lane / PER, col = c + 4 * (lane % PER);
             ok = row < R && col < last;
-            e = (uint32_t)(row * L + col);
+            e = (uint32_t)row * (uint32_t)L + (uint32_t)col;               // (where nothing is, it may wrap)
             return last - col;
         }
         const int f = 4 * (k * 64 + lane), have = min(last - c, STEP) * R;
@@ -348,7 +349,7 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int la
             const int s = WIDE ? 16 * t + y + 4 * j : 16 * t + 4 * y;
             const int l = WIDE ? c + 4 * x : c + 16 * j + x;
             ok = s < R && l < last;
-            e = (uint32_t)(WIDE ? s * L + l : l * R + s);
+            e = WIDE ? (uint32_t)s * (uint32_t)L + (uint32_t)l : (uint32_t)l * (uint32_t)R + (uint32_t)s;
             return WIDE ? last - l : R - s;
         };
         float4 u[NT][4];

@@ -406,6 +406,8 @@ def _linear_act(fn, name, op, layout, packed, absmax, mappings, act_in, cols_in,
     if act_in.device.index != torch.cuda.current_device() or packed.device != act_in.device:
         raise ValueError("tensors on another device than the current one")
     M, r = int(act_in.shape[0]), 0
+    if M > 0x7fffffff:
+        raise ValueError("too many tokens")
     if A is not None and B is not None and A.shape[0] > 0:
         _dev(A, torch.bfloat16, "A"); _dev(B, torch.bfloat16, "B")
         r = int(A.shape[0])
@@ -486,6 +488,8 @@ def lowra_act_bwd(dY, act: int, z=None, mul=None, bias_grad: bool = False, works
         raise ValueError("tensors on another device than the current one")
     shape, act = tuple(dY.shape), int(act)
     M, N = shape
+    if max(shape) > 0x7fffffff:
+        raise ValueError("dY: too large")
     _operand(z, shape, "z", dY.device); _operand(mul, shape, "mul", dY.device)
     dZ = torch.empty_like(dY) if act != ACT_NONE or mul is not None else None
     dmul = torch.empty_like(dY) if mul is not None else None
@@ -738,6 +742,8 @@ class MuonBatch:
                 _dev(t, dtype, name)
                 if t.dim() != 2 or t.shape != it.grad.shape or t.device != device:
                     raise ValueError(f"item {i}: {name}: shape or device mismatch")
+            if max(it.grad.shape) > 0x7fffffff:
+                raise ValueError(f"item {i}: too large")
             arr[i] = MuonItemRecord(int(it.grad.shape[0]), int(it.grad.shape[1]), float(it.scale), *(_ptr(t) for _, t, _ in fields))
             self._keep += [t for _, t, _ in fields]
         if device.index != torch.cuda.current_device():

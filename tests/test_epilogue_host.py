@@ -16,6 +16,10 @@ def test_act_bwd_refusals():
                dict(act=0, mul=2 * P, dmul=3 * P, z=None)):
         assert call(**kw) == lowra.INVALID_ARG, kw
     assert call(N=12) == lowra.UNSUPPORTED
+    for kw in (dict(M=(1 << 30) + 1), dict(N=(1 << 30) + 8), dict(M=0x7fffffff, db=P, ws=P, nb=1 << 40)):       # rows are rounded up in int
+        assert call(**kw) == lowra.UNSUPPORTED, kw
+    assert lowra.lowra_act_bwd_workspace_bytes(0x7fffffff, 8) == 0 and lowra.lowra_act_bwd_workspace_bytes(64, 12) == 0
+    assert lowra.lowra_act_bwd_workspace_bytes(1 << 30, 8) > 0
     for kw in (dict(dY=P + 8), dict(z=P + 2), dict(dZ=P + 4), dict(mul=P + 2), dict(db=P + 4)):
         assert call(**kw) == lowra.MISALIGNED, kw
     need = lowra.lowra_act_bwd_workspace_bytes(4096, 1024)

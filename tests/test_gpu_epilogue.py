@@ -305,6 +305,17 @@ def test_refusals():
     torch.cuda.synchronize()
 
 
+def test_more_columns_than_a_tile_addresses():
+    """256 rows of 2^22 columns reach 2^31 bytes: refused, where the call without an epilogue goes on."""
+    for N, K, fn, cols_in in ((1 << 22, 64, lowra.lowra_linear_fwd_act, 64), (8, 1 << 22, lowra.lowra_linear_bwd_input_act, 8)):
+        layout = lowra.Layout(K, np.full(N, 2, np.uint8), np.zeros(N, np.uint8), np.array([2], np.uint8))
+        packed = torch.zeros(layout.packed_bytes, dtype=torch.uint8, device="cuda")
+        absmax, mappings = torch.zeros((N, K // 64), device="cuda"), torch.zeros((1, 16), device="cuda")
+        with pytest.raises(lowra.LowraError) as e:
+            fn(layout, packed, absmax, mappings, torch.zeros((1, cols_in), dtype=torch.bfloat16, device="cuda"), None, None, 1.0, lowra.ACT_NONE)
+        assert e.value.status == lowra.UNSUPPORTED
+
+
 def test_graph_replays():
     L = ExactLayer(520, 1024, 64, 16, seed=11)
     few = ExactLayer(520, 1024, 4, 16, seed=12)

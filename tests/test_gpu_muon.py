@@ -220,6 +220,11 @@ def test_refusals():
     with pytest.raises(lowra.LowraError) as e:
         lowra.MuonBatch([lowra.MuonItem(**(ok | dict(grad=off)))])
     assert e.value.status == lowra.MISALIGNED
+    with pytest.raises(lowra.LowraError) as e:
+        lowra.MuonBatch([lowra.MuonItem(**ok), lowra.MuonItem(**ok)])
+    assert e.value.status == lowra.INVALID_ARG
+    shared = lowra.MuonBatch([lowra.MuonItem(**ok), lowra.MuonItem(z, z.clone(), z.clone())])       # inputs may be
+    shared.close()
     b = lowra.MuonBatch([lowra.MuonItem(**ok)])
     for kw in (dict(steps=0), dict(steps=65), dict(eps=0.0), dict(eps=float("nan"))):
         with pytest.raises(lowra.LowraError) as e:
