@@ -14,45 +14,53 @@ namespace lowra {
 
 namespace {
 
-constexpr int ACT_COLS = 512;            // columns per workgroup: 64 lanes x 8
-constexpr int ACT_WAVES = 4;
-static_assert(kActMaxSize <= 1 << 30, "rows and columns are rounded up in int");
+// Eight columns to a thread, LANES threads side by side; the rest of the workgroup has token rows of its own.  64 lanes read whole
+// rows, and the tokens are cut between workgroups whose sums a second launch adds up.  8 and 4 lanes (64 and 32 columns, 1024
+// threads) leave all tokens to one workgroup and need no second launch, but few units work.  Both ways, with bias gradient:
+//   gelu, 4096 columns, 24, 400, 777, 1000 tokens     9.5, 9.6, 10.2, 10.7 us in chunks; 8 lanes 6.3, 7.2, 12.2, 14.8; 4 lanes 6.3, 6.7, 9.9, 11.5
+//   gelu, 11008 columns, 160, 400, 777, 1200 tokens   9.7, 12.0, 15.0, 19.2 in chunks; 8 lanes 6.4, 9.8, 14.4, 19.1; 4 lanes 7.9, 13.2, 19.7, 27.6
+//   the sums alone, 4096 tokens of 1024, 2816, 4096 columns   8.6, 10.8, 11.8 in chunks; 8 lanes 9.7, 11.3, 11.7; 1200 tokens 8.6 and 5.5
+constexpr int act_threads(int LANES) { return LANES == 64 ? 256 : 1024; }
+int act_lanes(int M, int N, bool sums_alone) {
+    if (M > (sums_alone ? 2400 : 800) || N > 1 << 22) return 64;      // (a launch has less than 2^32 threads)
+    return !sums_alone && N <= 32 * device_compute_units() ? 4 : 8;
+}
 
 // Token rows per workgroup: enough workgroups to fill the chip several times, about sixteen rows each (777 x 4096, gelu: 9.5 us; eight
-// 9.55, thirty-two 10.4).  Few tokens are one workgroup's, which saves the launch that adds up the chunks: 24 x 4096, gelu, 9.4 -> 6.2;
-// 64 are too many for it (9.1 -> 10.3).
-int act_rows(int M, int N) {
-    if (M <= 48) return M;
-    const int strips = (N + ACT_COLS - 1) / ACT_COLS, want = 8 * device_compute_units();
+// 9.55, thirty-two 10.4).
+int act_rows(int M, int N, int lanes) {
+    if (lanes < 64) return M;
+    const int strips = (N + 511) / 512, want = 8 * device_compute_units();
     const int chunks = std::max(1, std::min((M + 15) / 16, (want + strips - 1) / strips));
     return (M + chunks - 1) / chunks;
 }
-int act_chunks(int M, int N) { const int rows = act_rows(M, N); return rows ? (M + rows - 1) / rows : 0; }
 
-__global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(int M, int N, int rows, BwdEpi e, const uint16_t* dY, uint16_t* dZ, float* sums) {
-    __shared__ float red[ACT_WAVES][8][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int col = blockIdx.x * ACT_COLS + lane * 8;
+template <int LANES>
+__global__ __launch_bounds__(act_threads(LANES)) void act_bwd_kernel(int M, int N, int rows, BwdEpi e, const uint16_t* dY, uint16_t* dZ, float* sums) {
+    constexpr int THREADS = act_threads(LANES), WAVES = THREADS / 64, STEP = THREADS / LANES;
+    __shared__ float red[WAVES][8][LANES];
+    const int lane = threadIdx.x % LANES, wave = threadIdx.x >> 6;
+    const int col = blockIdx.x * (8 * LANES) + lane * 8;
     const int m0 = blockIdx.y * rows, m1 = min(m0 + rows, M);
     float total[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (col < N) {                                                  // N is a multiple of 8
         with_act(e.act, [&](auto A) {
             constexpr int ACT = decltype(A)::value;
             constexpr int U = 4;                                    // rows whose operands are asked for together
-            for (int m = m0 + wave; m < m1; m += U * ACT_WAVES) {
+            for (int m = m0 + threadIdx.x / LANES; m < m1; m += U * STEP) {
                 Bf16Run<8> g[U];
                 EpiRun<BwdEpi, 8> r[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    if (m + u * ACT_WAVES < m1) {
-                        const size_t at = (size_t)(m + u * ACT_WAVES) * N + col;
+                    if (m + u * STEP < m1) {
+                        const size_t at = (size_t)(m + u * STEP) * N + col;
                         load_run<8>(dY + at, g[u]);
                         epi_load<8>(e, at, r[u]);
                     }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    if (m + u * ACT_WAVES < m1) {
-                        const size_t at = (size_t)(m + u * ACT_WAVES) * N + col;
+                    if (m + u * STEP < m1) {
+                        const size_t at = (size_t)(m + u * STEP) * N + col;
                         float v[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) v[i] = g[u][i];
@@ -66,11 +74,20 @@ __global__ __launch_bounds__(ACT_WAVES * 64) void act_bwd_kernel(int M, int N, i
     }
     if (!sums) return;                                              // uniform
 #pragma unroll
-    for (int i = 0; i < 8; ++i) red[wave][i][lane] = total[i];
+    for (int s = LANES; s < 64; s *= 2)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) total[i] += __shfl_xor(total[i], s);
+    if ((threadIdx.x & 63) < LANES) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) red[wave][i][lane] = total[i];
+    }
     __syncthreads();
-    for (int o = threadIdx.x; o < ACT_COLS; o += ACT_WAVES * 64) {
-        const int c = blockIdx.x * ACT_COLS + o;
-        if (c < N) sums[(size_t)blockIdx.y * N + c] = ((red[0][o & 7][o >> 3] + red[1][o & 7][o >> 3]) + red[2][o & 7][o >> 3]) + red[3][o & 7][o >> 3];
+    for (int o = threadIdx.x; o < 8 * LANES; o += THREADS) {
+        const int c = blockIdx.x * (8 * LANES) + o;
+        float v = red[0][o & 7][o >> 3];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += red[w][o & 7][o >> 3];
+        if (c < N) sums[(size_t)blockIdx.y * N + c] = v;
     }
 }
 
@@ -96,14 +113,21 @@ __global__ __launch_bounds__(256) void act_sum_kernel(const float* __restrict__ 
 }  // namespace
 
 size_t act_bwd_workspace_bytes(int M, int N) {
-    const int chunks = act_chunks(M, N);
-    return chunks > 1 ? (size_t)chunks * N * sizeof(float) : 0;
+    size_t most = 0;
+    for (const bool sums_alone : {false, true}) {
+        const int rows = act_rows(M, N, act_lanes(M, N, sums_alone));
+        if (rows < M) most = (size_t)((M + rows - 1) / rows) * N * sizeof(float);
+    }
+    return most;
 }
 
 hipError_t launch_act_bwd(int M, int N, const BwdEpi& e, const uint16_t* dY, uint16_t* dZ, float* db, void* workspace, hipStream_t st) {
-    const int rows = act_rows(M, N), chunks = act_chunks(M, N);
+    const int lanes = db ? act_lanes(M, N, !dZ && !e.dmul) : 64, rows = act_rows(M, N, lanes), chunks = (M + rows - 1) / rows;
     float* sums = !db ? nullptr : chunks > 1 ? static_cast<float*>(workspace) : db;
-    act_bwd_kernel<<<dim3((unsigned)((N + ACT_COLS - 1) / ACT_COLS), (unsigned)chunks), dim3(ACT_WAVES * 64), 0, st>>>(M, N, rows, e, dY, dZ, sums);
+    const dim3 grid((unsigned)((N + 8 * lanes - 1) / (8 * lanes)), (unsigned)chunks), block(act_threads(lanes));
+    if (lanes == 64) act_bwd_kernel<64><<<grid, block, 0, st>>>(M, N, rows, e, dY, dZ, sums);
+    else if (lanes == 8) act_bwd_kernel<8><<<grid, block, 0, st>>>(M, N, rows, e, dY, dZ, sums);
+    else act_bwd_kernel<4><<<grid, block, 0, st>>>(M, N, rows, e, dY, dZ, sums);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess || !db || chunks == 1) return err;
     act_sum_kernel<<<dim3((unsigned)((N + 31) / 32)), dim3(256), 0, st>>>(sums, chunks, N, db);

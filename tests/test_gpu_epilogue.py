@@ -133,7 +133,7 @@ def test_split_256_column_input_gradient():
 
 
 @pytest.mark.parametrize("act", ACTS)
-@pytest.mark.parametrize("M,N", [(1, 8), (3, 520), (48, 264), (49, 264), (64, 512), (777, 264), (4099, 1032)])
+@pytest.mark.parametrize("M,N", [(1, 8), (3, 520), (48, 264), (49, 264), (64, 512), (777, 264), (801, 1032), (260, 8200), (4099, 1032)])
 def test_activation_backward(M, N, act):
     dY, z, mul = normal((M, N), M), normal((M, N), M + 1, 2.0), normal((M, N), M + 2)
     for with_mul in (False, True):
