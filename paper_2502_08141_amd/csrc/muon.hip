@@ -17,6 +17,7 @@
 // Layouts of v_mfma_f64_16x16x4: A[i][k] and B[k][i] in lane i + 16 k; D[row][column] in lane column + 16 q, register v, with row = q + 4 v.
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "gemm_common.h"
 #include "muon.h"
@@ -73,6 +74,13 @@ __device__ __forceinline__ void store4_bf16(buffer_t r, bool ok, uint32_t e, int
 }
 __device__ __forceinline__ float at4(const float4& v, int e) { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; }
 
+// calls f with the number of tiles that R ranks reach: NT, or three of four.  (One 7B layer at rank 48 88 us with four, 69 so.)
+template <int NT, class F>
+__device__ __forceinline__ void with_tiles(int R, F&& f) {
+    if (NT == 4 && R <= 48) f(std::integral_constant<int, NT == 4 ? 3 : NT>{});
+    else f(std::integral_constant<int, NT>{});
+}
+
 struct Momentum { float beta; int nesterov; };
 // m' and u of one element
 __device__ __forceinline__ float momentum_of(const Momentum& mo, float g, float m) { return __builtin_fmaf(mo.beta, m, g); }
@@ -89,7 +97,8 @@ __device__ __forceinline__ float update_of(const Momentum& mo, float g, float m1
 constexpr int mu_step(int NT) { return 64 / NT; }
 constexpr int mu_stage(int NT) { return 16 * NT * (mu_step(NT) + 4); }     // floats: more than the 1024 of the other form
 template <int NT> struct GramSums { f64x4_t acc[mu_tiles(NT)]; };
-template <int NT, bool WIDE, bool VEC>
+// N: tiles that R reaches (of 64 ranks' four, three up to 48); the others' sums stay zero.
+template <int NT, int N, bool WIDE, bool VEC>
 __device__ __forceinline__ void muon_gram(const MuonItem& it, int first, int last, const Momentum& mo, float* mine, GramSums<NT>& sums) {
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -144,16 +153,16 @@ __device__ __forceinline__ void muon_gram(const MuonItem& it, int first, int las
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int e = 0; e < STEP / 4; ++e) {
-            double a[NT];
+            double a[N];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int t = 0; t < N; ++t) {
                 if (WIDE) a[t] = (double)mine[(16 * t + i) * LDW + 4 * e + q];
                 else a[t] = 16 * t + i < R ? (double)mine[(4 * e + q) * R + 16 * t + i] : 0.0;
             }
 #pragma unroll
-            for (int t1 = 0; t1 < NT; ++t1)
+            for (int t1 = 0; t1 < N; ++t1)
 #pragma unroll
-                for (int t2 = t1; t2 < NT; ++t2) sums.acc[mu_tile(NT, t1, t2)] = mfma64(a[t1], a[t2], sums.acc[mu_tile(NT, t1, t2)]);
+                for (int t2 = t1; t2 < N; ++t2) sums.acc[mu_tile(NT, t1, t2)] = mfma64(a[t1], a[t2], sums.acc[mu_tile(NT, t1, t2)]);
         }
         cur = nxt;
         c = cn;
@@ -172,13 +181,16 @@ __global__ __launch_bounds__(MU_THREADS, NT == 4 ? 2 : 4) void muon_gram_kernel(
 #pragma unroll
     for (int t = 0; t < TILES; ++t) s.acc[t] = f64x4_t{0.0, 0.0, 0.0, 0.0};
     const bool vec = ((it.wide ? it.L : it.R * it.L) & 3) == 0;
-    if (it.wide) {
-        if (vec) muon_gram<NT, true, true>(it, first, last, mo, sh.u[wave], s);
-        else muon_gram<NT, true, false>(it, first, last, mo, sh.u[wave], s);
-    } else {
-        if (vec) muon_gram<NT, false, true>(it, first, last, mo, sh.u[wave], s);
-        else muon_gram<NT, false, false>(it, first, last, mo, sh.u[wave], s);
-    }
+    with_tiles<NT>(it.R, [&](auto N_) __attribute__((always_inline)) {
+        constexpr int N = decltype(N_)::value;
+        if (it.wide) {
+            if (vec) muon_gram<NT, N, true, true>(it, first, last, mo, sh.u[wave], s);
+            else muon_gram<NT, N, true, false>(it, first, last, mo, sh.u[wave], s);
+        } else {
+            if (vec) muon_gram<NT, N, false, true>(it, first, last, mo, sh.u[wave], s);
+            else muon_gram<NT, N, false, false>(it, first, last, mo, sh.u[wave], s);
+        }
+    });
     __syncthreads();
     // the wavefronts' sums, in order
     if (wave > 0) {
@@ -251,25 +263,14 @@ __global__ __launch_bounds__(NT == 4 ? 1024 : NT == 2 ? 512 : 256) void muon_ite
     for (int r = 0; r < RP; ++r) trace += G[r * LD + r];
     const double norm = 1.0 / (sqrt(trace) + eps);
     __syncthreads();
+    if (NT == 4)                                                    // (tiles that the ranks do not reach are not computed)
+        for (int o = threadIdx.x; o < RP * LD; o += WAVES * 64) P[o] = 0.0;
     for (int o = threadIdx.x; o < RP * RP; o += WAVES * 64) G[(o / RP) * LD + o % RP] *= norm * norm;
     __syncthreads();
 
-    // tile (t1, t2) of the product of two symmetric matrices that commute
-    auto product = [&](const double* X, const double* Y, int t1, int t2) __attribute__((always_inline)) {
-        f64x4_t c = {0.0, 0.0, 0.0, 0.0};
-        const double *x = X + (16 * t1 + i) * LD + q, *y = Y + (16 * t2 + i) * LD + q;
-#pragma unroll
-        for (int k = 0; k < RP; k += 4) c = mfma64(x[k], y[k], c);
-        return c;
-    };
-    auto tiles = [&](int job, int& t1, int& t2) __attribute__((always_inline)) {
-        t1 = 0;
-        while (job >= NT - t1) { job -= NT - t1; ++t1; }
-        t2 = t1 + job;
-    };
     // One tile: a wavefront keeps the matrices in registers.  Register v of a result is row q + 4 v (or column, which is the same) at i, and
     // that is an operand for the four products k = q + 4 v: the sum over k may go in any order.  (A step 1.06 us in LDS, 0.57 so.)
-    if (NT == 1 && wave == 0) {
+    if constexpr (NT == 1) if (wave == 0) {
         f64x4_t g, p;
 #pragma unroll
         for (int v = 0; v < 4; ++v) g[v] = G[(q + 4 * v) * LD + i];
@@ -289,53 +290,69 @@ __global__ __launch_bounds__(NT == 4 ? 1024 : NT == 2 ? 512 : 256) void muon_ite
 #pragma unroll
         for (int v = 0; v < 4; ++v) P[(q + 4 * v) * LD + i] = p[v];
     }
-    if (NT == 1) __syncthreads();
-    for (int s = 0; s < (NT == 1 ? 0 : steps); ++s) {
-        const bool more = s + 1 < steps;
-        for (int job = wave; job < TILES; job += WAVES) {            // Q = a + b G + c G^2; P = Q in the first step
-            int t1, t2;
-            tiles(job, t1, t2);
-            const f64x4_t g2 = product(G, G, t1, t2);
+    if constexpr (NT == 1) __syncthreads();
+    if constexpr (NT > 1) with_tiles<NT>(it.R, [&](auto N_) __attribute__((always_inline)) {
+        constexpr int N = decltype(N_)::value, JOBS = mu_tiles(N);
+        // tile (t1, t2) of the product of two symmetric matrices that commute
+        auto product = [&](const double* X, const double* Y, int t1, int t2) __attribute__((always_inline)) {
+            f64x4_t c = {0.0, 0.0, 0.0, 0.0};
+            const double *x = X + (16 * t1 + i) * LD + q, *y = Y + (16 * t2 + i) * LD + q;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int r = 16 * t1 + q + 4 * v, c = 16 * t2 + i;
-                const double x = cc * g2[v] + cb * G[r * LD + c] + (r == c ? ca : 0.0);
-                place(Q, t1, t2, v * 64 + lane, x);
-                if (s == 0) place(P, t1, t2, v * 64 + lane, x);
-            }
-        }
-        __syncthreads();
-        f64x4_t pn = {0.0, 0.0, 0.0, 0.0};                            // a tile of the new P: kept until everyone has read the old one
-        int p1 = -1, p2 = 0;
-        for (int job = wave; job < 2 * TILES; job += WAVES) {        // T = G Q, and P Q (at most one tile of it for a wavefront)
-            int t1, t2;
-            if (job < TILES) {
-                if (!more) continue;
-                tiles(job, t1, t2);
-                const f64x4_t x = product(G, Q, t1, t2);
-#pragma unroll
-                for (int v = 0; v < 4; ++v) place(T, t1, t2, v * 64 + lane, x[v]);
-            } else if (s > 0) {
-                tiles(job - TILES, p1, p2);
-                pn = product(P, Q, p1, p2);
-            }
-        }
-        __syncthreads();
-        if (p1 >= 0) {
-#pragma unroll
-            for (int v = 0; v < 4; ++v) place(P, p1, p2, v * 64 + lane, pn[v]);
-        }
-        if (more) {
-            for (int job = wave; job < TILES; job += WAVES) {        // G = T Q
+            for (int k = 0; k < 16 * N; k += 4) c = mfma64(x[k], y[k], c);
+            return c;
+        };
+        auto tiles = [&](int job, int& t1, int& t2) __attribute__((always_inline)) {
+            t1 = 0;
+            while (job >= N - t1) { job -= N - t1; ++t1; }
+            t2 = t1 + job;
+        };
+        for (int s = 0; s < steps; ++s) {
+            const bool more = s + 1 < steps;
+            for (int job = wave; job < JOBS; job += WAVES) {            // Q = a + b G + c G^2; P = Q in the first step
                 int t1, t2;
                 tiles(job, t1, t2);
-                const f64x4_t x = product(T, Q, t1, t2);
+                const f64x4_t g2 = product(G, G, t1, t2);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) place(G, t1, t2, v * 64 + lane, x[v]);
+                for (int v = 0; v < 4; ++v) {
+                    const int r = 16 * t1 + q + 4 * v, c = 16 * t2 + i;
+                    const double x = cc * g2[v] + cb * G[r * LD + c] + (r == c ? ca : 0.0);
+                    place(Q, t1, t2, v * 64 + lane, x);
+                    if (s == 0) place(P, t1, t2, v * 64 + lane, x);
+                }
             }
+            __syncthreads();
+            f64x4_t pn = {0.0, 0.0, 0.0, 0.0};                            // a tile of the new P: kept until everyone has read the old one
+            int p1 = -1, p2 = 0;
+            for (int job = wave; job < 2 * JOBS; job += WAVES) {        // T = G Q, and P Q (at most one tile of it for a wavefront)
+                int t1, t2;
+                if (job < JOBS) {
+                    if (!more) continue;
+                    tiles(job, t1, t2);
+                    const f64x4_t x = product(G, Q, t1, t2);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) place(T, t1, t2, v * 64 + lane, x[v]);
+                } else if (s > 0) {
+                    tiles(job - JOBS, p1, p2);
+                    pn = product(P, Q, p1, p2);
+                }
+            }
+            __syncthreads();
+            if (p1 >= 0) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) place(P, p1, p2, v * 64 + lane, pn[v]);
+            }
+            if (more) {
+                for (int job = wave; job < JOBS; job += WAVES) {        // G = T Q
+                    int t1, t2;
+                    tiles(job, t1, t2);
+                    const f64x4_t x = product(T, Q, t1, t2);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) place(G, t1, t2, v * 64 + lane, x[v]);
+                }
+            }
+            __syncthreads();
         }
-        __syncthreads();
-    }
+    });
     double* dst = poly + (size_t)blockIdx.x * (RP * RP);
     auto element = [&](int p) { return it.wide ? p : (p & ~15) | (4 * (p & 3) + ((p >> 2) & 3)); };
     for (int o = threadIdx.x; o < RP * RP; o += WAVES * 64) {
@@ -355,7 +372,7 @@ __global__ __launch_bounds__(NT == 4 ? 1024 : NT == 2 ? 512 : 256) void muon_ite
 // 100.8 -> 97.7 us; where all ranks are rows 91 -> 87, all columns, whose halves touch 64 bytes of a row at a time, 94.4 -> 95.5).
 constexpr int mu_parts(int NT) { return NT == 4 ? 2 : 1; }
 struct MuonScalars { float lr, decay; };
-template <int NT, bool WIDE, bool VEC>
+template <int NT, int N, bool WIDE, bool VEC>
 __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int last, const Momentum& mo, const double* P, const MuonScalars& sc) {
     const int lane = threadIdx.x & 63, x = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -375,7 +392,7 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int la
             e = WIDE ? (uint32_t)s * (uint32_t)L + (uint32_t)l : (uint32_t)l * (uint32_t)R + (uint32_t)s;
             return WIDE ? last - l : R - s;
         };
-        float4 u[NT][4];
+        float4 u[N][4];
         auto load = [&](buffer_t r, int t, int j) __attribute__((always_inline)) {
             uint32_t e;
             bool ok;
@@ -383,12 +400,12 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int la
             return load4<VEC>(r, ok, e, n);
         };
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < N; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) u[t][j] = load(momentum, t, j);
         if (mo.nesterov) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < N; ++t)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float4 g = load(grad, t, j), m1 = u[t][j];
@@ -396,7 +413,7 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int la
                 }
         }
 #pragma unroll 1
-        for (int to = part * (NT / PARTS); to < (part + 1) * (NT / PARTS); ++to) {      // (one body: u in 64 bits takes half of the registers as it is)
+        for (int to = part * (NT / PARTS); to < min((part + 1) * (NT / PARTS), N); ++to) {      // (one body: u in 64 bits takes half of the registers as it is)
             float4 w[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = load(weight, to, j);
@@ -404,7 +421,7 @@ __device__ __forceinline__ void muon_apply(const MuonItem& it, int first, int la
 #pragma unroll
             for (int o = 0; o < 4; ++o) acc[o] = f64x4_t{0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < N; ++t)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const double p = P[((to * NT + t) * 4 + k) * 64 + lane];
@@ -440,13 +457,16 @@ __global__ __launch_bounds__(MU_THREADS, NT == 1 ? 4 : NT == 2 ? 3 : 2) void muo
     for (int o = 0; o < NT * NT; ++o) P[o * 256 + threadIdx.x] = poly[((size_t)item * (NT * NT) + o) * 256 + threadIdx.x];
     __syncthreads();
     const bool vec = ((it.wide ? it.L : it.R) & 3) == 0;
-    if (it.wide) {
-        if (vec) muon_apply<NT, true, true>(it, first, last, mo, P, sc);
-        else muon_apply<NT, true, false>(it, first, last, mo, P, sc);
-    } else {
-        if (vec) muon_apply<NT, false, true>(it, first, last, mo, P, sc);
-        else muon_apply<NT, false, false>(it, first, last, mo, P, sc);
-    }
+    with_tiles<NT>(it.R, [&](auto N_) __attribute__((always_inline)) {
+        constexpr int N = decltype(N_)::value;
+        if (it.wide) {
+            if (vec) muon_apply<NT, N, true, true>(it, first, last, mo, P, sc);
+            else muon_apply<NT, N, true, false>(it, first, last, mo, P, sc);
+        } else {
+            if (vec) muon_apply<NT, N, false, true>(it, first, last, mo, P, sc);
+            else muon_apply<NT, N, false, false>(it, first, last, mo, P, sc);
+        }
+    });
 }
 
 int mu_class(int R) { return R <= 16 ? 0 : R <= 32 ? 1 : 2; }
