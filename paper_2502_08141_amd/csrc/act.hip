@@ -3,8 +3,8 @@
 //
 // Memory bound: every operand is read or written once, 16 bytes per lane.  A thread keeps eight columns and walks down the
 // tokens, so that their sums stay in registers; the wavefronts of a workgroup meet in LDS, workgroups in the workspace, both
-// added in a fixed order.  Bias gradient alone of 4096 x 11008 (a read of 90 MB): 17.2 us, 5.2 TB/s, and 2.3 to add up the
-// chunks; gelu of 777 x 4096 (19 MB): 7.4 us and 2.3, between launch latency and bandwidth.
+// added in a fixed order.  Bias gradient alone of 4096 x 11008 (a read of 90 MB): 18.2 us, 4.9 TB/s; gelu of
+// 4096 x 4096 (101 MB) 22.7 us, 4.4 TB/s; of 777 x 4096 (19 MB) 9.7 us, latency and the activations on half of the units.
 #include <algorithm>
 
 #include "epilogue.h"
@@ -19,11 +19,14 @@ namespace {
 // threads) leave all tokens to one workgroup and need no second launch, but few units work.  Both ways, with bias gradient:
 //   gelu, 4096 columns, 24, 400, 777, 1000 tokens     9.5, 9.6, 10.2, 10.7 us in chunks; 8 lanes 6.3, 7.2, 12.2, 14.8; 4 lanes 6.3, 6.7, 9.9, 11.5
 //   gelu, 11008 columns, 160, 400, 777, 1200 tokens   9.7, 12.0, 15.0, 19.2 in chunks; 8 lanes 6.4, 9.8, 14.4, 19.1; 4 lanes 7.9, 13.2, 19.7, 27.6
-//   the sums alone, 4096 tokens of 1024, 2816, 4096 columns   8.6, 10.8, 11.8 in chunks; 8 lanes 9.7, 11.3, 11.7; 1200 tokens 8.6 and 5.5
+//   the sums alone, 1200 tokens of 1024, 4096, 11008 columns  7.3, 7.2, 10.5 in chunks; 8 lanes 5.2, 5.5, 7.8; of 20000 13.3 and 15.3
+//     (more strips than units); 3000 tokens 7.4, 10.2, 15.7; 7.7, 9.3, 14.0; 6000 tokens 8.8, 13.8, 29.7; 15.3, 15.8, 27.6
 constexpr int act_threads(int LANES) { return LANES == 64 ? 256 : 1024; }
 int act_lanes(int M, int N, bool sums_alone) {
-    if (M > (sums_alone ? 2400 : 800) || N > 1 << 22) return 64;      // (a launch has less than 2^32 threads)
-    return !sums_alone && N <= 32 * device_compute_units() ? 4 : 8;
+    const int units = device_compute_units();
+    const int most = N > 64 * units ? 400 : sums_alone ? 2048 + N / 4 : 800;
+    if (M > most || N > 1 << 22) return 64;                         // (a launch has less than 2^32 threads)
+    return !sums_alone && N <= 32 * units ? 4 : 8;
 }
 
 // Token rows per workgroup: enough workgroups to fill the chip several times, about sixteen rows each (777 x 4096, gelu: 9.5 us; eight
