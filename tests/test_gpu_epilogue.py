@@ -316,6 +316,32 @@ def test_more_columns_than_a_tile_addresses():
         assert e.value.status == lowra.UNSUPPORTED
 
 
+def test_outputs_past_four_gigabytes():
+    """The rows of a small call over and over: 138240 x 16384 values are 4.5 GB.  Every product is exact, so that the small call's bits
+    come out again whichever tiles the rows fall into."""
+    copies = 540
+    wide, tall = ExactLayer(16384, 64, 256, 8, seed=13), ExactLayer(64, 16384, 256, 8, seed=14)
+    big = lambda t: t.repeat(copies, 1)
+    same = lambda t, small: bool((t.view(copies, *small.shape) == small).all())
+    mul, z = normal((256, 16384), 1), normal((256, 16384), 2)
+    mul_big, z_big = big(mul), big(z)
+
+    few = fwd(wide, "silu", mul=mul, residual=z, keep_z=True)
+    many = lowra.lowra_linear_fwd_act(*wide.state(), big(wide.x), wide.A, wide.B, S, lowra.ACT_SILU, mul=mul_big, residual=z_big, keep_z=True)
+    assert all(same(m, f) for m, f in zip(many, few))
+    del many
+    few = bwd(tall, "gelu", z=z, mul=mul)
+    many = lowra.lowra_linear_bwd_input_act(*tall.state(), big(tall.dY), tall.A, tall.B, S, lowra.ACT_GELU, z=z_big, mul=mul_big)
+    assert all(same(m, f) for m, f in zip(many, few))
+    del many
+    few = lowra.lowra_act_bwd(mul, lowra.ACT_GELU_TANH, z=z, bias_grad=True)
+    many = lowra.lowra_act_bwd(mul_big, lowra.ACT_GELU_TANH, z=z_big, bias_grad=True)
+    assert same(many[0], few[0])
+    # sums of the same fp32 terms: at most 138240 / (8 x 256 / 32) + 64 + 2048 / 32 additions in a row, 2^-24 each; |dZ| is at most its bf16 rounding up
+    size = few[0].double().abs().sum(0) * 1.01
+    assert ((many[2].double() / copies - few[2].double()).abs() <= 2400 * 2.0 ** -24 * size).all()
+
+
 def test_graph_replays():
     L = ExactLayer(520, 1024, 64, 16, seed=11)
     few = ExactLayer(520, 1024, 4, 16, seed=12)

@@ -170,6 +170,31 @@ def test_a_wide_matrix_is_a_tall_one_transposed():
     assert float((ups[0] - ups[1].T).norm() / ups[0].norm()) <= 485 * 2.0 ** -23
 
 
+@pytest.mark.parametrize("rows,cols", [(17, (1 << 24) + 3), ((1 << 24) + 3, 17), (64, (1 << 23) - 1), ((1 << 23) - 4, 64)])
+def test_byte_offsets_up_to_two_gigabytes(rows, cols):
+    """Against the 64-bit products on the device, in pieces: one library product of 64 x 8388607 left the last columns of its last row
+    unwritten (they came out as a X1 + a X0, what the memory held before).  The tolerance is that of off_by's comment."""
+    gen = torch.Generator(device="cuda").manual_seed(rows % 1000)
+    g, m = (torch.randn(rows, cols, generator=gen, device="cuda") for _ in range(2))
+    out, update = torch.full_like(m, 3.0), torch.full_like(m, 3.0)
+    batch = lowra.MuonBatch([lowra.MuonItem(g, m, update=update, momentum_out=out)])
+    batch.run(lr=0.0, momentum=0.5, nesterov=False, steps=2)
+    assert torch.equal(out, torch.add(g, m, alpha=0.5))              # 0.5 m is exact, so one rounding either way
+    a, b, c = (f32(v) for v in ABC)
+    X = (out.T if rows > cols else out).double()
+    X /= X.square().sum().sqrt() + f32(1e-7)
+    for _ in range(2):
+        G = sum(p @ p.T.contiguous() for p in X.split(1 << 20, 1))
+        P = a * torch.eye(len(G), dtype=G.dtype, device="cuda") + b * G + c * G @ G
+        X = torch.cat([P @ p.contiguous() for p in X.split(1 << 20, 1)], 1)
+    X = X.T if rows > cols else X
+    assert float(torch.linalg.vector_norm(X - update) / torch.linalg.vector_norm(X)) <= 485 * 2.0 ** -23
+    for part in (slice(0, 4), slice(-4, None)):                      # the ends by themselves
+        want, got = (X[part], update[part]) if rows > cols else (X[:, part], update[:, part])
+        assert float((want - got).abs().max()) <= 485 * 2.0 ** -23 * float(X.abs().max())
+    batch.close()
+
+
 def test_streams_and_graphs():
     shapes = [(16, 512), (512, 16), (64, 300)]
     t = lambda s, i: torch.randn(s, generator=torch.Generator().manual_seed(i)).cuda()
