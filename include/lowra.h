@@ -283,7 +283,7 @@ lowra_status lowra_adapter_grads(const lowra_layout* layout, const uint16_t* x, 
 /* The same gradients from the rank-r intermediates the two linear calls of the step have already formed (Sec. 2.1: the
  * forward needs s x A^T, the input gradient s dY B), so that this call reads x and dY once and A, B not at all.
  * `lowra_linear_side_product` returns where a finished lowra_linear_fwd (op LOWRA_OP_LINEAR_FWD: s x A^T) or
- * lowra_linear_bwd_input (LOWRA_OP_LINEAR_BWD_INPUT: s dY B) call with the same M and r left its intermediate inside the
+ * lowra_linear_bwd_input (LOWRA_OP_LINEAR_BWD_INPUT: s dY B) call, or its form with an epilogue, with the same M and r left its intermediate inside the
  * workspace that was passed to it: bf16 [M][64] dev, row-major, valid until that workspace is written again; NULL when
  * the call keeps none in that form (r == 0, r > 64, or M <= 16 unless LOWRA_PATH_GEMM is set: the small-token kernels).
  * A host-side computation: nothing is launched.

@@ -316,6 +316,20 @@ def test_more_columns_than_a_tile_addresses():
         assert e.value.status == lowra.UNSUPPORTED
 
 
+@pytest.mark.parametrize("M", [4, 17, 40, 300])
+def test_rank_r_products_are_left_for_the_adapter_gradients(M):
+    L = ExactLayer(264, 576, M, 8, seed=15)
+    z = normal((M, 576), 1)
+    wf, wb = L.workspace(lowra.OP_LINEAR_FWD), L.workspace(lowra.OP_LINEAR_BWD_INPUT)
+    fwd(L, "gelu", mul=normal((M, 264), 2), keep_z=True, workspace=wf)
+    bwd(L, "gelu", z=z, residual=z, workspace=wb)
+    st, su = (lowra.lowra_linear_side_product(L.layout, op, M, 8, w) for op, w in ((lowra.OP_LINEAR_FWD, wf), (lowra.OP_LINEAR_BWD_INPUT, wb)))
+    assert (st is None) == (M <= 16) and (su is None) == (M <= 16)
+    if M > 16:
+        want = lowra.lowra_adapter_grads(L.layout, L.x, L.dY, L.A, L.B, S)
+        assert all(torch.equal(a, b) for a, b in zip(lowra.lowra_adapter_grads_from_side(L.layout, L.x, L.dY, 8, st, su), want))
+
+
 def test_outputs_past_four_gigabytes():
     """The rows of a small call over and over: 138240 x 16384 values are 4.5 GB.  Every product is exact, so that the small call's bits
     come out again whichever tiles the rows fall into."""
