@@ -118,6 +118,13 @@ static MidPlan mid_plan_call(const lowra_layout& L, const LinearArgs& a, int op,
         const MidPlan whole = mid_plan_of(L, op, a.M, a.r, gemm, ~(size_t)0);
         if (whole.splits <= 1 || mid_pieces(whole, room) > 0) return whole;
     }
+    // Few tokens with an epilogue: the mid-token kernel only with room for all the splits that it would have.  Without any, against the
+    // streaming kernel in the same workspace, rank 16, 1, 4 and 16 tokens: 4096 x 4096 70, 70, 70 us against 24, 29, 38; 11008 x 4096
+    // 173, 173, 174 against 32, 37, 46; 4096 x 11008 71, 71, 71 against 28, 36, 51; 1032 x 2048 23, 23, 23 against 20, 22, 24.
+    if (few) {
+        const MidPlan whole = mid_plan_of(L, op, a.M, a.r, gemm, ~(size_t)0, true);
+        few = whole.splits <= 1 || mid_part_bytes(whole) <= room;
+    }
     return mid_plan_of(L, op, a.M, a.r, gemm, room, few);
 }
 size_t linear_workspace_min(const lowra_layout& L, int op, int M, int r) {
