@@ -23,18 +23,21 @@ enum : int { kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSil
 constexpr float kLog2e = 1.44269504f;
 
 // The normal distribution function at -|z|, as 2 to the power of a polynomial in |z| (our own minimax fit of log2 Phi(-a) on
-// [0, 7]): within 4e-6 of it relatively up to |z| = 4, 7e-5 up to 7; beyond, the negative leading coefficient takes it to zero.
-// In this form the small tail keeps its relative accuracy, which 1 + erf loses, and one exp2 is the only slow instruction.
+// [0, 13]): within 7e-6 of it relatively up to |z| = 4, 4.1e-5 up to 7, 1.5e-4 up to 13, an eighteenth of half a bf16 step and less.  From
+// 12.95 on Phi(-a) is below 2^-126 and comes out as zero (the polynomial goes on falling).  In this form the small tail keeps its relative
+// accuracy, which 1 + erf loses, and one exp2 is the only slow instruction.
 __device__ __forceinline__ float normal_tail(float z) {
     const float a = __builtin_fabsf(z);
-    float q = -0x1.df6e4cp-20f;
-    q = __builtin_fmaf(q, a, 0x1.fd25bcp-15f);
-    q = __builtin_fmaf(q, a, -0x1.e477p-11f);
-    q = __builtin_fmaf(q, a, 0x1.16095ep-7f);
-    q = __builtin_fmaf(q, a, -0x1.b9b316p-5f);
-    q = __builtin_fmaf(q, a, -0x1.d58178p-2f);
-    q = __builtin_fmaf(q, a, -0x1.26b778p+0f);
-    q = __builtin_fmaf(q, a, -0x1.ffff92p-1f);
+    float q = -0x1.18b724p-29f;
+    q = __builtin_fmaf(q, a, 0x1.414014p-23f);
+    q = __builtin_fmaf(q, a, -0x1.40dfccp-18f);
+    q = __builtin_fmaf(q, a, 0x1.72c934p-14f);
+    q = __builtin_fmaf(q, a, -0x1.1631cap-10f);
+    q = __builtin_fmaf(q, a, 0x1.2265bp-7f);
+    q = __builtin_fmaf(q, a, -0x1.be47eap-5f);
+    q = __builtin_fmaf(q, a, -0x1.d517e2p-2f);
+    q = __builtin_fmaf(q, a, -0x1.26beaep+0f);
+    q = __builtin_fmaf(q, a, -0x1.fffedcp-1f);
     return __builtin_amdgcn_exp2f(q);
 }
 

@@ -1,10 +1,13 @@
-"""What include/lowra.h promises of the calls with an epilogue beyond their formulas: workspaces, tensors that share memory."""
+"""What include/lowra.h promises of the calls with an epilogue beyond their formulas: small results, workspaces, tensors that share
+memory."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2502_08141_amd import lowra
-from tests.epilogue_util import S
+from tests.epilogue_util import S, act64
 
 pytestmark = pytest.mark.gpu
 
@@ -73,3 +76,75 @@ def test_few_tokens_back_without_room_for_splits_stream(N, K, r, M):
     # scaled gradient and the level instead of the weight: five and four roundings
     wide = call(whole).double()
     assert float((got.double() - wide).norm() / wide.norm()) <= 9 * 2.0 ** -8
+
+
+# Where act(z) is small its relative accuracy counts: one rounding to bf16 (2^-8) and 2^-12 for the arithmetic in front of it, on the two
+# terms of a slope each.  gelu: Phi within 1.5e-4 (2^-12.7), the density's exponent z^2 log2(e) / 2 <= 118 rounded twice (118 x 2^-23 ln 2,
+# 2^-16.6); tanh form and silu: an exponent of at most 126 / log2(e) = 87 after five roundings (87 x 5 x 2^-24, 2^-15.2).
+# The smallest z: Phi, the density and the logistic function stay above 2^-126 there.
+TAILS = {"gelu": 12.75, "gelu_tanh": 9.875, "silu": 86.5}
+
+
+def tail_values(act):
+    """The bf16 numbers from -TAILS[act] up to -0.05, a multiple of eight of them."""
+    z = torch.arange(0x3d50, 0x4300, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    z = -z[z.double() <= TAILS[act]]
+    return z[z.numel() % 8:]
+
+
+def slope_terms64(z, act):
+    """act'(z) = the sum of these two."""
+    z = z.double()
+    if act == "gelu":
+        return 0.5 * torch.erfc(-z * math.sqrt(0.5)), z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    w, dw = (z, torch.ones_like(z)) if act == "silu" else \
+        (2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3), 2 * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * z * z))
+    s = 1 / (1 + torch.exp(-w))
+    return s, z * dw * s / (1 + torch.exp(w))
+
+
+def gelu64(z, act):
+    return z.double() * slope_terms64(z, act)[0]          # (1 + erf and 1 + tanh lose the tail in 64 bits too)
+
+
+@pytest.mark.parametrize("act", list(TAILS))
+def test_small_activations_are_relatively_exact(act):
+    z = tail_values(act)
+    ref, (s, d) = gelu64(z, act), slope_terms64(z, act)
+    assert z.double().min() <= -0.98 * TAILS[act] and torch.allclose(ref, act64(z, act), rtol=0, atol=1e-13)
+    ones = torch.ones(1, z.numel(), dtype=torch.bfloat16, device="cuda")
+    dZ, dmul, _ = (t if t is None else t[0].double().cpu() for t in lowra.lowra_act_bwd(ones, lowra.ACTS[act], z=z.cuda()[None], mul=ones))
+    bad = ~((dmul - ref).abs() <= ref.abs() * (2.0 ** -8 + 2.0 ** -12))
+    assert not bad.any(), list(zip(z[bad].tolist(), dmul[bad].tolist(), ref[bad].tolist()))[:8]
+    bad = ~((dZ - (s + d)).abs() <= (s + d).abs() * 2.0 ** -8 + (s + d.abs()) * 2.0 ** -12)
+    assert not bad.any(), list(zip(z[bad].tolist(), dZ[bad].tolist(), (s + d)[bad].tolist()))[:8]
+
+
+@pytest.mark.parametrize("path,M", [(0, 1), (0, 40), (lowra.PATH_GEMM, 40)])
+@pytest.mark.parametrize("act", list(TAILS))
+def test_small_activations_in_the_forwards_epilogue(act, path, M):
+    """No activations and a bias: v is the bias.  Each row has the tail once, from the few-token, the mid-token and the 256-column kernel."""
+    z = tail_values(act)
+    L = Layer(z.numel(), 128, M, 0, seed=22)
+    lowra.lowra_set_linear_path(path)
+    try:
+        y, kept = lowra.lowra_linear_fwd_act(*L.state(), torch.zeros_like(L.x), None, None, S, lowra.ACTS[act], bias=z.cuda(), keep_z=True)
+    finally:
+        lowra.lowra_set_linear_path(lowra.PATH_AUTO)
+    ref, y = gelu64(z, act), y.double().cpu()
+    assert torch.equal(kept.cpu(), z.expand(M, -1)) and torch.equal(y, y[:1].expand(M, -1))
+    assert ((y[0] - ref).abs() <= ref.abs() * (2.0 ** -8 + 2.0 ** -12)).all()
+
+
+@pytest.mark.parametrize("act", list(TAILS))
+def test_activations_past_the_smallest_normal_numbers(act):
+    """Results below 2^-119 (a factor below 2^-126, times |z| up to 100) may be zero; beyond, they are."""
+    z = torch.cat([torch.linspace(-1.2 * TAILS[act], -TAILS[act], 256), -torch.logspace(3, 38, 256)]).bfloat16()
+    ones = torch.ones(1, z.numel(), dtype=torch.bfloat16, device="cuda")
+    dZ, dmul, _ = (t if t is None else t[0].double().cpu() for t in lowra.lowra_act_bwd(ones, lowra.ACTS[act], z=z.cuda()[None], mul=ones))
+    ref, (s, d) = gelu64(z, act), slope_terms64(z, act)
+    d = torch.nan_to_num(d)                               # (a square or a cube past 2^1024)
+    small = 2.0 ** -112
+    assert ((dmul - torch.nan_to_num(ref)).abs() <= ref.abs() * (2.0 ** -8 + 2.0 ** -12) + small).all()
+    assert ((dZ - (s + d)).abs() <= (s + d).abs() * 2.0 ** -8 + (s + d.abs()) * 2.0 ** -12 + small).all()
+    assert (dmul[256:] == 0).all() and (dZ[256:] == 0).all()
