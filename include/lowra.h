@@ -199,8 +199,8 @@ enum { LOWRA_ACT_NONE = 0, LOWRA_ACT_RELU = 1, LOWRA_ACT_GELU = 2, LOWRA_ACT_GEL
  * mul a gated layer is two calls: u by lowra_linear_fwd, then act(gate) u by this one.  All operands bf16 dev, 16-byte aligned;
  * null: not there.  v and y are computed in fp32 from the fp32 sums and rounded once.
  *   residual may be y itself (the call adds to y); otherwise no operand overlaps y or z.
- * Arguments, workspace and errors otherwise as in lowra_linear_fwd; INVALID_ARG also for a null or unknown epilogue and when the
- * current device is not the layout's; UNSUPPORTED also from N = 2^22 on. */
+ * Arguments, workspace and errors otherwise as in lowra_linear_fwd; INVALID_ARG also for a null or unknown epilogue, for such an
+ * overlap and when the current device is not the layout's; UNSUPPORTED also from N = 2^22 on. */
 typedef struct lowra_fwd_epilogue {
     int act;                    /* LOWRA_ACT_* */
     const uint16_t* bias;       /* [N] */
@@ -239,7 +239,7 @@ lowra_status lowra_linear_bwd_input_act(const lowra_layout* layout, const uint8_
  *   (with LOWRA_ACT_NONE and no mul dZ is dY: pass null for the bias gradient alone); dZ may be dY itself; otherwise nothing overlaps an output.
  *   workspace: dev, >= lowra_act_bwd_workspace_bytes(M, N), 16-byte aligned; unused without db.
  * The sums are added in a fixed order.  M == 0 writes zeros to db.  INVALID_ARG: a negative size, an unknown activation, a missing
- * dY, z or mul, no output at all; UNSUPPORTED: N % 8 != 0, M or N above 2^30; MISALIGNED; WORKSPACE_TOO_SMALL. */
+ * dY, z or mul, no output at all, such an overlap; UNSUPPORTED: N % 8 != 0, M or N above 2^30; MISALIGNED; WORKSPACE_TOO_SMALL. */
 size_t lowra_act_bwd_workspace_bytes(int M, int N);
 lowra_status lowra_act_bwd(int M, int N, int act, const uint16_t* dY, const uint16_t* z, const uint16_t* mul, uint16_t* dZ,
                            uint16_t* dmul, float* db, void* workspace, size_t workspace_bytes, void* stream);

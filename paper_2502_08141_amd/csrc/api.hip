@@ -33,6 +33,25 @@ lowra_status plan_rows(int N, int K, int group, const uint8_t* bits, int64_t* of
     return LOWRA_OK;
 }
 
+// Whether an output of a call overlaps another one or an operand.  out[0] may be inputs[0] itself: every element of that operand is read
+// by the thread that writes the result in its place, before it does.
+struct Span { const void* p; size_t bytes; };
+bool overlap(const Span& a, const Span& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+template <size_t O, size_t I>
+bool outputs_overlap(const Span (&outputs)[O], const Span (&inputs)[I]) {
+    for (size_t o = 0; o < O; ++o) {
+        for (size_t other = 0; other < o; ++other)
+            if (overlap(outputs[o], outputs[other])) return true;
+        for (size_t i = 0; i < I; ++i)
+            if (overlap(outputs[o], inputs[i]) && !(o == 0 && i == 0 && outputs[o].p == inputs[i].p)) return true;
+    }
+    return false;
+}
+size_t scale_bytes(const lowra_layout* L) { return (size_t)L->N * L->G * (L->scale_bf16 ? 2 : 4); }
+
 }  // namespace
 
 // ---- scratch of lowra_linear_fwd_static: device memory that exists without any allocation call.
@@ -481,7 +500,11 @@ lowra_status lowra_linear_fwd_act(const lowra_layout* L, const uint8_t* packed, 
     if (st != LOWRA_OK || M == 0 || L->N == 0) return st;
     if (L->N > lowra::kEpiMaxColumns) return LOWRA_UNSUPPORTED;
     if (!aligned16(e->bias) || !aligned16(e->mul) || !aligned16(e->residual) || !aligned16(e->z)) return LOWRA_MISALIGNED;
-    if (e->z && (e->z == y || e->z == e->residual || e->z == e->mul)) return LOWRA_INVALID_ARG;
+    const size_t in = (size_t)M * L->K * 2, size = (size_t)M * L->N * 2;
+    if (outputs_overlap({Span{y, size}, Span{e->z, size}},
+                        {Span{e->residual, size}, Span{e->mul, size}, Span{e->bias, (size_t)L->N * 2}, Span{x, in}, Span{A, (size_t)r * L->K * 2}, Span{B, (size_t)L->N * r * 2},
+                         Span{packed, L->packed_bytes}, Span{absmax, scale_bytes(L)}, Span{mappings, (size_t)L->C * lowra::kTableStride * 4}}))
+        return LOWRA_INVALID_ARG;
     if (!on_current_device(L)) return LOWRA_INVALID_ARG;
     const lowra::FwdEpi epi{e->act, e->bias, e->mul, e->residual, e->z};
     lowra::LinearArgs a{packed, absmax, mappings, x, M, A, B, r, s, y, workspace, usable_bytes(workspace, workspace_bytes)};
@@ -500,7 +523,11 @@ lowra_status lowra_linear_bwd_input_act(const lowra_layout* L, const uint8_t* pa
     if (L->N == 0) return LOWRA_UNSUPPORTED;                      // (an empty contraction is not worth an epilogue of its own)
     if ((e->act != LOWRA_ACT_NONE || e->dmul) && !e->z) return LOWRA_INVALID_ARG;
     if (!aligned16(e->z) || !aligned16(e->mul) || !aligned16(e->residual) || !aligned16(e->dmul)) return LOWRA_MISALIGNED;
-    if (e->dmul && (e->dmul == dX || e->dmul == e->residual || e->dmul == e->z || e->dmul == e->mul)) return LOWRA_INVALID_ARG;
+    const size_t in = (size_t)M * L->N * 2, size = (size_t)M * L->K * 2;
+    if (outputs_overlap({Span{dX, size}, Span{e->dmul, size}},
+                        {Span{e->residual, size}, Span{e->z, size}, Span{e->mul, size}, Span{dY, in}, Span{A, (size_t)r * L->K * 2}, Span{B, (size_t)L->N * r * 2},
+                         Span{packed, L->packed_bytes}, Span{absmax, scale_bytes(L)}, Span{mappings, (size_t)L->C * lowra::kTableStride * 4}}))
+        return LOWRA_INVALID_ARG;
     if (!on_current_device(L)) return LOWRA_INVALID_ARG;
     const lowra::BwdEpi epi{e->act, e->z, e->mul, e->residual, e->dmul};
     lowra::LinearArgs a{packed, absmax, mappings, dY, M, A, B, r, s, dX, workspace, usable_bytes(workspace, workspace_bytes)};
@@ -522,13 +549,14 @@ lowra_status lowra_act_bwd(int M, int N, int act, const uint16_t* dY, const uint
     if (M == 0) return !db || lowra::launch_zero_bf16(reinterpret_cast<uint16_t*>(db), (size_t)N * 2, st) == hipSuccess ? LOWRA_OK : LOWRA_HIP_ERROR;
     if (!dY || ((act != LOWRA_ACT_NONE || dmul) && !z)) return LOWRA_INVALID_ARG;
     if (!aligned16(dY) || !aligned16(z) || !aligned16(mul) || !aligned16(dZ) || !aligned16(dmul)) return LOWRA_MISALIGNED;
-    if (dmul && (dmul == dY || dmul == dZ || dmul == z || dmul == mul)) return LOWRA_INVALID_ARG;
     const size_t need = db ? lowra::act_bwd_workspace_bytes(M, N) : 0;
     if (need > 0) {
         if (!workspace) return LOWRA_INVALID_ARG;
         if (!aligned16(workspace)) return LOWRA_MISALIGNED;
         if (workspace_bytes < need) return LOWRA_WORKSPACE_TOO_SMALL;
     }
+    const size_t size = (size_t)M * N * 2;
+    if (outputs_overlap({Span{dZ, size}, Span{dmul, size}, Span{db, (size_t)N * 4}}, {Span{dY, size}, Span{z, size}, Span{mul, size}})) return LOWRA_INVALID_ARG;
     const lowra::BwdEpi epi{act, z, mul, nullptr, dmul};
     return lowra::launch_act_bwd(M, N, epi, dY, dZ, db, workspace, st) == hipSuccess ? LOWRA_OK : LOWRA_HIP_ERROR;
 }

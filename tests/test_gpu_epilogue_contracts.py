@@ -148,3 +148,45 @@ def test_activations_past_the_smallest_normal_numbers(act):
     assert ((dmul - torch.nan_to_num(ref)).abs() <= ref.abs() * (2.0 ** -8 + 2.0 ** -12) + small).all()
     assert ((dZ - (s + d)).abs() <= (s + d).abs() * 2.0 ** -8 + (s + d.abs()) * 2.0 ** -12 + small).all()
     assert (dmul[256:] == 0).all() and (dZ[256:] == 0).all()
+
+
+def test_operands_that_overlap_an_output_are_refused():
+    L = Layer(64, 128, 40, 8, seed=23)
+    buf = torch.zeros(1 << 17, dtype=torch.bfloat16, device="cuda")
+    at = lambda off, shape: buf[off:off + shape[0] * shape[1]].view(shape)
+    f, b = (40, 64), (40, 128)
+
+    def refused(fn, act, **kw):
+        with pytest.raises(lowra.LowraError) as e:
+            fn(*L.state(), act, *L.adapters(), lowra.ACT_GELU, **kw)
+        assert e.value.status == lowra.INVALID_ARG, kw
+
+    for d in (-8, 0, 8, 40 * 64 - 8, -40 * 64 + 8):              # (16 bytes and more, and one chunk in common)
+        y = at(30000, f)
+        shifted = at(30000 + d, f)
+        refused(lowra.lowra_linear_fwd_act, L.x, y=y, mul=shifted)
+        refused(lowra.lowra_linear_fwd_act, L.x, y=y, z=shifted)
+        refused(lowra.lowra_linear_fwd_act, L.x, z=y, mul=shifted)
+        refused(lowra.lowra_linear_fwd_act, L.x, z=y, residual=shifted)
+        if d:
+            refused(lowra.lowra_linear_fwd_act, L.x, y=y, residual=shifted)
+    refused(lowra.lowra_linear_fwd_act, at(20000, b), y=at(20000 + 40 * 128 - 8, f))
+    refused(lowra.lowra_linear_fwd_act, L.x, y=at(20000, f), bias=buf[20000 + 40 * 64 - 8:][:64])
+    z = at(60000, b)
+    for d in (-8, 0, 8, 40 * 128 - 8, -40 * 128 + 8):
+        dX = at(30000, b)
+        shifted = at(30000 + d, b)
+        refused(lowra.lowra_linear_bwd_input_act, L.dY, z=shifted, dX=dX)
+        refused(lowra.lowra_linear_bwd_input_act, L.dY, z=z, mul=shifted, dX=dX)
+        refused(lowra.lowra_linear_bwd_input_act, L.dY, z=z, mul=L.x, dmul=shifted, dX=dX)
+        refused(lowra.lowra_linear_bwd_input_act, L.dY, z=shifted, mul=L.x, dmul=dX)
+        refused(lowra.lowra_linear_bwd_input_act, L.dY, z=z, mul=shifted, dmul=dX)
+        refused(lowra.lowra_linear_bwd_input_act, L.dY, z=z, mul=L.x, residual=shifted, dmul=dX)
+        if d:
+            refused(lowra.lowra_linear_bwd_input_act, L.dY, z=z, residual=shifted, dX=dX)
+    refused(lowra.lowra_linear_bwd_input_act, at(20000, f), z=z, dX=at(20000 + 40 * 64 - 8, b))
+    # neighbours, and the residual itself
+    y, kept = lowra.lowra_linear_fwd_act(*L.state(), L.x, *L.adapters(), lowra.ACT_GELU, y=at(30000, f), z=at(30000 + 40 * 64, f), residual=at(30000, f),
+                                         mul=at(30000 - 40 * 64, f), bias=buf[30000 + 2 * 40 * 64:][:64])
+    assert y.isfinite().all() and kept.isfinite().all()
+    torch.cuda.synchronize()
