@@ -186,7 +186,9 @@ PyObject* linear_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const long activation = PyLong_AsLong(a[9]);
         if (PyErr_Occurred() || activation != (int)activation) return none();
         const at::Tensor* ws = plain(a[14], at::kByte);
-        if (!ws || ws->device() != act->device() || packed->device() != act->device() || act->get_device() != c10::hip::current_device()) return none();
+        if (!ws || act->get_device() != c10::hip::current_device()) return none();
+        for (const at::Tensor* t : {ws, packed, absmax, mappings, A, B})
+            if (t && t->device() != act->device()) return none();
         void* const wp = ws->data_ptr();
         const size_t ws_bytes = (size_t)ws->numel();
         const float s = (float)PyFloat_AS_DOUBLE(a[8]);

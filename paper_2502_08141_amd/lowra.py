@@ -386,6 +386,12 @@ def lowra_linear_bwd_input(layout: Layout, packed, absmax, mappings, dY, A, B, s
                    absmax, mappings, dY, layout.N, layout.K, A, B, s, dX, workspace)
 
 
+def _here(device, *tensors):
+    """`device` is the current one, and the tensors are on it."""
+    if device.index != torch.cuda.current_device() or any(t.device != device for t in tensors):
+        raise ValueError("tensors on another device than the current one")
+
+
 def _operand(t, shape, name: str, device):
     """An optional bf16 operand of an epilogue."""
     if t is not None:
@@ -403,8 +409,7 @@ def _linear_act(fn, name, op, layout, packed, absmax, mappings, act_in, cols_in,
     _dev(act_in, torch.bfloat16, "activation")
     if act_in.dim() != 2 or act_in.shape[1] != cols_in:
         raise ValueError("activation shape mismatch")
-    if act_in.device.index != torch.cuda.current_device() or packed.device != act_in.device:
-        raise ValueError("tensors on another device than the current one")
+    _here(act_in.device, packed, absmax, mappings)
     M, r = int(act_in.shape[0]), 0
     if M > 0x7fffffff:
         raise ValueError("too many tokens")
@@ -413,6 +418,7 @@ def _linear_act(fn, name, op, layout, packed, absmax, mappings, act_in, cols_in,
         r = int(A.shape[0])
         if tuple(A.shape) != (r, layout.K) or tuple(B.shape) != (layout.N, r):
             raise ValueError("LoRA operand shape mismatch")
+        _here(act_in.device, A, B)
     else:
         A = B = None
     if out is None:
@@ -421,7 +427,7 @@ def _linear_act(fn, name, op, layout, packed, absmax, mappings, act_in, cols_in,
     record, second = epilogue(M)
     if workspace is None:
         workspace = torch.empty(layout.workspace_bytes(op, M, r), dtype=torch.uint8, device=act_in.device)
-    _dev(workspace, torch.uint8, "workspace")
+    _here(act_in.device, _dev(workspace, torch.uint8, "workspace"))
     _check(fn(layout.handle, _ptr(packed), _ptr(absmax), _ptr(mappings), _ptr(act_in), M, _ptr(A), _ptr(B), r, float(s), C.addressof(record),
               _ptr(out), _ptr(workspace), workspace.numel(), _stream()), name)
     return out, second
@@ -484,8 +490,7 @@ def lowra_act_bwd(dY, act: int, z=None, mul=None, bias_grad: bool = False, works
     _dev(dY, torch.bfloat16, "dY")
     if dY.dim() != 2:
         raise ValueError("dY: shape mismatch")
-    if dY.device.index != torch.cuda.current_device():
-        raise ValueError("tensors on another device than the current one")
+    _here(dY.device)
     shape, act = tuple(dY.shape), int(act)
     M, N = shape
     if max(shape) > 0x7fffffff:
@@ -496,7 +501,7 @@ def lowra_act_bwd(dY, act: int, z=None, mul=None, bias_grad: bool = False, works
     db = torch.empty(N, dtype=torch.float32, device=dY.device) if bias_grad else None
     if workspace is None:
         workspace = torch.empty(lowra_act_bwd_workspace_bytes(M, N) if bias_grad else 0, dtype=torch.uint8, device=dY.device)
-    _dev(workspace, torch.uint8, "workspace")
+    _here(dY.device, _dev(workspace, torch.uint8, "workspace"))
     _check(lib().lowra_act_bwd(M, N, act, _ptr(dY), _ptr(z), _ptr(mul), _ptr(dZ), _ptr(dmul), _ptr(db), _ptr(workspace), workspace.numel(), _stream()),
            "lowra_act_bwd")
     return dZ, dmul, db
@@ -746,12 +751,11 @@ class MuonBatch:
                 raise ValueError(f"item {i}: too large")
             arr[i] = MuonItemRecord(int(it.grad.shape[0]), int(it.grad.shape[1]), float(it.scale), *(_ptr(t) for _, t, _ in fields))
             self._keep += [t for _, t, _ in fields]
-        if device.index != torch.cuda.current_device():
-            raise ValueError("tensors on another device than the current one")
+        _here(device)
         need = int(lib().lowra_muon_batch_workspace_bytes(len(items), C.addressof(arr)))
         if workspace is None:
             workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
-        _dev(workspace, torch.uint8, "workspace")
+        _here(device, _dev(workspace, torch.uint8, "workspace"))
         self._keep.append(workspace)
         _check(lib().lowra_muon_batch_create(len(items), C.addressof(arr), _ptr(workspace), workspace.numel(), C.addressof(self.handle)),
                "lowra_muon_batch_create")
