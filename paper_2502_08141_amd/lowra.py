@@ -455,10 +455,11 @@ def lowra_linear_fwd_act(layout: Layout, packed, absmax, mappings, x, A, B, s, a
 
 
 def lowra_linear_bwd_input_act(layout: Layout, packed, absmax, mappings, dY, A, B, s, act: int, z=None, mul=None, residual=None, dX=None, dmul=None,
-                               workspace=None):
+                               workspace=None, mul_grad: bool = True):
     """g = dY What + s (dY B) A + residual -> (dX, dmul): dX [M,K] bf16 = g mul act'(z), and with `mul` dmul [M,K] bf16 = g act(z), else
-    None: the gradients of z and mul of the layer's input act(z) mul.  z, mul, residual: [M,K] bf16."""
-    if dX is None and dmul is None and workspace is not None and layout.__class__ is Layout:
+    None: the gradients of z and mul of the layer's input act(z) mul.  z, mul, residual: [M,K] bf16; without `mul_grad` (mul is frozen)
+    there is no dmul."""
+    if dX is None and dmul is None and mul_grad and workspace is not None and layout.__class__ is Layout:
         res = _call.linear_act(1, layout.native, packed, absmax, mappings, dY, A, B, s, act, z, mul, residual, False, workspace)
         if res is not None:
             return _native(res, "lowra_linear_bwd_input_act")
@@ -467,7 +468,7 @@ def lowra_linear_bwd_input_act(layout: Layout, packed, absmax, mappings, dY, A, 
         second, shape = dmul, (M, layout.K)
         for t, n in ((z, "z"), (mul, "mul"), (residual, "residual")):
             _operand(t, shape, n, dY.device)
-        if second is None and mul is not None:
+        if second is None and mul is not None and mul_grad:
             second = torch.empty(shape, dtype=torch.bfloat16, device=dY.device)
         _operand(second, shape, "dmul", dY.device)
         return BwdEpilogue(int(act), _ptr(z), _ptr(mul), _ptr(residual), _ptr(second)), second
@@ -480,10 +481,11 @@ def lowra_act_bwd_workspace_bytes(M: int, N: int) -> int:
     return int(lib().lowra_act_bwd_workspace_bytes(int(M), int(N)))
 
 
-def lowra_act_bwd(dY, act: int, z=None, mul=None, bias_grad: bool = False, workspace=None):
+def lowra_act_bwd(dY, act: int, z=None, mul=None, bias_grad: bool = False, workspace=None, dZ=None, dmul=None, db=None, mul_grad: bool = True):
     """dY [M,N] bf16, the gradient of act(z) mul -> (dZ, dmul, db): dZ bf16 = dY mul act'(z) (None where it would be dY), dmul bf16 =
-    dY act(z) (None without `mul`), db fp32 [N] = the sum of dZ over the tokens (None without `bias_grad`)."""
-    if workspace is not None and _lib is not None:
+    dY act(z) (None without `mul`, or without `mul_grad`: mul is frozen), db fp32 [N] = the sum of dZ over the tokens (None without
+    `bias_grad`).  What is given of dZ (dY itself, for one), dmul and db is written there."""
+    if dZ is None and dmul is None and db is None and mul_grad and workspace is not None and _lib is not None:
         res = _call.act_bwd(dY, act, z, mul, bias_grad, workspace)
         if res is not None:
             return _native(res, "lowra_act_bwd")
@@ -496,11 +498,19 @@ def lowra_act_bwd(dY, act: int, z=None, mul=None, bias_grad: bool = False, works
     if max(shape) > 0x7fffffff:
         raise ValueError("dY: too large")
     _operand(z, shape, "z", dY.device); _operand(mul, shape, "mul", dY.device)
-    dZ = torch.empty_like(dY) if act != ACT_NONE or mul is not None else None
-    dmul = torch.empty_like(dY) if mul is not None else None
-    db = torch.empty(N, dtype=torch.float32, device=dY.device) if bias_grad else None
+    if dZ is None and (act != ACT_NONE or mul is not None):
+        dZ = torch.empty_like(dY)
+    if dmul is None and mul is not None and mul_grad:
+        dmul = torch.empty_like(dY)
+    _operand(dZ, shape, "dZ", dY.device); _operand(dmul, shape, "dmul", dY.device)
+    if db is None and bias_grad:
+        db = torch.empty(N, dtype=torch.float32, device=dY.device)
+    if db is not None:
+        _here(dY.device, _dev(db, torch.float32, "db"))
+        if tuple(db.shape) != (N,):
+            raise ValueError("db: shape mismatch")
     if workspace is None:
-        workspace = torch.empty(lowra_act_bwd_workspace_bytes(M, N) if bias_grad else 0, dtype=torch.uint8, device=dY.device)
+        workspace = torch.empty(lowra_act_bwd_workspace_bytes(M, N) if db is not None else 0, dtype=torch.uint8, device=dY.device)
     _here(dY.device, _dev(workspace, torch.uint8, "workspace"))
     _check(lib().lowra_act_bwd(M, N, act, _ptr(dY), _ptr(z), _ptr(mul), _ptr(dZ), _ptr(dmul), _ptr(db), _ptr(workspace), workspace.numel(), _stream()),
            "lowra_act_bwd")

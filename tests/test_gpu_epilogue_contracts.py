@@ -190,3 +190,49 @@ def test_operands_that_overlap_an_output_are_refused():
                                          mul=at(30000 - 40 * 64, f), bias=buf[30000 + 2 * 40 * 64:][:64])
     assert y.isfinite().all() and kept.isfinite().all()
     torch.cuda.synchronize()
+
+
+# the sizes reach the strips of 32 columns, those of 64, and the chunks of tokens
+@pytest.mark.parametrize("M,N", [(1, 264), (400, 1032), (300, 8200), (900, 520), (2100, 264)])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_activation_backward_in_place(M, N, act):
+    gen = torch.Generator().manual_seed(M)
+    dY, z, mul = (torch.randn(M, N, generator=gen).bfloat16().cuda() for _ in range(3))
+    for m in (None, mul):
+        if act == "none" and m is None:
+            continue
+        for bias_grad in (False, True):
+            kw = dict(z=z, mul=m, bias_grad=bias_grad)
+            want = lowra.lowra_act_bwd(dY, lowra.ACTS[act], **kw)
+            g = dY.clone()
+            got = lowra.lowra_act_bwd(g, lowra.ACTS[act], dZ=g, **kw)
+            assert got[0] is g and all((a is None and b is None) or torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_activation_backward_into_the_callers_tensors_and_without_dmul():
+    M, N = 40, 264
+    gen = torch.Generator().manual_seed(3)
+    dY, z, mul = (torch.randn(M, N, generator=gen).bfloat16().cuda() for _ in range(3))
+    want = lowra.lowra_act_bwd(dY, lowra.ACT_SILU, z=z, mul=mul, bias_grad=True)
+    outs = [torch.full_like(t, 7.0) for t in want]
+    got = lowra.lowra_act_bwd(dY, lowra.ACT_SILU, z=z, mul=mul, dZ=outs[0], dmul=outs[1], db=outs[2])
+    assert all(a is b and torch.equal(a, c) for a, b, c in zip(got, outs, want))
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    for w in (None, ws):
+        dZ, dmul, db = lowra.lowra_act_bwd(dY, lowra.ACT_SILU, z=z, mul=mul, bias_grad=True, workspace=w, mul_grad=False)
+        assert dmul is None and torch.equal(dZ, want[0]) and torch.equal(db, want[2])
+    # a frozen gate without an activation needs no z; a copy where dZ is dY
+    dZ, dmul, _ = lowra.lowra_act_bwd(dY, lowra.ACT_NONE, mul=mul, mul_grad=False)
+    assert dmul is None and torch.equal(dZ, (dY.float() * mul.float()).bfloat16())
+    dZ, _, _ = lowra.lowra_act_bwd(dY, lowra.ACT_NONE, dZ=outs[0])
+    assert dZ is outs[0] and torch.equal(dZ, dY)
+    for bad, err in ((dict(dZ=outs[2]), TypeError), (dict(dmul=outs[0][:39]), ValueError), (dict(db=outs[0]), TypeError), (dict(db=outs[2][:256]), ValueError)):
+        with pytest.raises(err):
+            lowra.lowra_act_bwd(dY, lowra.ACT_SILU, z=z, mul=mul, **bad)
+    # nothing from a call of the linear either
+    L = Layer(264, 128, M, 8, seed=24)
+    zk, mk = (torch.randn(M, 128, generator=gen).bfloat16().cuda() for _ in range(2))
+    want = lowra.lowra_linear_bwd_input_act(*L.state(), L.dY, *L.adapters(), lowra.ACT_SILU, z=zk, mul=mk)
+    for w in (None, ws):
+        dX, dmul = lowra.lowra_linear_bwd_input_act(*L.state(), L.dY, *L.adapters(), lowra.ACT_SILU, z=zk, mul=mk, workspace=w, mul_grad=False)
+        assert dmul is None and torch.equal(dX, want[0])
