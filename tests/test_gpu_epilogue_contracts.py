@@ -236,3 +236,37 @@ def test_activation_backward_into_the_callers_tensors_and_without_dmul():
     for w in (None, ws):
         dX, dmul = lowra.lowra_linear_bwd_input_act(*L.state(), L.dY, *L.adapters(), lowra.ACT_SILU, z=zk, mul=mk, workspace=w, mul_grad=False)
         assert dmul is None and torch.equal(dX, want[0])
+
+
+@pytest.mark.parametrize("size,path", [((520, 1024, 1, 16), lowra.PATH_GEMV), ((520, 1024, 16, 16), lowra.PATH_GEMV), ((2048, 512, 300, 16), lowra.PATH_GEMM),
+                                       ((2048, 512, 300, 16), lowra.PATH_AUTO)])
+def test_residual_in_place_in_every_last_launch(size, path):
+    """The streaming kernel's sum, the sum of the 256-column kernel's split tiles, that of the mid-token kernel's."""
+    L = Layer(*size, seed=25)
+    z, res = (torch.randn(L.M, L.K, generator=torch.Generator().manual_seed(i)).bfloat16().cuda() for i in range(2))
+    lowra.lowra_set_linear_path(path)
+    try:
+        want, _ = lowra.lowra_linear_bwd_input_act(*L.state(), L.dY, *L.adapters(), lowra.ACT_SILU, z=z, residual=res)
+        got, _ = lowra.lowra_linear_bwd_input_act(*L.state(), L.dY, *L.adapters(), lowra.ACT_SILU, z=z, residual=res, dX=res)
+    finally:
+        lowra.lowra_set_linear_path(lowra.PATH_AUTO)
+    assert got is res and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("mix", [(0.5, 0.5, 0.0), (0.4, 0.3, 0.3)])
+@pytest.mark.parametrize("size", [(264, 576, 1, 8), (520, 1024, 16, 16), (136, 4096, 5, 64), (264, 832, 40, 0), (1032, 576, 300, 24), (2048, 512, 300, 64)])
+def test_an_empty_epilogue_leaves_the_plain_calls_bits(size, mix):
+    """Weights, levels and rank-r products of any mantissa: the calls with an epilogue round where the plain calls do and nowhere else."""
+    L = Layer(*size, seed=26, mix=mix)
+    paths = [(lowra.PATH_AUTO, L.M > 16), (lowra.PATH_GEMM, True)] + [(lowra.PATH_GEMV, True)] * (L.M <= 16)
+    for path, both in paths:
+        lowra.lowra_set_linear_path(path)
+        try:
+            if path != lowra.PATH_GEMV:                    # (the streaming forward has no epilogue)
+                y, _ = lowra.lowra_linear_fwd_act(*L.state(), L.x, *L.adapters(), lowra.ACT_NONE)
+                assert torch.equal(y, lowra.lowra_linear_fwd(*L.state(), L.x, *L.adapters()))
+            if both:                                       # (few tokens back take another kernel with an epilogue)
+                dX, _ = lowra.lowra_linear_bwd_input_act(*L.state(), L.dY, *L.adapters(), lowra.ACT_NONE)
+                assert torch.equal(dX, lowra.lowra_linear_bwd_input(*L.state(), L.dY, *L.adapters()))
+        finally:
+            lowra.lowra_set_linear_path(lowra.PATH_AUTO)
