@@ -503,12 +503,12 @@ def lowra_act_bwd(dY, act: int, z=None, mul=None, bias_grad: bool = False, works
     if dmul is None and mul is not None and mul_grad:
         dmul = torch.empty_like(dY)
     _operand(dZ, shape, "dZ", dY.device); _operand(dmul, shape, "dmul", dY.device)
-    if db is None and bias_grad:
-        db = torch.empty(N, dtype=torch.float32, device=dY.device)
     if db is not None:
         _here(dY.device, _dev(db, torch.float32, "db"))
         if tuple(db.shape) != (N,):
             raise ValueError("db: shape mismatch")
+    elif bias_grad:
+        db = torch.empty(N, dtype=torch.float32, device=dY.device)
     if workspace is None:
         workspace = torch.empty(lowra_act_bwd_workspace_bytes(M, N) if db is not None else 0, dtype=torch.uint8, device=dY.device)
     _here(dY.device, _dev(workspace, torch.uint8, "workspace"))
