@@ -192,7 +192,7 @@ lowra_status lowra_linear_bwd_input(const lowra_layout* layout, const uint8_t* p
 /* ---- the linear with what stands around it in a layer: bias, activation, gate and residual in the epilogue.
  * Activations: LOWRA_ACT_GELU is z Phi(z), LOWRA_ACT_GELU_TANH its tanh form, LOWRA_ACT_SILU z / (1 + exp(-z)).  Small results are
  * as exact relatively as large ones until Phi, or the logistic function of the other two, is below 2^-126 (z = -12.95, -10.0 and
- * -87.3): it then counts as zero.  Infinite z give the limits. */
+ * -87.3): from there on it may count as zero.  Infinite z give the limits. */
 enum { LOWRA_ACT_NONE = 0, LOWRA_ACT_RELU = 1, LOWRA_ACT_GELU = 2, LOWRA_ACT_GELU_TANH = 3, LOWRA_ACT_SILU = 4 };
 
 /* Forward:  v = x What^T + s (x A^T) B^T + bias;  y = act(v) mul + residual;  z = v rounded to bf16, for the backward pass.  With

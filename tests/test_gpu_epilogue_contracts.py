@@ -79,7 +79,7 @@ def test_few_tokens_back_without_room_for_splits_stream(N, K, r, M):
 
 
 # Where act(z) is small its relative accuracy counts: one rounding to bf16 (2^-8) and 2^-12 for the arithmetic in front of it, on the two
-# terms of a slope each.  gelu: Phi within 1.5e-4 (2^-12.7), the density's exponent z^2 log2(e) / 2 <= 118 rounded twice (118 x 2^-23 ln 2,
+# terms of a slope each.  gelu: Phi within 8e-6 (2^-16.9), the density's exponent z^2 log2(e) / 2 <= 118 rounded twice (118 x 2^-23 ln 2,
 # 2^-16.6); tanh form and silu: an exponent of at most 126 / log2(e) = 87 after five roundings (87 x 5 x 2^-24, 2^-15.2).
 # The smallest z: Phi, the density and the logistic function stay above 2^-126 there.
 TAILS = {"gelu": 12.75, "gelu_tanh": 9.875, "silu": 86.5}
@@ -118,6 +118,20 @@ def test_small_activations_are_relatively_exact(act):
     assert not bad.any(), list(zip(z[bad].tolist(), dmul[bad].tolist(), ref[bad].tolist()))[:8]
     bad = ~((dZ - (s + d)).abs() <= (s + d).abs() * 2.0 ** -8 + (s + d.abs()) * 2.0 ** -12)
     assert not bad.any(), list(zip(z[bad].tolist(), dZ[bad].tolist(), (s + d)[bad].tolist()))[:8]
+
+
+@pytest.mark.parametrize("act", list(TAILS))
+def test_slopes_are_exact_to_fp32_in_the_bias_gradient(act):
+    """One token and a gradient of ones: db is the slope before it is rounded to bf16.  Its two terms for |z| <= 4 (s: the distribution or
+    logistic function; z dw s (1 - s) or z times the density): s within 6e-7, one unit each of exp2, the reciprocal and two products
+    (5 x 2^-23), together 2^-19.7; silu: an exponent of 5.8 rounded twice (5.8 x 2^-23 ln 2) in place of the fit; tanh form: one of 16 after
+    five roundings (16 x 5 x 2^-24 ln 2, 2^-18.2) in both terms; and s - s^2 is off by 2^-24 of s, times z dw."""
+    z = torch.linspace(-4, 4, 1024).bfloat16()
+    s, d = slope_terms64(z, act)
+    db = lowra.lowra_act_bwd(torch.ones(1, 1024, dtype=torch.bfloat16, device="cuda"), lowra.ACTS[act], z=z.cuda()[None], bias_grad=True)[2].double().cpu()
+    dw = 2 * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * z.double() ** 2) if act == "gelu_tanh" else 1.0
+    tol = (s + d.abs()) * 2.0 ** (-17 if act == "gelu_tanh" else -19) + 2.0 ** -23 * (z.double() * dw).abs()
+    assert ((db - (s + d)).abs() <= tol).all(), float(((db - (s + d)).abs() / (s + d.abs())).max())
 
 
 @pytest.mark.parametrize("path,M", [(0, 1), (0, 40), (lowra.PATH_GEMM, 40)])
