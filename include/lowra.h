@@ -197,7 +197,8 @@ enum { LOWRA_ACT_NONE = 0, LOWRA_ACT_RELU = 1, LOWRA_ACT_GELU = 2, LOWRA_ACT_GEL
 
 /* Forward:  v = x What^T + s (x A^T) B^T + bias;  y = act(v) mul + residual;  z = v rounded to bf16, for the backward pass.  With
  * mul a gated layer is two calls: u by lowra_linear_fwd, then act(gate) u by this one.  All operands bf16 dev, 16-byte aligned;
- * null: not there.  v and y are computed in fp32 from the fp32 sums and rounded once.
+ * null: not there.  v and y are computed in fp32 from the fp32 sums and rounded once; what is multiplied is bf16 as in lowra_linear_fwd
+ * (decoded weights, or up to 16 tokens levels, there with less of a rounding, and s x A^T).
  *   residual may be y itself (the call adds to y); otherwise no operand overlaps y or z.
  * Arguments, workspace and errors otherwise as in lowra_linear_fwd; INVALID_ARG also for a null or unknown epilogue, for such an
  * overlap and when the current device is not the layout's; UNSUPPORTED also from N = 2^22 on. */

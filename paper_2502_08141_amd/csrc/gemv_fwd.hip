@@ -16,7 +16,7 @@
 // Decode: two codes (2, 4 or 8 bits) index the channel's pair table in LDS, whose entry is the two
 // UNSCALED levels as bf16 (App. A.2's lookup); the absmax multiplies the fp32 dot product of the
 // group instead of every weight -- the same sum in another order, with one bf16 rounding per level
-// instead of per product.  One table read per two weights for every width, no per-group set-up.
+// instead of per product (with an epilogue a smaller one, below).  One table read per two weights for every width, no per-group set-up.
 // Tokens are the MFMA rows and channels its columns, so a lane's results belong to its own channel.
 //
 // The activations of a block (16 tokens x 256 columns, 8 KB, the same for every workgroup: L2)
@@ -231,16 +231,52 @@ __device__ __forceinline__ void gemv_body(const GemvParams& p, const E& epi, con
     float* lev = reinterpret_cast<float*>(gv_smem + LEV0) + i * GV_LEV;
     if (wave == 0) {
         *reinterpret_cast<float4*>(lev + 4 * kg) = lv;
-        if (kg == 0) reinterpret_cast<int*>(gv_smem + NL0)[i] = rec.n;
+        if (kg == 0) {
+            reinterpret_cast<int*>(gv_smem + NL0)[i] = rec.n;
+            if (!std::is_same<E, NoEpi>::value) reinterpret_cast<uint32_t*>(lev)[16] = ~0u;
+        }
     }
     if (PER == 1) ask_inputs();
     __syncthreads();                                               // the levels
+    // With an epilogue the levels of a 1- or 2-bit channel go into the table times m / (the largest one's magnitude), and its scales take
+    // the inverse: the largest is then m, a whole number from 128 to 255, exactly, and of 4 W such numbers the workgroup takes the one
+    // whose other levels lie closest to bf16 values.  (As they are, two or four levels that happen to lie badly are off by up to 2^-8 in
+    // every group, which the sum does not average out: outputs of 4096 x 4096 1.7e-3 to 3.9e-3 off in the norm, depending on the table,
+    // 1.55e-3 to 2.1e-3 so, with the result's own rounding 1.66e-3.  One token of 11008 x 4096 15.1 -> 15.6 us, 256 x 512 6.2 -> 6.3; a second
+    // table with what bf16 leaves off was as exact and took 21.2.  The sixteen levels of a 4-bit channel average out among themselves,
+    // 2.3e-3.  Calls without an epilogue keep their bits.)
+    float level_scale = 1.0f, table_scale = 1.0f;
+    if constexpr (!std::is_same<E, NoEpi>::value) {
+        const float4 l = *reinterpret_cast<const float4*>(lev);
+        const float l2 = two ? l.z : 0.0f, l3 = two ? l.w : 0.0f;
+        const float most = fmaxf(fmaxf(fabsf(l.x), fabsf(l.y)), fmaxf(fabsf(l2), fabsf(l3)));
+        auto whole = [](uint32_t c) { return 128.0f + (float)(c * (32 / W)); };
+        auto scale_to = [&](float m) { return m * __builtin_amdgcn_rcpf(most); };
+        const uint32_t c = threadIdx.x >> 4;
+        const float m = whole(c), to = scale_to(m);
+        const float v[4] = {l.x * to, l.y * to, l2 * to, l3 * to};
+        const uint32_t p01 = pack_bf16x2(v[0], v[1]), p23 = pack_bf16x2(v[2], v[3]);
+        const float off = fmaxf(fmaxf(fabsf(v[0] - bf16_bits_to_float(p01)), fabsf(v[1] - __builtin_bit_cast(float, p01 & 0xffff0000u))),
+                                fmaxf(fabsf(v[2] - bf16_bits_to_float(p23)), fabsf(v[3] - __builtin_bit_cast(float, p23 & 0xffff0000u))));
+        uint32_t key = (__builtin_bit_cast(uint32_t, off * __builtin_amdgcn_rcpf(m)) & ~63u) | c;      // what is off, then c: one number to compare
+        const uint2v_t k32 = __builtin_amdgcn_permlane32_swap(key, key, false, false);
+        key = min(k32.x, k32.y);
+        const uint2v_t k16 = __builtin_amdgcn_permlane16_swap(key, key, false, false);
+        key = min(k16.x, k16.y);
+        uint32_t* best = reinterpret_cast<uint32_t*>(lev + 16);
+        if (kg == 0) atomicMin(best, key);                         // (a minimum: the order does not matter)
+        __syncthreads();
+        if (!four && most > 1e-30f && most < 1e30f) {              // (else as they are: a reciprocal would not be finite)
+            const float mb = whole(*best & 63u);
+            level_scale = scale_to(mb); table_scale = most * __builtin_amdgcn_rcpf(mb);
+        }
+    }
     // my channel's pair table, entry e = two codes (low, high) -> two bf16 (unscaled levels; the group scale multiplies the
     // group's dot product)
     uint8_t* tabp = gv_smem + i * GV_TABROW;
     const int nent = 1 << (2 * bits);
     for (int e = (int)(threadIdx.x >> 4); e < nent; e += 4 * W)
-        *reinterpret_cast<uint32_t*>(tabp + 4 * e) = pack_bf16x2(lev[e & ((1 << bits) - 1)], lev[e >> bits]);
+        *reinterpret_cast<uint32_t*>(tabp + 4 * e) = pack_bf16x2(lev[e & ((1 << bits) - 1)] * level_scale, lev[e >> bits] * level_scale);
     if (!FUSE && p.RT > 0 && tpart < p.tparts) {
         for (int o = to; o < nt; o += W * 64) {                    // (more entries than threads: one part, the later entries from memory)
             float v = 0.0f;
@@ -323,8 +359,8 @@ __device__ __forceinline__ void gemv_body(const GemvParams& p, const E& epi, con
                 // my block of this round has landed (so has everything else I asked for); ask for the next
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 if (!x_all && q + 1 < per) issue_x(q + 1);
-                const float a4[4] = {row_ok ? sc[q].x : 0.0f, row_ok && 4 * blk + 1 < p.G ? sc[q].y : 0.0f,
-                                     row_ok && 4 * blk + 2 < p.G ? sc[q].z : 0.0f, row_ok && 4 * blk + 3 < p.G ? sc[q].w : 0.0f};
+                const float a4[4] = {row_ok ? sc[q].x * table_scale : 0.0f, row_ok && 4 * blk + 1 < p.G ? sc[q].y * table_scale : 0.0f,
+                                     row_ok && 4 * blk + 2 < p.G ? sc[q].z * table_scale : 0.0f, row_ok && 4 * blk + 3 < p.G ? sc[q].w * table_scale : 0.0f};
                 // I loaded group kg of my channel; MFMA step (g, h) wants from me the 8 codes
                 // k = 64 g + 32 h + 8 kg .. + 8 of group g: piece kg of each half of the group goes
                 // to lane kg of the lane that loaded it

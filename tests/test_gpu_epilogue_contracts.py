@@ -15,15 +15,16 @@ pytestmark = pytest.mark.gpu
 class Layer:
     """A quantized layer with values of any mantissa: two kernels that add its products in another order give other bits."""
 
-    def __init__(self, N, K, M, r, seed=0, mix=(0.4, 0.3, 0.3)):
+    def __init__(self, N, K, M, r, seed=0, mix=(0.4, 0.3, 0.3), per_channel=False, tables=None):
         rng = np.random.default_rng([seed, N, K, M, r])
         gen = torch.Generator().manual_seed(seed + 100)
         self.N, self.K, self.M, self.r = N, K, M, r
         bits = rng.choice(np.array([1, 2, 4], np.uint8), size=N, p=mix)
-        self.layout = lowra.Layout(K, bits, np.searchsorted([1, 2, 4], bits).astype(np.int32), np.array([1, 2, 4], np.uint8))
+        cb, widths = (np.arange(N), bits) if per_channel else (np.searchsorted([1, 2, 4], bits), np.array([1, 2, 4], np.uint8))
+        self.layout = lowra.Layout(K, bits, cb.astype(np.int32), widths)
         self.packed = torch.from_numpy(rng.integers(0, 256, self.layout.packed_bytes, dtype=np.uint8)).cuda()
         self.absmax = (torch.rand(N, K // 64, generator=gen) + 0.5).cuda()
-        self.mp = torch.randn(3, 16, generator=gen).cuda()
+        self.mp = (torch.randn(widths.size, 16, generator=gen) if tables is None else tables).cuda()
         n = lambda *s: torch.randn(*s, generator=gen).bfloat16().cuda()
         self.x, self.dY = n(M, K), n(M, N)
         self.A, self.B = (n(r, K), n(N, r)) if r else (None, None)
@@ -272,15 +273,72 @@ def test_residual_in_place_in_every_last_launch(size, path):
 def test_an_empty_epilogue_leaves_the_plain_calls_bits(size, mix):
     """Weights, levels and rank-r products of any mantissa: the calls with an epilogue round where the plain calls do and nowhere else."""
     L = Layer(*size, seed=26, mix=mix)
-    paths = [(lowra.PATH_AUTO, L.M > 16), (lowra.PATH_GEMM, True)] + [(lowra.PATH_GEMV, True)] * (L.M <= 16)
-    for path, both in paths:
+    few = L.M <= 16                                        # (other roundings in the forward, another kernel in the input gradient)
+    for path in [lowra.PATH_GEMM] + [lowra.PATH_GEMV if few else lowra.PATH_AUTO]:
         lowra.lowra_set_linear_path(path)
         try:
-            if path != lowra.PATH_GEMV:                    # (the streaming forward has no epilogue)
+            if not few or path == lowra.PATH_GEMM:
                 y, _ = lowra.lowra_linear_fwd_act(*L.state(), L.x, *L.adapters(), lowra.ACT_NONE)
                 assert torch.equal(y, lowra.lowra_linear_fwd(*L.state(), L.x, *L.adapters()))
-            if both:                                       # (few tokens back take another kernel with an epilogue)
-                dX, _ = lowra.lowra_linear_bwd_input_act(*L.state(), L.dY, *L.adapters(), lowra.ACT_NONE)
-                assert torch.equal(dX, lowra.lowra_linear_bwd_input(*L.state(), L.dY, *L.adapters()))
+            dX, _ = lowra.lowra_linear_bwd_input_act(*L.state(), L.dY, *L.adapters(), lowra.ACT_NONE)
+            assert torch.equal(dX, lowra.lowra_linear_bwd_input(*L.state(), L.dY, *L.adapters()))
         finally:
             lowra.lowra_set_linear_path(lowra.PATH_AUTO)
+
+
+def exact_fwd(L):
+    W = lowra.lowra_dequantize(*L.state(), out_dtype=torch.float32).double().cpu()
+    v = L.x.double().cpu() @ W.T
+    return v if L.A is None else v + S * (L.x.double().cpu() @ L.A.double().cpu().T) @ L.B.double().cpu().T
+
+
+# one wavefront form of each kind: 4, 8 and 16 wavefronts, one round and several
+FEW = [(264, 576, 1), (520, 1024, 16), (520, 2048, 7), (136, 4096, 5), (264, 4096, 16), (136, 11008, 2), (8200, 4096, 1), (8200, 1024, 3)]
+
+
+@pytest.mark.parametrize("N,K,M", FEW)
+def test_few_tokens_forward_levels_between_two_bf16_values(N, K, M):
+    """Levels in the ratios 1 : -1 and 1 : -1 : 1/2 : -1/2 times 1 + 2^-8, which lies in the middle between two bf16 values: multiples of
+    one number, they are exact whatever that number is.  An output is off by its rounding (2^-8), by the fp32 scale's (2^-21) and
+    by the sum's (K additions of 2^-24 each at most, of the sum of the magnitudes)."""
+    c = 1 + 2.0 ** -8
+    tables = torch.zeros(3, 16)
+    tables[0, :2], tables[1, :4] = torch.tensor([-c, c]), torch.tensor([-c, -c / 2, c / 2, c])
+    L = Layer(N, K, M, 0, seed=27, mix=(0.5, 0.5, 0.0), tables=tables)
+    ref = exact_fwd(L)
+    W = lowra.lowra_dequantize(*L.state(), out_dtype=torch.float32).double().cpu().abs()
+    y, _ = lowra.lowra_linear_fwd_act(*L.state(), L.x, None, None, S, lowra.ACT_NONE)
+    assert ((y.double().cpu() - ref).abs() <= ref.abs() * 2.0 ** -8 * (1 + 2.0 ** -8) + (2.0 ** -21 + min(K, 512) * 2.0 ** -24) * (L.x.double().cpu().abs() @ W.T)).all()
+
+
+@pytest.mark.parametrize("N,K,M", FEW)
+def test_few_tokens_forward_rounds_little_but_its_result(N, K, M):
+    """Any levels, one table per channel.  Of 16 to 64 multiples the best one's largest error is expected at 0.4 of a rounding for the
+    three free levels of a 2-bit channel (u^3 = 1 / 16), 0.06 for the one of a 1-bit channel: at most 0.4 x 2^-8 / sqrt(3) = 2^-10.1 in the norm beside
+    the result's own rounding; rounded as they are they would be 2^-9.3 off.  The rank-r product is rounded to bf16: 2^-8 / sqrt(3) = 2^-8.8 of
+    its part of the result in the norm."""
+    L = Layer(N, K, M, 8, seed=28, mix=(0.5, 0.5, 0.0), per_channel=True)
+    both = exact_fwd(L)
+    side = S * (L.x.double().cpu() @ L.A.double().cpu().T) @ L.B.double().cpu().T
+    for A, B, ref, more in ((L.A, L.B, both, 2.0 ** -8.8 * float(side.norm() / both.norm())), (None, None, both - side, 0.0)):
+        far = lambda t: float((t.double().cpu() - ref).norm() / ref.norm())
+        y, _ = lowra.lowra_linear_fwd_act(*L.state(), L.x, A, B, S, lowra.ACT_NONE)
+        assert far(y) ** 2 <= far(ref.bfloat16()) ** 2 + 2.0 ** -20.2 * 1.1 + more ** 2
+        if A is None:
+            assert far(lowra.lowra_linear_fwd(*L.state(), L.x, None, None, S)) > far(y)
+
+
+def test_few_tokens_forward_with_levels_of_any_size():
+    """Zero levels, levels near the ends of fp32 and infinite ones (which stay in their channel)."""
+    L0 = Layer(64, 512, 3, 0, seed=29, mix=(0.0, 1.0, 0.0), per_channel=True)
+    tables = L0.mp.clone()
+    for row, f in ((0, 0.0), (1, 1e-36), (2, 1e-31), (3, 1e30), (4, 1e34), (5, 2.0 ** 100), (6, 2.0 ** -100)):
+        tables[row] *= f
+    tables[7, 1:4], tables[8, 2], tables[9, 0] = 0.0, float("inf"), float("nan")
+    L = Layer(64, 512, 3, 0, seed=29, mix=(0.0, 1.0, 0.0), per_channel=True, tables=tables)
+    y = lowra.lowra_linear_fwd_act(*L.state(), L.x, None, None, S, lowra.ACT_NONE)[0].double().cpu()
+    ref = exact_fwd(L)
+    assert (y[:, 0] == 0).all() and not y[:, 8].isfinite().any() and y[:, 9].isnan().all()
+    others = [i for i in range(64) if i not in (0, 8, 9)]
+    for i in others:                                       # a rounding of every level and of the result, in the norm over three tokens and 512 features
+        assert float((y[:, i] - ref[:, i]).norm()) <= 2 * 2.0 ** -8 * float((L.x.double().cpu().square() @ lowra.lowra_dequantize(*L.state(), out_dtype=torch.float32).double().cpu()[i].square()).sum().sqrt()), i
