@@ -15,7 +15,8 @@
  *   - bf16 tensors are passed as uint16_t bit patterns.
  *   - The caller owns every buffer.  The library allocates device memory only inside
  *     lowra_layout_create (a few small index arrays; freed in lowra_layout_destroy) and
- *     lowra_fwd_batch_create (the batch's descriptors; freed in lowra_fwd_batch_destroy).
+ *     lowra_fwd_batch_create, lowra_bwd_batch_create and lowra_muon_batch_create (the batch's
+ *     descriptors; freed in the batch's destroy).
  *   - Every compute call enqueues on `stream` (a hipStream_t passed as void*, NULL = the
  *     default stream) and returns without synchronising.
  *   - Errors are returned as lowra_status; nothing throws or aborts.  Arguments are validated
@@ -111,7 +112,8 @@ size_t lowra_packed_bytes(const lowra_layout* layout);
  * non-zero at r == 0; and, for the token counts whose contractions are split between workgroups, the splits'
  * fp32 partial sums and tiles (at most 64 MiB).  A linear call with less is refused only below what it cannot do
  * without (all but the room for these splits): it then forms the rank-r product in one workgroup per 16 rows,
- * with the same bits, and splits the main contraction less, which takes longer and adds in another order. */
+ * with the same bits, and splits the main contraction less, which takes longer and adds in another order (an input
+ * gradient of up to 16 tokens with an epilogue: in another kernel). */
 size_t lowra_workspace_bytes(const lowra_layout* layout, int op, int M, int r);
 
 /* Quantize (App. A.1).  For every 64-element group: absmax a = max|w| is stored; every weight is

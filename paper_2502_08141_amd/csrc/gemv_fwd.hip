@@ -238,13 +238,14 @@ __device__ __forceinline__ void gemv_body(const GemvParams& p, const E& epi, con
     }
     if (PER == 1) ask_inputs();
     __syncthreads();                                               // the levels
-    // With an epilogue the levels of a 1- or 2-bit channel go into the table times m / (the largest one's magnitude), and its scales take
-    // the inverse: the largest is then m, a whole number from 128 to 255, exactly, and of 4 W such numbers the workgroup takes the one
-    // whose other levels lie closest to bf16 values.  (As they are, two or four levels that happen to lie badly are off by up to 2^-8 in
-    // every group, which the sum does not average out: outputs of 4096 x 4096 1.7e-3 to 3.9e-3 off in the norm, depending on the table,
-    // 1.55e-3 to 2.1e-3 so, with the result's own rounding 1.66e-3.  One token of 11008 x 4096 15.1 -> 15.6 us, 256 x 512 6.2 -> 6.3; a second
-    // table with what bf16 leaves off was as exact and took 21.2.  The sixteen levels of a 4-bit channel average out among themselves,
-    // 2.3e-3.  Calls without an epilogue keep their bits.)
+    // With an epilogue the levels of a 1- or 2-bit channel go into the table times m / (the largest one's magnitude), and its scales
+    // take the inverse: the largest is then m, a whole number from 128 to 255, exactly, and of 4 W such numbers the workgroup takes
+    // the one whose other levels lie closest to bf16 values.  (As they are, two or four levels that happen to lie badly are off by
+    // up to 2^-8 in every group, which the sum does not average out: outputs of 4096 x 4096 1.7e-3 to 3.9e-3 off in the norm,
+    // depending on the table, 1.55e-3 to 2.2e-3 so with up to a third of 4-bit channels, the result's own rounding 1.66e-3 of it.
+    // One token of 11008 x 4096 15.1 -> 15.6 us, 256 x 512 6.2 -> 6.3; a second table with what bf16 leaves off was as exact and
+    // took 21.2.  The sixteen levels of a 4-bit channel average out in part among themselves: 1.8e-3 to 2.7e-3.  Calls without an
+    // epilogue keep their bits.)
     float level_scale = 1.0f, table_scale = 1.0f;
     if constexpr (!std::is_same<E, NoEpi>::value) {
         const float4 l = *reinterpret_cast<const float4*>(lev);

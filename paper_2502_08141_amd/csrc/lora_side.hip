@@ -24,7 +24,8 @@ __device__ __forceinline__ void wait_newer(int newer) {
     }
 }
 
-// out[m][j] = bf16( s * sum_c P[m][c] Q[j][c] ), j < 16 CT (rows j >= r of Q count as zero).
+// out[m][j] = bf16( s * sum_c P[m][c] Q[j][c] ), j < 16 CT (rows j >= r of Q count as zero).  The sums are fp32; bf16 is what the matrix
+// instructions of the products with B or A take, and its rounding (2^-8 at most) is of the rank-r term alone.
 //
 // One workgroup per 16 PT token rows and one slice of the contraction (grid.y).  PT = 1 with a single
 // slice: M = 4096 fills all 256 compute units.  Tall inputs take PT = 4 and split the contraction
