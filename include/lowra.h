@@ -15,7 +15,7 @@
  *   - bf16 tensors are passed as uint16_t bit patterns.
  *   - The caller owns every buffer.  The library allocates device memory only inside
  *     lowra_layout_create (a few small index arrays; freed in lowra_layout_destroy) and
- *     lowra_fwd_batch_create, lowra_bwd_batch_create and lowra_muon_batch_create (the batch's
+ *     lowra_fwd_batch_create, lowra_bwd_batch_create, lowra_muon_batch_create and lowra_adamw_batch_create (the batch's
  *     descriptors; freed in the batch's destroy).
  *   - Every compute call enqueues on `stream` (a hipStream_t passed as void*, NULL = the
  *     default stream) and returns without synchronising.
@@ -344,6 +344,122 @@ lowra_status lowra_muon_batch_create(int n, const lowra_muon_item* items, void* 
                                      lowra_muon_batch** out);
 lowra_status lowra_muon_batch_run(const lowra_muon_batch* batch, const lowra_muon_step* step, void* stream);
 void lowra_muon_batch_destroy(lowra_muon_batch* batch);
+
+/* ---- what else a fine-tuning step of such a layer needs: norms, rotary positions, the loss over the vocabulary, AdamW.
+ *
+ * Norms over the rows of x [M,N]:   xh = (x - mean) rstd,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)   (LOWRA_NORM_RMS: mean = 0)
+ *   forward    y = xh weight + bias
+ *   backward   g = dY weight;   dX = rstd (g - mean(g) - xh mean(g xh)) + residual   (LOWRA_NORM_RMS: without mean(g))
+ *              dweight[n] = sum_m dY xh;   dbias[n] = sum_m dY
+ * x, y, dY, residual (a gradient that reaches x by another way), dX [M,N], weight, bias [N] bf16 dev | dweight, dbias [N] fp32 dev (out).
+ * weight, bias, residual: null: not there; dX, dweight, dbias: null: not asked for.  The backward pass needs nothing of the forward
+ * pass but x.  Everything is fp32, each output rounded once; the sums are added in a fixed order.  A row that holds an infinity or a NaN spoils
+ * its own row, and the sums.  y may be x itself, dX may be residual itself; otherwise nothing overlaps an output.
+ *   workspace: dev, >= lowra_norm_bwd_workspace_bytes(M, N), 16-byte aligned; unused without dweight and dbias.
+ * M == 0 writes zeros to dweight and dbias.  INVALID_ARG: a negative size, an unknown kind, eps below zero, a missing operand, no output
+ * at all, residual without dX, such an overlap; UNSUPPORTED: N % 8 != 0, N above 16384, M above 2^30; MISALIGNED; WORKSPACE_TOO_SMALL. */
+enum { LOWRA_NORM_LAYER = 0, LOWRA_NORM_RMS = 1 };
+lowra_status lowra_norm_fwd(int M, int N, int kind, const uint16_t* x, const uint16_t* weight, const uint16_t* bias, float eps,
+                            uint16_t* y, void* stream);
+size_t lowra_norm_bwd_workspace_bytes(int M, int N);
+lowra_status lowra_norm_bwd(int M, int N, int kind, const uint16_t* dY, const uint16_t* x, const uint16_t* weight, float eps,
+                            const uint16_t* residual, uint16_t* dX, float* dweight, float* dbias, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Rotary positions of up to four tensors of heads (queries and keys) in one launch:  with the angle positions[m] f_j the pair (a, b)
+ * of a head's first `rot` columns becomes magnitude (a cos - b sin, a sin + b cos); columns from rot on stay as they are.  Pair j is
+ * the columns j and j + rot/2 (LOWRA_ROPE_HALF), or 2 j and 2 j + 1 (LOWRA_ROPE_INTERLEAVED).  inverse: by the negative angle, times the same
+ * magnitude, which is the gradient of the forward call.
+ *   tensors: host array of n entries (read before the call returns): x, y [M tokens][heads][D] bf16 dev with strides in elements
+ *   (the columns of a head are contiguous; 2-byte alignment is enough, 16-byte runs are fastest).  y may be x, with the same strides; otherwise no y
+ *   overlaps another y or an x (heads of several tensors between each other in one row, at the same token stride, do not).
+ *   positions [M] int32 dev (negative ones turn backwards) | turns [rot/2] uint64 dev, from lowra_rope_frequencies: the fraction of a full turn
+ *   per position in units of 2^-64, so that the angle is exact at every position.  Sine and cosine are exact to fp32 rounding; outputs are rounded once.
+ * INVALID_ARG: n <= 0, a non-positive size, rot > D, an unknown layout, a missing pointer, a negative stride, a y whose heads overlap, an
+ * overlap as above; UNSUPPORTED: n > 4, odd rot, D above 2^20, M above 2^30, more than 2^32 elements or 2^20 heads; MISALIGNED (turns: 8 bytes, positions: 4, tensors: 2). */
+enum { LOWRA_ROPE_HALF = 0, LOWRA_ROPE_INTERLEAVED = 1 };
+typedef struct lowra_rope_tensor {
+    const uint16_t* x;
+    uint16_t* y;
+    int heads;
+    int64_t x_token_stride, x_head_stride, y_token_stride, y_head_stride;
+} lowra_rope_tensor;
+lowra_status lowra_rope(int n, const lowra_rope_tensor* tensors, int M, int D, int rot, int layout, const int32_t* positions,
+                        const uint64_t* turns, float magnitude, int inverse, void* stream);
+
+/* Host only: the frequencies f_j = base^(-2 j / rot) radians per position, j < rot/2, as fractions of a turn (above), stretched for contexts
+ * longer than the `original` one that a model was trained with:
+ *   SCALE_NONE    as they are
+ *   SCALE_LINEAR  f / factor
+ *   SCALE_BASE    with base factor^(rot / (rot - 2)) in place of base: the slowest pair is slowed by factor, the fastest not at all
+ *   SCALE_TURNS   f (k + (1 - k) / factor), k = (turns - low) / (high - low) within 0..1, turns = original f / 2 pi: the pairs that turn
+ *                 `high` times or more in the original context stay, those that turn `low` times or less are slowed
+ *   SCALE_INDEX   the same with k a ramp over the pairs' numbers, from floor(i(high)) to ceil(i(low)), at least 0 and at most rot - 1, i(t) =
+ *                 rot log(original / (2 pi t)) / (2 log base)
+ * Unused parameters are ignored.  INVALID_ARG: rot <= 0, base not above one, factor below one, original, low or high - low not above zero
+ * where they are used, an unknown scaling, a null pointer; UNSUPPORTED: odd rot, rot above 2^20, SCALE_BASE with rot == 2. */
+enum { LOWRA_ROPE_SCALE_NONE = 0, LOWRA_ROPE_SCALE_LINEAR = 1, LOWRA_ROPE_SCALE_BASE = 2, LOWRA_ROPE_SCALE_TURNS = 3, LOWRA_ROPE_SCALE_INDEX = 4 };
+lowra_status lowra_rope_frequencies(int rot, double base, int scaling, double factor, int original, double low, double high,
+                                    uint64_t* turns_host);
+
+/* Softmax cross entropy over a vocabulary of V words, with the gradient of the hidden states; the logits are never in memory:
+ *   z = h W^T;   lse = log sum_v exp z_v;   loss = lse - z_target;   dH = weight (softmax(z) - e_target) W
+ * The head W is frozen (as the base is, Sec. 3), so it has no gradient.
+ *   h [M,K], W [V,K] bf16 dev | targets [M] int32 dev: a token whose target is outside 0..V-1 (padding) has loss 0 and a gradient of zeros,
+ *   whatever its h holds | weights [M] fp32 dev or null (one): of a token's loss in what is differentiated, e.g. 1 / number of targets
+ *   loss [M] fp32 dev (out, without the weight) | lse [M] fp32 dev (out) or null | dH [M,K] bf16 dev (out) or null: the loss alone
+ *   workspace: dev, >= lowra_vocab_loss_workspace_bytes(M, V, K, dH wanted), 16-byte aligned; about 256 MiB + 64 MiB at most (tokens are taken in pieces),
+ *   unless 256 tokens' rows of K fp32 sums or V words alone take more
+ * Products are bf16 with fp32 sums; the probabilities are rounded to bf16 before they meet W, but not the target's term, which is fp32 and
+ * keeps its digits where the model is sure; a probability below 2^-126 of the largest may count as zero.  The order of all sums is fixed.  A NaN or an infinity in a row of h stays in its row.
+ * M == 0 is a no-op.  INVALID_ARG: M < 0, V <= 0, K <= 0, a missing pointer, an output or the workspace that overlaps anything; UNSUPPORTED: K % 8
+ * != 0, V above 2^21, K above 2^20, M above 2^30; MISALIGNED; WORKSPACE_TOO_SMALL. */
+size_t lowra_vocab_loss_workspace_bytes(int M, int V, int K, int grad);
+lowra_status lowra_vocab_loss(int M, int V, int K, const uint16_t* h, const uint16_t* W, const int32_t* targets, const float* weights,
+                              float* loss, float* lse, uint16_t* dH, void* workspace, size_t workspace_bytes, void* stream);
+
+/* AdamW on every tensor of a batch (the adapters of any number of layers, norm weights), one launch for each width of the states:
+ *   g = grad_scale grad;   m' = b1 m + (1 - b1) g;   v' = b2 v + (1 - b2) g^2        (each product and sum rounded to fp32 by itself)
+ *   w' = w - lr lr_scale ((m' / (1 - b1^step)) / (sqrt(v' / (1 - b2^step)) + eps) + weight_decay decay_scale w)
+ * state_bits 32: m and v are fp32.  state_bits 8: they are one byte an element, in groups of 64 consecutive elements (the last one may be short) with
+ * the group's largest magnitude A in fp32 (absmax, [ceil(count / 64)]): m a signed code q for sgn(q) (q / 127)^2 A, v an unsigned one for
+ * (q / 255)^4 A, evaluated in fp32 as (u |u|) A and ((u u)(u u)) A with u = q times the fp32 reciprocal of 127 or 255.  A magnitude x is coded as
+ * the number of k >= 0 with (k + 1/2)^2 A < 127^2 x, or (k + 1/2)^4 A < 255^4 x, compared in 64 bits; a v above zero as 1 at least.  w' is formed
+ * from m' and v' before they are coded.  Zeroed bytes are zero states.  What is not finite spoils its element with 32-bit states and its group with 8-bit ones.
+ *   items: host array of n entries (read during create only); device pointers, 16-byte aligned (absmax: 4), that stay valid and in place for the
+ *   life of the batch; m_out, v_out, m_absmax_out, v_absmax_out and weight_out may be the inputs of that name (in place), nothing else overlaps an output.
+ *   grad_scale: one fp32 dev or null (one), e.g. the factor of a gradient clipping, without a wait for it.
+ * A run takes the scalars (a captured one repeats those it was captured with) and only launches.  create allocates device memory for the descriptors and
+ * copies them synchronously; destroy frees.
+ * create: INVALID_ARG (null / n <= 0 / count <= 0 / a missing pointer; absmax is needed with 8 bits and null with 32; an output that overlaps
+ * anything else of the batch, so no tensor is in it twice), UNSUPPORTED (other state_bits, more than 2^31 elements), MISALIGNED, OUT_OF_MEMORY, HIP_ERROR.
+ * run: INVALID_ARG (null, step < 1, a beta outside [0, 1), eps below zero, another device than the one of create), MISALIGNED, HIP_ERROR. */
+typedef struct lowra_adamw_item {
+    int64_t count;
+    int state_bits;
+    float lr_scale, decay_scale;
+    const float* grad;
+    const void *m, *v;
+    const float *m_absmax, *v_absmax;
+    const float* weight;
+    void *m_out, *v_out;
+    float *m_absmax_out, *v_absmax_out;
+    float* weight_out;
+    uint16_t* weight_bf16;       /* w' rounded to bf16 (out), or null */
+} lowra_adamw_item;
+typedef struct lowra_adamw_step {
+    double lr, beta_one, beta_two, eps, weight_decay;
+    int64_t step;                /* from 1 */
+} lowra_adamw_step;
+typedef struct lowra_adamw_batch lowra_adamw_batch;
+lowra_status lowra_adamw_batch_create(int n, const lowra_adamw_item* items, lowra_adamw_batch** out);
+lowra_status lowra_adamw_batch_run(const lowra_adamw_batch* batch, const lowra_adamw_step* step, const float* grad_scale, void* stream);
+void lowra_adamw_batch_destroy(lowra_adamw_batch* batch);
+
+/* What 8-bit states stand for: out[i] = sgn(q) (q / 127)^2 A (is_signed: m) or (q / 255)^4 A (v), as above.
+ *   codes [count] bytes, out [count] fp32 dev, 16-byte aligned | absmax [ceil(count / 64)] fp32 dev.  INVALID_ARG: count < 0, a null pointer, an
+ *   overlap; UNSUPPORTED: more than 2^33; MISALIGNED. */
+lowra_status lowra_adamw_state(int64_t count, int is_signed, const void* codes, const float* absmax, float* out, void* stream);
 
 /* Alternating low-rank initialisation of the adapter (Sec. 4.1, "Using LoftQ as low-rank initializer";
  * App. D; the paper runs five steps): from B A = 0, each step quantizes W - B A with the layout's widths

@@ -6,6 +6,7 @@
 #include <numeric>
 
 #include "../../include/lowra.h"
+#include "api_util.h"
 #include "epilogue.h"
 #include "gemm_mid.h"
 #include "muon.h"
@@ -18,7 +19,6 @@ constexpr int kMaxRank = 128;
 constexpr int kFwdTileRows = 256;
 
 bool valid_bits(int b) { return b == 1 || b == 2 || b == 4; }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 lowra_status plan_rows(int N, int K, int group, const uint8_t* bits, int64_t* off) {
     if (!bits && N > 0) return LOWRA_INVALID_ARG;
@@ -33,23 +33,6 @@ lowra_status plan_rows(int N, int K, int group, const uint8_t* bits, int64_t* of
     return LOWRA_OK;
 }
 
-// Whether an output of a call overlaps another one or an operand.  out[0] may be inputs[0] itself: every element of that operand is read
-// by the thread that writes the result in its place, before it does.
-struct Span { const void* p; size_t bytes; };
-bool overlap(const Span& a, const Span& b) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-    return a.p && b.p && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
-}
-template <size_t O, size_t I>
-bool outputs_overlap(const Span (&outputs)[O], const Span (&inputs)[I]) {
-    for (size_t o = 0; o < O; ++o) {
-        for (size_t other = 0; other < o; ++other)
-            if (overlap(outputs[o], outputs[other])) return true;
-        for (size_t i = 0; i < I; ++i)
-            if (overlap(outputs[o], inputs[i]) && !(o == 0 && i == 0 && outputs[o].p == inputs[i].p)) return true;
-    }
-    return false;
-}
 size_t scale_bytes(const lowra_layout* L) { return (size_t)L->N * L->G * (L->scale_bf16 ? 2 : 4); }
 
 }  // namespace

@@ -28,6 +28,10 @@ PATH_AUTO, PATH_GEMV, PATH_GEMM, PATH_GEMV_GENERAL = 0, 1, 2, 3
 SCALE_FP32, SCALE_BF16 = 0, 1
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
+NORM_LAYER, NORM_RMS = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_TURNS, ROPE_SCALE_INDEX = 0, 1, 2, 3, 4
+ROPE_SCALINGS = {"none": ROPE_SCALE_NONE, "linear": ROPE_SCALE_LINEAR, "base": ROPE_SCALE_BASE, "turns": ROPE_SCALE_TURNS, "index": ROPE_SCALE_INDEX}
 
 SYMBOLS = [
     "lowra_status_string", "lowra_plan_rows", "lowra_layout_create", "lowra_layout_destroy", "lowra_layout_set_scale_dtype",
@@ -40,6 +44,9 @@ SYMBOLS = [
     "lowra_bwd_batch_workspace_bytes", "lowra_bwd_batch_create", "lowra_bwd_batch_run", "lowra_bwd_batch_destroy",
     "lowra_linear_fwd_act", "lowra_linear_bwd_input_act", "lowra_act_bwd", "lowra_act_bwd_workspace_bytes",
     "lowra_muon_batch_workspace_bytes", "lowra_muon_batch_create", "lowra_muon_batch_run", "lowra_muon_batch_destroy",
+    "lowra_norm_fwd", "lowra_norm_bwd", "lowra_norm_bwd_workspace_bytes", "lowra_rope", "lowra_rope_frequencies",
+    "lowra_vocab_loss", "lowra_vocab_loss_workspace_bytes",
+    "lowra_adamw_batch_create", "lowra_adamw_batch_run", "lowra_adamw_batch_destroy", "lowra_adamw_state",
     "lowra_measure_copy", "lowra_measure_read", "lowra_measure_mfma", "lowra_measure_mfma_random",
 ]
 
@@ -70,6 +77,23 @@ class MuonStep(C.Structure):
     """lowra_muon_step."""
     _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("nesterov", C.c_int), ("weight_decay", C.c_float), ("steps", C.c_int),
                 ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("eps", C.c_float)]
+
+
+class RopeTensor(C.Structure):
+    """lowra_rope_tensor (device pointers, strides in elements)."""
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("heads", C.c_int)] + [(n, C.c_int64) for n in (
+        "x_token_stride", "x_head_stride", "y_token_stride", "y_head_stride")]
+
+
+class AdamWItemRecord(C.Structure):
+    """lowra_adamw_item (device pointers)."""
+    _fields_ = [("count", C.c_int64), ("state_bits", C.c_int), ("lr_scale", C.c_float), ("decay_scale", C.c_float)] + [(n, C.c_void_p) for n in (
+        "grad", "m", "v", "m_absmax", "v_absmax", "weight", "m_out", "v_out", "m_absmax_out", "v_absmax_out", "weight_out", "weight_bf16")]
+
+
+class AdamWStep(C.Structure):
+    """lowra_adamw_step."""
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta_one", "beta_two", "eps", "weight_decay")] + [("step", C.c_int64)]
 
 
 class LowraError(RuntimeError):
@@ -136,6 +160,20 @@ def lib() -> C.CDLL:
         L.lowra_muon_batch_run.argtypes = [vp, vp, vp]
         L.lowra_muon_batch_destroy.restype = None
         L.lowra_muon_batch_destroy.argtypes = [vp]
+        L.lowra_norm_fwd.argtypes = [C.c_int] * 3 + [u16p] * 3 + [C.c_float, u16p, vp]
+        L.lowra_norm_bwd_workspace_bytes.restype = C.c_size_t
+        L.lowra_norm_bwd_workspace_bytes.argtypes = [C.c_int, C.c_int]
+        L.lowra_norm_bwd.argtypes = [C.c_int] * 3 + [u16p] * 3 + [C.c_float, u16p, u16p, f32p, f32p, vp, C.c_size_t, vp]
+        L.lowra_rope_frequencies.argtypes = [C.c_int, C.c_double, C.c_int, C.c_double, C.c_int, C.c_double, C.c_double, vp]
+        L.lowra_rope.argtypes = [C.c_int, vp] + [C.c_int] * 4 + [vp, vp, C.c_float, C.c_int, vp]
+        L.lowra_vocab_loss_workspace_bytes.restype = C.c_size_t
+        L.lowra_vocab_loss_workspace_bytes.argtypes = [C.c_int] * 4
+        L.lowra_vocab_loss.argtypes = [C.c_int] * 3 + [u16p, u16p, vp, f32p, f32p, f32p, u16p, vp, C.c_size_t, vp]
+        L.lowra_adamw_batch_create.argtypes = [C.c_int, vp, vp]
+        L.lowra_adamw_batch_run.argtypes = [vp, vp, f32p, vp]
+        L.lowra_adamw_batch_destroy.restype = None
+        L.lowra_adamw_batch_destroy.argtypes = [vp]
+        L.lowra_adamw_state.argtypes = [C.c_int64, C.c_int, vp, f32p, f32p, vp]
         L.lowra_channel_mse.argtypes = [C.c_int, C.c_int, f32p, f32p, f32p, f32p, vp]
         L.lowra_assign_precisions.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_double, C.c_void_p]
         L.lowra_measure_copy.argtypes = [vp, vp, C.c_size_t, vp]
@@ -785,6 +823,226 @@ class MuonBatch:
             self.close()
         except Exception:
             pass
+
+
+def _rows(t, name: str):
+    """A contiguous bf16 device tensor of rows, at most 2^31 - 1 each way, on the current device -> its shape."""
+    _dev(t, torch.bfloat16, name)
+    if t.dim() != 2 or max(t.shape) > 0x7fffffff:
+        raise ValueError(f"{name}: shape mismatch")
+    _here(t.device)
+    return int(t.shape[0]), int(t.shape[1])
+
+
+def _typed(t, dtype, shape, name: str, device):
+    """An optional tensor of this type, shape and device."""
+    if t is not None:
+        _here(device, _dev(t, dtype, name))
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: shape mismatch")
+    return t
+
+
+def lowra_norm_fwd(x, weight=None, bias=None, kind: int = NORM_LAYER, eps: float = 1e-5, y=None):
+    """y [M,N] bf16 = (x - mean) / sqrt(mean((x - mean)^2) + eps) weight + bias over the rows of x [M,N] bf16; NORM_RMS: mean = 0.  weight, bias:
+    [N] bf16 or None; y may be x."""
+    M, N = _rows(x, "x")
+    _operand(weight, (N,), "weight", x.device); _operand(bias, (N,), "bias", x.device)
+    if y is None:
+        y = torch.empty_like(x)
+    _operand(y, (M, N), "y", x.device)
+    _check(lib().lowra_norm_fwd(M, N, int(kind), _ptr(x), _ptr(weight), _ptr(bias), float(eps), _ptr(y), _stream()), "lowra_norm_fwd")
+    return y
+
+
+def lowra_norm_bwd_workspace_bytes(M: int, N: int) -> int:
+    return int(lib().lowra_norm_bwd_workspace_bytes(int(M), int(N)))
+
+
+def lowra_norm_bwd(dY, x, weight=None, kind: int = NORM_LAYER, eps: float = 1e-5, residual=None, input_grad: bool = True, weight_grad: bool = False,
+                   bias_grad: bool = False, dX=None, dweight=None, dbias=None, workspace=None):
+    """The way back of lowra_norm_fwd for dY [M,N] bf16 -> (dX, dweight, dbias): dX bf16 with `residual` [M,N] bf16 added (None without `input_grad`),
+    dweight and dbias fp32 [N] (None without `weight_grad`, `bias_grad`).  What is given of the three is written there; dX may be residual."""
+    M, N = _rows(dY, "dY")
+    device = dY.device
+    _operand(x, (M, N), "x", device); _operand(weight, (N,), "weight", device); _operand(residual, (M, N), "residual", device)
+    if x is None:
+        raise ValueError("x is missing")
+    if dX is None and input_grad:
+        dX = torch.empty_like(dY)
+    _operand(dX, (M, N), "dX", device)
+    if dweight is None and weight_grad:
+        dweight = torch.empty(N, dtype=torch.float32, device=device)
+    if dbias is None and bias_grad:
+        dbias = torch.empty(N, dtype=torch.float32, device=device)
+    _typed(dweight, torch.float32, (N,), "dweight", device); _typed(dbias, torch.float32, (N,), "dbias", device)
+    if workspace is None:
+        workspace = torch.empty(lowra_norm_bwd_workspace_bytes(M, N) if dweight is not None or dbias is not None else 0, dtype=torch.uint8, device=device)
+    _here(device, _dev(workspace, torch.uint8, "workspace"))
+    _check(lib().lowra_norm_bwd(M, N, int(kind), _ptr(dY), _ptr(x), _ptr(weight), float(eps), _ptr(residual), _ptr(dX), _ptr(dweight), _ptr(dbias),
+                                _ptr(workspace), workspace.numel(), _stream()), "lowra_norm_bwd")
+    return dX, dweight, dbias
+
+
+def lowra_rope_frequencies(rot: int, base: float = 10000.0, scaling: int = ROPE_SCALE_NONE, factor: float = 1.0, original: int = 0, low: float = 1.0,
+                           high: float = 8.0, device="cuda"):
+    """The plan of lowra_rope for `rot` columns: the pairs' frequencies base^(-2 j / rot), stretched as `scaling` (ROPE_SCALE_*) says, as an int64
+    tensor [rot/2] of 2^-64 turns a position on `device`."""
+    turns = np.zeros(max(int(rot) // 2, 1), np.uint64)
+    _check(lib().lowra_rope_frequencies(int(rot), float(base), int(scaling), float(factor), int(original), float(low), float(high), turns.ctypes.data),
+           "lowra_rope_frequencies")
+    return torch.from_numpy(turns.view(np.int64)).to(device)
+
+
+def lowra_rope(x, positions, turns, layout: int = ROPE_HALF, inverse: bool = False, magnitude: float = 1.0, out=None):
+    """Rotary positions of x [M, heads, D] bf16, or of a list of up to four of those (queries and keys) with the same M and D, by positions [M]
+    int32 and the plan `turns` (lowra_rope_frequencies), whose length says how many columns are turned.  Tokens and heads may have any stride, the
+    columns are contiguous.  `out`: where to write, of the same shapes (x itself: in place); new tensors without it.  `inverse`: the way back."""
+    many = isinstance(x, (list, tuple))
+    xs = list(x) if many else [x]
+    if not xs or len(xs) > 4:
+        raise ValueError("one to four tensors")
+    for t in xs:
+        if not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.is_cuda and t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] == 1)):
+            raise TypeError("x: need bf16 device tensors [tokens, heads, columns] with contiguous columns")
+    M, D, device = int(xs[0].shape[0]), int(xs[0].shape[2]), xs[0].device
+    _here(device, *xs, _dev(positions, torch.int32, "positions"), _dev(turns, torch.int64, "turns"))
+    if max(M, D) > 0x7fffffff or tuple(positions.shape) != (M,) or turns.dim() != 1:
+        raise ValueError("positions or turns: shape mismatch")
+    if out is None:
+        ys = [torch.empty(t.shape, dtype=torch.bfloat16, device=device) for t in xs]
+    else:
+        ys = list(out) if isinstance(out, (list, tuple)) else [out]
+    if len(ys) != len(xs):
+        raise ValueError("out: as many tensors as x")
+    arr = (RopeTensor * len(xs))()
+    for i, (a, b) in enumerate(zip(xs, ys)):
+        if not (b.dtype is torch.bfloat16 and b.is_cuda and b.dim() == 3 and (b.stride(2) == 1 or b.shape[2] == 1)):
+            raise TypeError("out: need bf16 device tensors [tokens, heads, columns] with contiguous columns")
+        if a.shape != b.shape or a.shape[0] != M or a.shape[2] != D or b.device != device:
+            raise ValueError("shape or device mismatch")
+        arr[i] = RopeTensor(a.data_ptr(), b.data_ptr(), int(a.shape[1]), a.stride(0), a.stride(1), b.stride(0), b.stride(1))
+    _check(lib().lowra_rope(len(xs), C.addressof(arr), M, D, 2 * int(turns.shape[0]), int(layout), _ptr(positions), _ptr(turns), float(magnitude), int(bool(inverse)),
+                            _stream()), "lowra_rope")
+    return ys if many else ys[0]
+
+
+def lowra_vocab_loss_workspace_bytes(M: int, V: int, K: int, grad: bool = True) -> int:
+    return int(lib().lowra_vocab_loss_workspace_bytes(int(M), int(V), int(K), int(bool(grad))))
+
+
+def lowra_vocab_loss(h, W, targets, weights=None, grad: bool = True, loss=None, lse=None, dH=None, workspace=None):
+    """Cross entropy of h [M,K] bf16 through the frozen head W [V,K] bf16 against targets [M] int32 (outside 0..V-1: no target, loss 0) ->
+    (loss fp32 [M], lse fp32 [M], dH bf16 [M,K]): dH is the gradient of the sum of weights loss with respect to h (weights: [M] fp32, None: ones), None
+    without `grad`."""
+    M, K = _rows(h, "h")
+    V, _ = _rows(W, "W")
+    device = h.device
+    _here(device, W, _dev(targets, torch.int32, "targets"))
+    if W.shape[1] != K or tuple(targets.shape) != (M,):
+        raise ValueError("shape mismatch")
+    _typed(weights, torch.float32, (M,), "weights", device)
+    loss = torch.empty(M, dtype=torch.float32, device=device) if loss is None else loss
+    lse = torch.empty(M, dtype=torch.float32, device=device) if lse is None else lse
+    _typed(loss, torch.float32, (M,), "loss", device); _typed(lse, torch.float32, (M,), "lse", device)
+    if dH is None and grad:
+        dH = torch.empty_like(h)
+    _operand(dH, (M, K), "dH", device)
+    if workspace is None:
+        workspace = torch.empty(lowra_vocab_loss_workspace_bytes(M, V, K, dH is not None), dtype=torch.uint8, device=device)
+    _here(device, _dev(workspace, torch.uint8, "workspace"))
+    _check(lib().lowra_vocab_loss(M, V, K, _ptr(h), _ptr(W), _ptr(targets), _ptr(weights), _ptr(loss), _ptr(lse), _ptr(dH), _ptr(workspace), workspace.numel(),
+                                  _stream()), "lowra_vocab_loss")
+    return loss, lse, dH
+
+
+@dataclasses.dataclass
+class AdamWItem:
+    """One tensor of an AdamWBatch: grad and weight fp32 device tensors of any one shape; m and v fp32 (32-bit states), or m int8 and v uint8 with
+    m_absmax and v_absmax fp32 [ceil(elements / 64)] (8-bit states).  The outputs are the tensors themselves where they are not given (in place); weight_bf16: a
+    bf16 copy of the new weights."""
+    grad: torch.Tensor
+    m: torch.Tensor
+    v: torch.Tensor
+    weight: torch.Tensor
+    m_absmax: torch.Tensor | None = None
+    v_absmax: torch.Tensor | None = None
+    weight_bf16: torch.Tensor | None = None
+    lr_scale: float = 1.0
+    decay_scale: float = 1.0
+    m_out: torch.Tensor | None = None
+    v_out: torch.Tensor | None = None
+    m_absmax_out: torch.Tensor | None = None
+    v_absmax_out: torch.Tensor | None = None
+    weight_out: torch.Tensor | None = None
+
+
+class AdamWBatch:
+    """The AdamW step on a list of AdamWItem (lowra_adamw_batch_*).  Every tensor is kept alive by the object: the library holds their addresses."""
+
+    def __init__(self, items):
+        self.handle = C.c_void_p()
+        if not items:
+            raise ValueError("empty batch")
+        self.device = device = items[0].grad.device
+        arr = (AdamWItemRecord * len(items))()
+        self._keep = []
+        for i, it in enumerate(items):
+            count, shape = it.grad.numel(), it.grad.shape
+            eight = it.m.dtype is torch.int8
+            groups = torch.Size([(count + 63) // 64])
+            own = lambda name: getattr(it, name) if getattr(it, name + "_out") is None else getattr(it, name + "_out")
+            fields = [("grad", it.grad, torch.float32, shape), ("m", it.m, torch.int8 if eight else torch.float32, shape),
+                      ("v", it.v, torch.uint8 if eight else torch.float32, shape), ("m_absmax", it.m_absmax, torch.float32, groups),
+                      ("v_absmax", it.v_absmax, torch.float32, groups), ("weight", it.weight, torch.float32, shape)]
+            fields += [(n + "_out", own(n), *next(f[2:] for f in fields if f[0] == n)) for n in ("m", "v", "m_absmax", "v_absmax", "weight")]
+            fields.append(("weight_bf16", it.weight_bf16, torch.bfloat16, shape))
+            for name, t, dtype, want in fields:
+                if t is None and (name == "weight_bf16" or ("absmax" in name and not eight)):
+                    continue
+                _dev(t, dtype, name)
+                if t.shape != want or t.device != device:
+                    raise ValueError(f"item {i}: {name}: shape or device mismatch")
+            if not eight and any(t is not None for name, t, _, _ in fields if "absmax" in name):
+                raise ValueError(f"item {i}: absmax with 32-bit states")
+            by = {name: _ptr(t) for name, t, _, _ in fields}
+            arr[i] = AdamWItemRecord(count=count, state_bits=8 if eight else 32, lr_scale=float(it.lr_scale), decay_scale=float(it.decay_scale), **by)
+            self._keep += [t for _, t, _, _ in fields]
+        _here(device)
+        _check(lib().lowra_adamw_batch_create(len(items), C.addressof(arr), C.addressof(self.handle)), "lowra_adamw_batch_create")
+
+    def run(self, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, step: int = 1, grad_scale=None):
+        """One step, number `step` from 1; grad_scale: a device tensor of one fp32, a factor of all gradients."""
+        if grad_scale is not None:
+            _here(self.device, _dev(grad_scale, torch.float32, "grad_scale"))
+            if grad_scale.numel() != 1:
+                raise ValueError("grad_scale: need one element")
+        s = AdamWStep(lr, betas[0], betas[1], eps, weight_decay, step)
+        _check(lib().lowra_adamw_batch_run(self.handle, C.addressof(s), _ptr(grad_scale), _stream()), "lowra_adamw_batch_run")
+
+    def close(self):
+        if self.handle:
+            lib().lowra_adamw_batch_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def lowra_adamw_state(codes, absmax, out=None):
+    """What 8-bit states of an AdamWItem stand for: codes int8 (m) or uint8 (v) of any shape, absmax fp32 [ceil(elements / 64)] -> fp32 of that shape."""
+    if codes.dtype not in (torch.int8, torch.uint8):
+        raise TypeError("codes: need int8 or uint8")
+    _here(codes.device, _dev(codes, codes.dtype, "codes"))
+    _typed(absmax, torch.float32, ((codes.numel() + 63) // 64,), "absmax", codes.device)
+    if out is None:
+        out = torch.empty(codes.shape, dtype=torch.float32, device=codes.device)
+    _typed(out, torch.float32, tuple(codes.shape), "out", codes.device)
+    _check(lib().lowra_adamw_state(codes.numel(), int(codes.dtype is torch.int8), _ptr(codes), _ptr(absmax), _ptr(out), _stream()), "lowra_adamw_state")
+    return out
 
 
 def lowra_channel_mse(W, thresholds3, mappings3):

@@ -1,0 +1,233 @@
+"""Layer and root-mean-square norm, forward and backward, against their formulas in 64 bits."""
+import pytest
+import torch
+
+from paper_2502_08141_amd import lowra
+
+pytestmark = pytest.mark.gpu
+
+LAYER, RMS = lowra.NORM_LAYER, lowra.NORM_RMS
+EPS = 1e-5
+
+
+def f32(v):
+    return float(torch.tensor(v, dtype=torch.float32))
+
+
+def inputs(M, N, seed=0, shift=0.25, std=1.0):
+    g = torch.Generator().manual_seed(seed * 1000003 + M * 131 + N)
+    r = lambda *s, k=1.0: (torch.randn(*s, generator=g) * k)
+    return {"x": (r(M, N, k=std) + shift).bfloat16(), "dY": r(M, N).bfloat16(), "weight": (1 + 0.2 * r(N)).bfloat16(), "bias": r(N, k=0.5).bfloat16(),
+            "residual": r(M, N).bfloat16()}
+
+
+def formulas(i, kind, weight, bias, residual, eps=EPS):
+    x, eps = i["x"].double(), f32(eps)
+    N = x.shape[1]
+    d = x - x.mean(1, keepdim=True) if kind == LAYER else x
+    rstd = 1 / torch.sqrt((d * d).mean(1, keepdim=True) + eps)
+    xh = d * rstd
+    w = i["weight"].double() if weight else torch.ones(N, dtype=torch.float64)
+    b = i["bias"].double() if bias else torch.zeros(N, dtype=torch.float64)
+    dY = i["dY"].double()
+    g = dY * w
+    dX = g - xh * (g * xh).mean(1, keepdim=True)
+    dX = rstd * (dX - g.mean(1, keepdim=True) if kind == LAYER else dX)
+    if residual:
+        dX = dX + i["residual"].double()
+    return {"y": xh * w + b, "dX": dX, "dweight": (dY * xh).sum(0), "dbias": dY.sum(0), "xh": xh, "rstd": rstd, "g": g, "d": d}
+
+
+# Sums of a row: a thread adds at most 64 terms one after another and the rest in a tree of at most ten, a product's rounding before: 75 x 2^-24
+# of the sum of the terms' magnitudes at worst, below 2^-17.  The mean is then off by 2^-17 of mean |x|, and with it every deviation; rstd by half of
+# the relative error of the sum of squares and of that shift.
+def tolerances(i, f, kind, M):
+    x = i["x"].double()
+    e = 2.0 ** -17
+    shift = e * x.abs().mean(1, keepdim=True) if kind == LAYER else 0.0 * x[:, :1]
+    xh = f["xh"]
+    rel = e + shift * f["rstd"] * xh.abs().mean(1, keepdim=True) + shift ** 2 * f["rstd"] ** 2      # of rstd
+    off_xh = xh.abs() * (rel + 2.0 ** -22) + shift * f["rstd"]
+    w = (f["g"] / torch.where(i["dY"].double() == 0, 1.0, i["dY"].double())).abs()
+    g = f["g"].abs()
+    gm, gx = g.mean(1, keepdim=True), (g * xh.abs()).mean(1, keepdim=True)
+    along = (f["g"] * xh).mean(1, keepdim=True).abs()
+    off_dX = f["rstd"] * (e * gm + xh.abs() * (e * gx + (g * off_xh).mean(1, keepdim=True)) + along * off_xh + (rel + 2.0 ** -21) * (g + gm + xh.abs() * along))
+    # down the tokens: one addition a row and workgroup, then the workgroups' in groups
+    off_dw = (i["dY"].double().abs() * off_xh).sum(0) + (M + 80) * 2.0 ** -24 * (i["dY"].double() * xh).abs().sum(0)
+    off_db = (M + 80) * 2.0 ** -24 * i["dY"].double().abs().sum(0)
+    return {"xh": off_xh, "dX": off_dX, "dweight": off_dw, "dbias": off_db, "w": w}
+
+
+def near(got, ref, off, what, half_step=0.0):
+    got = got.double().cpu()
+    bad = ~((got - ref).abs() <= ref.abs() * half_step * (1 + half_step) + off * (1 + half_step) + 1e-38)
+    assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[:3].tolist(), got[bad][:3].tolist(), ref[bad][:3].tolist())
+
+
+SIZES = [(1, 8), (3, 64), (5, 504), (4, 512), (7, 520), (9, 1024), (2, 1032), (6, 2048), (5, 2056), (3, 4096), (2, 5120), (2, 8192), (2, 8200), (2, 16376),
+         (2, 16384), (333, 1024), (777, 128), (2100, 72), (1500, 4096)]
+
+
+@pytest.mark.parametrize("M,N", SIZES)
+@pytest.mark.parametrize("kind", [LAYER, RMS])
+def test_forward(M, N, kind):
+    i = inputs(M, N)
+    for weight, bias in ((True, False), (True, True), (False, False), (False, True)):
+        f = formulas(i, kind, weight, bias, False)
+        t = tolerances(i, f, kind, M)
+        y = lowra.lowra_norm_fwd(i["x"].cuda(), i["weight"].cuda() if weight else None, i["bias"].cuda() if bias else None, kind, EPS)
+        w = i["weight"].double().abs() if weight else 1.0
+        near(y, f["y"], t["xh"] * w + 2.0 ** -22 * (f["xh"].abs() * w + f["y"].abs()), "y", 2.0 ** -8)
+
+
+@pytest.mark.parametrize("M,N", SIZES)
+@pytest.mark.parametrize("kind", [LAYER, RMS])
+def test_backward(M, N, kind):
+    i = inputs(M, N, 1)
+    c = {k: v.cuda() for k, v in i.items()}
+    for weight, residual in ((True, True), (True, False), (False, True)):
+        f = formulas(i, kind, weight, False, residual)
+        t = tolerances(i, f, kind, M)
+        dX, dw, db = lowra.lowra_norm_bwd(c["dY"], c["x"], c["weight"] if weight else None, kind, EPS, residual=c["residual"] if residual else None,
+                                          weight_grad=True, bias_grad=True)
+        near(dX, f["dX"], t["dX"] + 2.0 ** -22 * f["dX"].abs(), "dX", 2.0 ** -8)
+        near(dw, f["dweight"], t["dweight"], "dweight")
+        near(db, f["dbias"], t["dbias"], "dbias")
+
+
+def test_against_autograd_and_differences():
+    """The formulas that the other tests use are torch's gradient, and that of differences."""
+    i = inputs(6, 40, 2)
+    for kind in (LAYER, RMS):
+        f = formulas(i, kind, True, True, False)
+        def fwd(x, w, b):
+            d = x - x.mean(1, keepdim=True) if kind == LAYER else x
+            return d / torch.sqrt((d * d).mean(1, keepdim=True) + f32(EPS)) * w + b
+        args = [i[n].double().requires_grad_() for n in ("x", "weight", "bias")]
+        got = torch.autograd.grad(fwd(*args), args, i["dY"].double())
+        for a, n in zip(got, ("dX", "dweight", "dbias")):
+            assert torch.allclose(a, f[n], rtol=1e-10, atol=1e-12)
+        dX = lowra.lowra_norm_bwd(i["dY"].cuda(), i["x"].cuda(), i["weight"].cuda(), kind, EPS)[0].double().cpu()
+        h = 1e-5
+        for m, n in ((0, 0), (3, 17), (5, 39)):
+            step = torch.zeros_like(args[0])
+            step[m, n] = h
+            w, b = i["weight"].double(), i["bias"].double()
+            slope = ((fwd(i["x"].double() + step, w, b) - fwd(i["x"].double() - step, w, b)) * i["dY"].double()).sum() / (2 * h)
+            assert abs(float(slope - dX[m, n])) <= 2.0 ** -8 * abs(float(slope)) + 1e-6
+
+
+@pytest.mark.parametrize("kind", [LAYER, RMS])
+def test_what_is_asked_for(kind):
+    """Each output alone has the bits that it has beside the others; buffers are the caller's."""
+    i = {k: v.cuda() for k, v in inputs(70, 1032, 3).items()}
+    full = lowra.lowra_norm_bwd(i["dY"], i["x"], i["weight"], kind, EPS, residual=i["residual"], weight_grad=True, bias_grad=True)
+    dX, dw, db = lowra.lowra_norm_bwd(i["dY"], i["x"], i["weight"], kind, EPS, residual=i["residual"])
+    assert dw is None and db is None and torch.equal(dX, full[0])
+    dX, dw, db = lowra.lowra_norm_bwd(i["dY"], i["x"], i["weight"], kind, EPS, input_grad=False, weight_grad=True)
+    assert dX is None and db is None and torch.equal(dw, full[1])
+    dX, dw, db = lowra.lowra_norm_bwd(i["dY"], i["x"], i["weight"], kind, EPS, input_grad=False, bias_grad=True)
+    assert dX is None and dw is None and torch.equal(db, full[2])
+    outs = [torch.full_like(t, float("nan")) for t in full]
+    ws = torch.full((lowra.lowra_norm_bwd_workspace_bytes(70, 1032) + 64,), 255, dtype=torch.uint8, device="cuda")
+    got = lowra.lowra_norm_bwd(i["dY"], i["x"], i["weight"], kind, EPS, residual=i["residual"], dX=outs[0], dweight=outs[1], dbias=outs[2], workspace=ws)
+    assert all(a is b and torch.equal(a, c) for a, b, c in zip(got, outs, full))
+    assert bool((ws[-64:] == 255).all())
+    res = i["residual"].clone()                                   # in place
+    assert torch.equal(lowra.lowra_norm_bwd(i["dY"], i["x"], i["weight"], kind, EPS, residual=res, dX=res)[0], full[0])
+    x = i["x"].clone()
+    y = lowra.lowra_norm_fwd(i["x"], i["weight"], i["bias"], kind, EPS)
+    assert lowra.lowra_norm_fwd(x, i["weight"], i["bias"], kind, EPS, y=x) is x and torch.equal(x, y)
+
+
+@pytest.mark.parametrize("N", [64, 1024, 4096])
+def test_rows_do_not_touch_each_other(N):
+    """Infinities and NaN stay in their row; rows of zeros and of one value; nothing before or behind the tensors is written."""
+    i = inputs(12, N, 4)
+    x = i["x"]
+    x[3, 5], x[4, 0], x[5, N - 1] = float("nan"), float("inf"), float("-inf")
+    x[6], x[7] = 0.0, 3.0
+    good = [0, 1, 2, 6, 7, 8, 9, 10, 11]
+    big = torch.full((14, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    for kind in (LAYER, RMS):
+        f = formulas(i, kind, True, True, False)
+        y = lowra.lowra_norm_fwd(x.cuda(), i["weight"].cuda(), i["bias"].cuda(), kind, EPS, y=big[1:13])
+        assert bool((big[0] == 7).all() and (big[13] == 7).all())
+        t = tolerances(i, f, kind, 12)
+        near(y[good], f["y"][good], (t["xh"] * i["weight"].double().abs() + 2.0 ** -22 * f["y"].abs())[good] + 2.0 ** -22, "y", 2.0 ** -8)
+        assert bool(y[3].isnan().all())
+        dX = lowra.lowra_norm_bwd(i["dY"].cuda(), x.cuda(), i["weight"].cuda(), kind, EPS)[0]
+        near(dX[good], f["dX"][good], t["dX"][good] + 2.0 ** -22 * f["dX"][good].abs(), "dX", 2.0 ** -8)
+        assert bool(dX[3].isnan().all())
+
+
+def test_large_mean_keeps_its_digits():
+    """Deviations are squared about the mean: a mean of 256 deviations costs the mean's own rounding only."""
+    i = inputs(8, 4096, 5, shift=256.0)
+    f = formulas(i, LAYER, True, False, False)
+    y = lowra.lowra_norm_fwd(i["x"].cuda(), i["weight"].cuda(), None, LAYER, EPS)
+    # the mean's sums: 2^-17 of 256 deviations at worst
+    near(y, f["y"], 2.0 ** -17 * 300 * f["rstd"] * i["weight"].double().abs() * (1 + f["xh"].abs()) , "y", 2.0 ** -8)
+
+
+def test_no_tokens():
+    e = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    assert lowra.lowra_norm_fwd(e).shape == (0, 64)
+    dX, dw, db = lowra.lowra_norm_bwd(e, e, weight_grad=True, bias_grad=True, dweight=torch.ones(64, device="cuda"), dbias=torch.ones(64, device="cuda"))
+    assert dX.shape == (0, 64) and not dw.any() and not db.any()
+
+
+def test_streams_and_graphs():
+    """On a stream of its own, and captured and replayed with new inputs, against the eager calls."""
+    a, b = ({k: v.cuda() for k, v in inputs(300, 4096, s).items()} for s in (6, 7))
+    def call(i):
+        return [lowra.lowra_norm_fwd(i["x"], i["weight"], i["bias"]),
+                *lowra.lowra_norm_bwd(i["dY"], i["x"], i["weight"], residual=i["residual"], weight_grad=True, bias_grad=True, workspace=ws)]
+    ws = torch.empty(lowra.lowra_norm_bwd_workspace_bytes(300, 4096), dtype=torch.uint8, device="cuda")
+    want = {n: [t.clone() for t in call(i)] for n, i in (("a", a), ("b", b))}
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = call(a)
+    s.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want["a"]))
+    live = {k: v.clone() for k, v in a.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call(live)
+    for n, i in (("a", a), ("b", b), ("a", a), ("b", b)):
+        for k, v in live.items():
+            v.copy_(i[k])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(out, want[n]))
+        call(b)                                                   # eager work between the replays
+
+
+def test_binding_refusals():
+    i = {k: v.cuda() for k, v in inputs(4, 64, 8).items()}
+    with pytest.raises(TypeError):
+        lowra.lowra_norm_fwd(i["x"].float())
+    with pytest.raises(TypeError):
+        lowra.lowra_norm_fwd(i["x"].T)
+    with pytest.raises(ValueError):
+        lowra.lowra_norm_fwd(i["x"], i["weight"][:32])
+    with pytest.raises(ValueError):
+        lowra.lowra_norm_bwd(i["dY"], i["x"][:2])
+    with pytest.raises(ValueError):
+        lowra.lowra_norm_bwd(i["dY"], i["x"], dweight=torch.empty(63, device="cuda"))
+    with pytest.raises(TypeError):
+        lowra.lowra_norm_bwd(i["dY"], i["x"], dweight=torch.empty(64, device="cuda", dtype=torch.bfloat16))
+    for call in (lambda: lowra.lowra_norm_fwd(i["x"], kind=2),
+                 lambda: lowra.lowra_norm_bwd(i["dY"], i["x"], dX=i["dY"]), lambda: lowra.lowra_norm_bwd(i["dY"], i["x"], dX=i["x"]),
+                 lambda: lowra.lowra_norm_bwd(i["dY"], i["x"], input_grad=False)):
+        with pytest.raises(lowra.LowraError) as e:
+            call()
+        assert e.value.status == lowra.INVALID_ARG
+    with pytest.raises(lowra.LowraError) as e:
+        lowra.lowra_norm_bwd(i["dY"], i["x"], weight_grad=True, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == lowra.WORKSPACE_TOO_SMALL
+    with pytest.raises(lowra.LowraError) as e:
+        lowra.lowra_norm_fwd(torch.zeros(2, 12, dtype=torch.bfloat16, device="cuda"))
+    assert e.value.status == lowra.UNSUPPORTED
