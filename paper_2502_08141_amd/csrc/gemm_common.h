@@ -183,6 +183,10 @@ __device__ __forceinline__ void dma16_b(bufdesc_t desc, uint32_t voff, uint32_t 
     asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
                  : : "v"(voff), "s"(desc), "s"(soff), "s"(lds_base_uniform) : "memory");
 }
+__device__ __forceinline__ void dma4_b(bufdesc_t desc, uint32_t voff, uint32_t lds_base_uniform) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds"
+                 : : "v"(voff), "s"(desc), "s"(lds_base_uniform) : "memory");
+}
 __device__ __forceinline__ void dma_wait_all() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
 // 8 one-bit codes (low byte of c) -> 8 bf16 through the byte table Q = [lo0, lo1, hi0, hi1]

@@ -1,12 +1,17 @@
 // Softmax cross entropy over a vocabulary and its gradient, without the logits in memory (the loss of the paper's fine-tuning runs, Sec. 2.1):
 //   z = h W^T;   loss = log(sum_v exp z_v) - z_t;   dH = w (softmax(z) - e_t) W
 //
-// Two matrix products.  The first forms a tile of 256 words x 256 tokens of z in fp32 registers and leaves of it what does not depend on the
-// other words: per token the tile's largest z, the sum of exp(z - largest) over the words but the target, z_t where the tile has it, and, for the gradient,
-// the exponentials themselves in bf16 (the target's as zero).  A pass over these statistics gives loss and lse; another one
-// turns the exponentials into probabilities times the token's weight, where they lie; the second product multiplies them with W.
-// The target's own term, (p_t - 1) W_t, is added in fp32: p_t is near one for most tokens of a trained model, and its rounding would be the
-// gradient's error.  p_t - 1 and the loss come from the sum without the target, so that they keep their digits there.
+// Two matrix products and two small passes.  The first product forms a tile of 256 words x 256 tokens of z in fp32 registers and leaves of it what
+// does not depend on the other words: per token a whole number n not far from log2 e times the tile's largest z, the sum of 2^(z log2 e - n) over the words but
+// the target, z_t where the tile has it, and, for the gradient, the exponentials themselves in bf16 (the target's as zero).  fp32 and bf16 reach from
+// 2^-126 to 2^127, so n is zero where the largest is between 2^-32 and 2^64 (z from -22 to 44) and the multiple of 64 below elsewhere; what is less
+// than 2^-94 of the largest may be lost.  A pass over these numbers gives loss and lse, and
+// how far each tile's n is below the token's largest.  The second product multiplies the exponentials with W.  Where tiles of a token differ in n,
+// it brings them to the token's scale on the way into the matrix unit, a subtraction from their exponents and exact; for tokens whose n are all the same
+// it has a loop without (4096 x 32000 x 4096: 895 us with the subtraction, 818 without; a pass over the exponentials before it 90).  The token's factor
+// weight / sum meets the fp32 sums.  So a probability is rounded once, to bf16.  The target's own term, weight (p_t - 1) W_t, is added in fp32: p_t is near
+// one for most tokens of a trained model, and its rounding would be the gradient's error.  p_t - 1 and the loss come from the sum without the target, so
+// that they keep their digits there.
 // Tokens go in pieces whose exponentials fit kLossPiece bytes, so that neither the logits nor anything else of size M x V is ever there at once.
 // (Pieces of the vocabulary would have to form z a second time for the gradient: 6 M V K operations in place of 4.)
 #include <algorithm>
@@ -18,14 +23,16 @@ namespace lowra {
 
 namespace {
 
-constexpr int TILE = 256, DEPTH = 64, THREADS = 512;
-constexpr int OPB = TILE * DEPTH * 2;                    // one operand of a step: 32 KB
-constexpr int SMEM = 4 * OPB;                            // two stages of both
+constexpr int THREADS = 512, WAVES = 8, DEPTH = 64;      // a step of either product: 64 features or words
 typedef short v4i16_t __attribute__((ext_vector_type(4)));
+typedef short v8i16_t __attribute__((ext_vector_type(8)));
+typedef unsigned short v2u16_t __attribute__((ext_vector_type(2)));
+typedef unsigned short v8u16_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) v4i16_t* lds_v4i16_ptr;
 
-constexpr float kLeast = -2e38f;                         // below every z that counts; times log2 e still finite, so that exp(-inf - kLeast) is zero
-struct LossStat { float most, sum; };                    // of a tile's words, the target aside in the sum
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLeast = -2e38f;                         // below every z that counts; times log2 e still finite, so that 2^(-inf - it) is zero
+struct LossStat { float shift, sum; };                   // of a tile's words: n, and the sum with the target aside
 
 struct LossParams {
     const uint16_t *h, *W;
@@ -33,305 +40,401 @@ struct LossParams {
     const float* weights;
     float *loss, *lse;
     uint16_t* dH;
-    int M, V, K, VP, tiles;                              // this piece's tokens; VP: words in whole tiles
-    LossStat* stats;                                     // [M][tiles]
+    int M, V, K, VP, tiles, tile_shift;                  // this piece's tokens; VP: words in whole tiles of 2^tile_shift
+    LossStat* stats;                                     // [tiles][M]
     float* zt;                                           // [M]
-    float2* rows;                                        // [M]: lse, weight (p_t - 1)
+    uint32_t* drop;                                      // [tiles][M]: exponents below the token's scale, as both halves' bits
+    uint32_t* uneven;                                    // [M / 64]: some token of these has such a tile
+    float2* rows;                                        // [M]: weight / sum, weight (p_t - 1)
     uint16_t* P;                                         // [M][VP]
     float* part;                                         // [splits][M][K]
     int splits, words_per_split;
 };
 
-// ---- first product: 256 words (operand A) x 256 tokens (operand B) a workgroup; wavefront (wv, wt) has 128 words x 64 tokens
-__global__ __launch_bounds__(THREADS) void loss_logits_kernel(LossParams p) {
-    extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ float join[2][TILE];
-    const uint32_t smem_lds = (uint32_t)(uintptr_t)(lptr_t)smem;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tile = xcd_tile(blockIdx.x, gridDim.x), tiles_m = (p.M + TILE - 1) / TILE;
-    const int mt = tile % tiles_m, vt = tile / tiles_m, m0 = mt * TILE, v0 = vt * TILE;      // workgroups of an L2 share words
-    const int steps = (p.K + DEPTH - 1) / DEPTH;
-    // transfers: wavefronts 0..3 bring the words' rows, 4..7 the tokens'; each 8 times 8 rows of 128 bytes
-    const bool tok = wave >= 4;
-    const int first_row = (wave & 3) * 64, last = (tok ? p.M - m0 : p.V - v0) - 1;
-    const bufdesc_t src = buffer_desc(tok ? p.h + (size_t)m0 * p.K : p.W + (size_t)v0 * p.K);
-    uint32_t voff[8];
-    int chunk[8];
+// The tile of a workgroup: runs of `group` tiles of one operand against all of the other, so that the workgroups of an L2 share both (4096 x 32768 x
+// 4096: 880 us; one operand's tiles all against two of the other's 955).
+__device__ __forceinline__ void tile_of(int tile, int major, int minor, int group, int& a, int& b) {
+    const int g = tile / (group * minor), r = tile - g * group * minor, n = min(group, major - g * group);
+    a = g * group + r % n;
+    b = r / n;
+}
+
+template <int N>
+__device__ __forceinline__ void wait_transfers() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+
+// The steps of a product.  A step's operands are two tiles of one of STAGES stages in LDS.  fetch(s, i) asks for transfer i of T of step s (of which some steps may leave
+// out all but WT); read(s, kk, i)
+// for operand registers i of R of slice kk (16 deep) of step s; mul(kk, j) is matrix instruction j of N of a slice.  The only barrier of a step stands before its last
+// slice, when that slice's operands are in registers: the stage is free from there on for step s + STAGES, whose transfers are dealt over two slices (back to back
+// they hold up the issue: 900 -> 850 us), and step s + 1 is there, so that its first operands are read under the last slice's products.
+template <int STAGES, int T, int WT, int R, int N, class Fetch, class Read, class Mul>
+__device__ __forceinline__ void product_steps(int steps, Fetch fetch, Read read, Mul mul) {
+    constexpr int H = (T + 1) / 2;                       // transfers in the first of the two slices
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = first_row + 8 * i + (lane >> 3);
-        chunk[i] = (lane & 7) ^ ((r >> 1) & 7);
-        voff[i] = (uint32_t)min(r, last) * (uint32_t)p.K * 2u + (uint32_t)chunk[i] * 16u;
-    }
-    auto fetch = [&](int s) __attribute__((always_inline)) {
-        const uint32_t dst = smem_lds + (uint32_t)(s & 1) * (2 * OPB) + (tok ? OPB : 0) + (uint32_t)first_row * ROWB;
-        if ((s + 1) * DEPTH <= p.K) {
+    for (int s = 0; s < STAGES; ++s)
+        if (s < steps) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dma16_b(src, voff[i], (uint32_t)s * (DEPTH * 2u), dst + i * 1024u);
-        } else {                                         // the features past K come as zeros
-#pragma unroll
-            for (int i = 0; i < 8; ++i) dma16_b(src, s * DEPTH + 8 * chunk[i] < p.K ? voff[i] : 0x80000000u, (uint32_t)s * (DEPTH * 2u), dst + i * 1024u);
+            for (int i = 0; i < T; ++i) fetch(s, i);
         }
-    };
-    const int wv = wave >> 2, wt = wave & 3, fi = lane & 31, half = lane >> 5, fsw = (fi >> 1) & 7;
-    floatx16_t acc[4][2];
+    if (steps >= STAGES) wait_transfers<WT * (STAGES - 1)>();
+    else wait_transfers<0>();
+    asm volatile("s_barrier" : : : "memory");
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
-    fetch(0);
+    for (int i = 0; i < R; ++i) read(0, 0, i);
     for (int s = 0; s < steps; ++s) {
-        dma_wait_all();
-        __syncthreads();                                 // step s is there, and the last readers of the other stage are done
-        if (s + 1 < steps) fetch(s + 1);
-        const uint8_t* st = smem + (s & 1) * (2 * OPB);
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
-            const int koff = ((2 * kk + half) ^ fsw) << 4;
-            bf16x8_t fa[4], fb[2];
+            if (kk == 3) {
+                if (STAGES > 2 && s + STAGES - 1 < steps) wait_transfers<WT * (STAGES - 2)>();
+                else wait_transfers<0>();
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+                __builtin_amdgcn_s_setprio(1);
+            }
+            if (kk == 1) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-            for (int a = 0; a < 4; ++a) fa[a] = *reinterpret_cast<const bf16x8_t*>(st + (wv * 128 + a * 32 + fi) * ROWB + koff);
+            for (int j = 0; j < N; ++j) {
+                mul(kk, j);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) fb[b] = *reinterpret_cast<const bf16x8_t*>(st + OPB + (wt * 64 + b * 32 + fi) * ROWB + koff);
+                for (int i = j * R / N; i < (j + 1) * R / N; ++i) {
+                    if (kk < 3) read(s, kk + 1, i);
+                    else read(s + 1, 0, i);              // (past the last step: registers that nothing uses)
+                }
+                if (kk == 3 && s + STAGES < steps) {
 #pragma unroll
-            for (int a = 0; a < 4; ++a)
+                    for (int i = j * H / N; i < (j + 1) * H / N; ++i) fetch(s + STAGES, i);
+                }
+                if (kk == 0 && s > 0 && s + STAGES - 1 < steps) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[a], fb[b], acc[a][b], 0, 0, 0);
+                    for (int i = j * (T - H) / N; i < (j + 1) * (T - H) / N; ++i) fetch(s + STAGES - 1, H + i);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     }
-    // accumulator v of tile (a, b): word wv 128 + 32 a + 8 (v / 4) + 4 half + v % 4, token wt 64 + 32 b + fi
-    const int words = p.V - v0;
-    float most[2];
-    int target[2];
+}
+
+// ---- first product.  Words are the matrix instruction's rows, tokens its columns, so that a token's words lie in one lane and its other half: WV x (8 / WV)
+// wavefronts, each with AT x BT tiles of 32 words x 32 tokens.
+template <int WV, int AT, int BT, int STAGES>
+struct Logits {
+    static constexpr int WORDS = WV * AT * 32, TOKENS = WAVES / WV * BT * 32, STAGE = (WORDS + TOKENS) * ROWB, SMEM = STAGES * STAGE;
+    static_assert(TOKENS * WORDS * 2 <= SMEM, "the exponentials of a tile");
+};
+template <int WV, int AT, int BT, int STAGES>
+__global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
+    using S = Logits<WV, AT, BT, STAGES>;
+    constexpr int WORDS = S::WORDS, TOKENS = S::TOKENS, TW = WORDS / 64, TT = TOKENS / 64;       // transfers of a wavefront: eight rows each
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ float join[WV][TOKENS];
+    const uint32_t smem_lds = (uint32_t)(uintptr_t)(lptr_t)smem;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int vt, mt;
+    tile_of(xcd_tile(blockIdx.x, gridDim.x), p.tiles, (p.M + TOKENS - 1) / TOKENS, 8, vt, mt);
+    const int m0 = mt * TOKENS, v0 = vt * WORDS, steps = (p.K + DEPTH - 1) / DEPTH;
+    const bufdesc_t src_w = buffer_desc(p.W + (size_t)v0 * p.K), src_h = buffer_desc(p.h + (size_t)m0 * p.K);
+    uint32_t off_w[TW], off_h[TT];                       // rows past the end: the last one again
+    auto offset = [&](int r, int last) __attribute__((always_inline)) { return (uint32_t)min(r, last) * (uint32_t)p.K * 2u + (uint32_t)((lane & 7) ^ ((r >> 1) & 7)) * 16u; };
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int t = wt * 64 + b * 32 + fi;
-        target[b] = m0 + t < p.M ? (int)((uint32_t)p.targets[m0 + t] - (uint32_t)v0) : -1;
-        most[b] = kLeast;
+    for (int i = 0; i < TW; ++i) off_w[i] = offset(wave * (8 * TW) + 8 * i + (lane >> 3), p.V - v0 - 1);
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
+    for (int i = 0; i < TT; ++i) off_h[i] = offset(wave * (8 * TT) + 8 * i + (lane >> 3), p.M - m0 - 1);
+    // lanes of the last step whose features lie past K get zeros; a row's chunk order depends on bit 3 of its number
+    uint32_t past[2];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int word = wv * 128 + a * 32 + 8 * (v >> 2) + 4 * half + (v & 3);
-                if (word < words) most[b] = fmaxf(most[b], acc[a][b][v]);
-            }
-        most[b] = fmaxf(most[b], __shfl_xor(most[b], 32));
-        if (half == 0) join[wv][t] = most[b];
+    for (int i = 0; i < 2; ++i) past[i] = (steps - 1) * DEPTH + 8 * ((lane & 7) ^ ((4 * i + (lane >> 4)) & 7)) < p.K ? 0u : 0x80000000u;
+    auto fetch = [&](int s, int i) __attribute__((always_inline)) {
+        const uint32_t stage = smem_lds + (uint32_t)(s % STAGES) * S::STAGE, soff = (uint32_t)s * (DEPTH * 2u), end = s == steps - 1 ? ~0u : 0u;
+        if (i < TW) dma16_b(src_w, off_w[i < TW ? i : 0] | (past[(wave * TW + i) & 1] & end), soff, stage + (uint32_t)(wave * TW + i) * 1024u);
+        else dma16_b(src_h, off_h[i < TW ? 0 : i - TW] | (past[(wave * TT + i - TW) & 1] & end), soff, stage + WORDS * ROWB + (uint32_t)(wave * TT + i - TW) * 1024u);
+    };
+    const int wv = wave / (WAVES / WV), wt = wave % (WAVES / WV), fi = lane & 31, half = lane >> 5;
+    int koff[4];
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) koff[kk] = ((2 * kk + half) ^ ((fi >> 1) & 7)) << 4;
+    const int a0 = (wv * AT * 32 + fi) * ROWB, b0 = WORDS * ROWB + (wt * BT * 32 + fi) * ROWB;
+    floatx16_t acc[AT][BT];
+#pragma unroll
+    for (int a = 0; a < AT; ++a)
+#pragma unroll
+        for (int b = 0; b < BT; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
+    bf16x8_t fa[2][AT], fb[2][BT];
+    product_steps<STAGES, TW + TT, TW + TT, AT + BT, AT * BT>(
+        steps, fetch,
+        [&](int s, int kk, int i) __attribute__((always_inline)) {
+            const uint8_t* st = smem + (s % STAGES) * S::STAGE + koff[kk];
+            if (i < AT) fa[kk & 1][i < AT ? i : 0] = *reinterpret_cast<const bf16x8_t*>(st + a0 + i * 32 * ROWB);
+            else fb[kk & 1][i < AT ? 0 : i - AT] = *reinterpret_cast<const bf16x8_t*>(st + b0 + (i - AT) * 32 * ROWB);
+        },
+        [&](int kk, int j) __attribute__((always_inline)) {
+            acc[j / BT][j % BT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[kk & 1][j / BT], fb[kk & 1][j % BT], acc[j / BT][j % BT], 0, 0, 0);
+        });
+    // accumulator v of tile (a, b): word wv 32 AT + 32 a + 8 (v / 4) + 4 half + v % 4, token wt 32 BT + 32 b + fi
+    const int words = p.V - v0, w0 = wv * AT * 32 + 4 * half, t0 = wt * BT * 32 + fi;
+    if (words < WORDS) {                                 // uniform: words past V
+#pragma unroll
+        for (int a = 0; a < AT; ++a)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (w0 + a * 32 + 8 * (v >> 2) + (v & 3) >= words) {
+#pragma unroll
+                    for (int b = 0; b < BT; ++b) acc[a][b][v] = -INFINITY;
+                }
+    }
+    float shift[BT], sum[BT];
+#pragma unroll
+    for (int b = 0; b < BT; ++b) {
+        float most = kLeast;
+#pragma unroll
+        for (int a = 0; a < AT; ++a)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) most = fmaxf(most, acc[a][b][v]);
+        most = fmaxf(most, __shfl_xor(most, 32));
+        if (half == 0) join[wv][t0 + 32 * b] = most;
+        // the target leaves the sum
+        const int m = m0 + t0 + 32 * b;
+        const uint32_t target = m < p.M ? (uint32_t)p.targets[m] : ~0u, mine = target < (uint32_t)p.V ? target - (uint32_t)(v0 + w0) : ~0u;
+        if (__any(mine < AT * 32)) {
+#pragma unroll
+            for (int a = 0; a < AT; ++a)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (mine == (uint32_t)(a * 32 + 8 * (v >> 2) + (v & 3))) {
+                        p.zt[m] = acc[a][b][v];
+                        acc[a][b][v] = -INFINITY;
+                    }
+        }
     }
     __syncthreads();
 #pragma unroll
-    for (int b = 0; b < 2; ++b) most[b] = fmaxf(join[0][wt * 64 + b * 32 + fi], join[1][wt * 64 + b * 32 + fi]);
+    for (int b = 0; b < BT; ++b) {
+        float most = join[0][t0 + 32 * b];
+#pragma unroll
+        for (int w = 1; w < WV; ++w) most = fmaxf(most, join[w][t0 + 32 * b]);
+        const float n = most * kLog2e;
+        shift[b] = n >= -32.0f && n <= 64.0f ? 0.0f : 64.0f * floorf(n * (1.0f / 64.0f));
+    }
     __syncthreads();
-    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int t = wt * 64 + b * 32 + fi;
+    for (int b = 0; b < BT; ++b) {
+        sum[b] = 0.0f;
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
+        for (int a = 0; a < AT; ++a)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const int word = wv * 128 + a * 32 + 8 * (v >> 2) + 4 * half + (v & 3);
-                const float z = acc[a][b][v];
-                float e = __builtin_amdgcn_exp2f((z - most[b]) * 1.4426950408889634f);      // (the difference first: its rounding does not grow with z)
-                if (word >= words || word == target[b]) e = 0.0f;
-                if (word == target[b] && word < words) p.zt[m0 + t] = z;
-                sum[b] += e;
-                acc[a][b][v] = e;
+                acc[a][b][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[a][b][v], kLog2e, -shift[b]));
+                sum[b] += acc[a][b][v];
             }
         sum[b] += __shfl_xor(sum[b], 32);
-        if (half == 0) join[wv][t] = sum[b];
+        if (half == 0) join[wv][t0 + 32 * b] = sum[b];
+    }
+    if (p.P) {                                           // the exponentials to LDS: a row a token, 16-byte chunks in another order for each of 32 tokens
+#pragma unroll
+        for (int b = 0; b < BT; ++b)
+#pragma unroll
+            for (int a = 0; a < AT; ++a)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = wv * AT * 4 + a * 4 + q;
+                    *reinterpret_cast<uint2*>(smem + (t0 + 32 * b) * (WORDS * 2) + ((c ^ (fi & (WORDS / 8 - 1))) << 4) + 8 * half) =
+                        make_uint2(pack_bf16x2(acc[a][b][4 * q], acc[a][b][4 * q + 1]), pack_bf16x2(acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]));
+                }
     }
     __syncthreads();
     if (wv == 0 && half == 0) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int t = wt * 64 + b * 32 + fi;
-            if (m0 + t < p.M) p.stats[(size_t)(m0 + t) * p.tiles + vt] = LossStat{most[b], join[0][t] + join[1][t]};
+        for (int b = 0; b < BT; ++b) {
+            const int t = t0 + 32 * b;
+            float s = join[0][t];
+#pragma unroll
+            for (int w = 1; w < WV; ++w) s += join[w][t];
+            if (m0 + t < p.M) p.stats[(size_t)vt * p.M + m0 + t] = LossStat{shift[b], s};
         }
     }
     if (!p.P) return;                                    // uniform
-    // the exponentials through LDS: rows of 512 bytes a token, 16-byte chunks in another order for each of 32 tokens
+    constexpr int CH = WORDS / 8;                        // chunks a row
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int t = wt * 64 + b * 32 + fi;
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = (wv * 128 + a * 32 + 8 * q) >> 3;
-                *reinterpret_cast<uint2*>(smem + t * 512 + ((c ^ fi) << 4) + 8 * half) =
-                    make_uint2(pack_bf16x2(acc[a][b][4 * q], acc[a][b][4 * q + 1]), pack_bf16x2(acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]));
-            }
+    for (int i = 0; i < TOKENS * CH / THREADS; ++i) {
+        const int t = i * (THREADS / CH) + tid / CH, c = tid % CH;
+        if (m0 + t < p.M) *reinterpret_cast<uint4*>(p.P + (size_t)(m0 + t) * p.VP + v0 + 8 * c) = *reinterpret_cast<const uint4*>(smem + t * (WORDS * 2) + ((c ^ (t & 31 & (CH - 1))) << 4));
     }
+}
+
+// ---- 64 tokens a workgroup, a lane each; the tiles dealt to sixteen wavefronts
+__global__ __launch_bounds__(1024) void loss_rows_kernel(LossParams p) {
+    __shared__ float join[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = blockIdx.x * 64 + lane, at = min(m, p.M - 1);
+    float most = kLeast * kLog2e;
+#pragma unroll 8
+    for (int i = wave; i < p.tiles; i += 16) most = fmaxf(most, p.stats[(size_t)i * p.M + at].shift);
+    join[wave][lane] = most;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < TILE * 32 / THREADS; ++i) {
-        const int t = i * (THREADS / 32) + (tid >> 5), c = tid & 31;
-        if (m0 + t < p.M) *reinterpret_cast<uint4*>(p.P + (size_t)(m0 + t) * p.VP + v0 + 8 * c) = *reinterpret_cast<const uint4*>(smem + t * 512 + ((c ^ (t & 31)) << 4));
+    for (int w = 0; w < 16; ++w) most = fmaxf(most, join[w][lane]);
+    __syncthreads();
+    float others = 0.0f;
+    bool uneven = false;
+#pragma unroll 8
+    for (int i = wave; i < p.tiles; i += 16) {
+        const LossStat st = p.stats[(size_t)i * p.M + at];
+        others += ldexpf(st.sum, (int)fmaxf(st.shift - most, -1000.0f));      // (2^-128 by itself is none in fp32)
+        // an exponential times 2^-d: bf16 has its exponent from bit 7 on, and 255 leaves nothing of any
+        uneven = uneven || st.shift != most;
+        if (p.drop && m < p.M) p.drop[(size_t)i * p.M + m] = ((uint32_t)fminf(most - st.shift, 255.0f) << 7) * 0x10001u;
     }
-}
-
-// ---- a wavefront a token: loss, lse and the target's factor
-__global__ __launch_bounds__(256) void loss_rows_kernel(LossParams p) {
-    const int m = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (m >= p.M) return;
-    const LossStat* st = p.stats + (size_t)m * p.tiles;
+    join[wave][lane] = others;
+    const int any = __syncthreads_or(uneven);
+    if (p.uneven && threadIdx.x == 0) p.uneven[blockIdx.x] = (uint32_t)(any != 0);
+    if (wave != 0 || m >= p.M) return;
+    for (int w = 1; w < 16; ++w) others += join[w][lane];
     const int t = p.targets[m];
     const bool there = t >= 0 && t < p.V;
-    const float zt = there ? p.zt[m] : kLeast;
-    float most = zt;
-    for (int i = lane; i < p.tiles; i += 64) most = fmaxf(most, st[i].most);
-    for (int s = 32; s; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
-    float others = 0.0f;
-    for (int i = lane; i < p.tiles; i += 64) others += st[i].sum * __builtin_amdgcn_exp2f((st[i].most - most) * 1.4426950408889634f);
-    for (int s = 32; s; s >>= 1) others += __shfl_xor(others, s);
-    if (lane != 0) return;
-    const float et = there ? expf(zt - most) : 0.0f, total = others + et;
-    const float log_total = zt == most ? log1pf(others) : logf(total);      // (e_t is one: by the others alone)
-    const float lse = most + log_total;
-    p.loss[m] = there ? (most - zt) + log_total : 0.0f;
-    if (p.lse) p.lse[m] = lse;
+    const float xt = there ? __builtin_fmaf(p.zt[m], kLog2e, -most) : -INFINITY, et = exp2f(xt), total = others + et, log_total = logf(total);
+    if (p.lse) p.lse[m] = __builtin_fmaf(most, kLn2, log_total);
+    const float ratio = others / et;                     // (past fp32 where the target is 2^-126 of the others)
+    p.loss[m] = !there ? 0.0f : ratio < 3e38f ? log1pf(ratio) : log_total - xt * kLn2;
     if (p.rows) {
         const float w = !there ? 0.0f : p.weights ? p.weights[m] : 1.0f;
-        p.rows[m] = make_float2(lse, there ? -w * (others / total) : 0.0f);
+        p.rows[m] = make_float2(w / total, -w * (others / total));
     }
 }
 
-// ---- the exponentials of a tile become weight times probability, where they lie; nothing for a token without a target, whatever it holds
-__global__ __launch_bounds__(256) void loss_scale_kernel(LossParams p) {
-    const int parts = (p.VP / 8 + 1023) / 1024, m = blockIdx.x / parts;
-    const int t = p.targets[m];
-    const bool there = t >= 0 && t < p.V;
-    const float w = !there ? 0.0f : p.weights ? p.weights[m] : 1.0f, lse = p.rows[m].x;
-    uint4* row = reinterpret_cast<uint4*>(p.P + (size_t)m * p.VP);
-    const int c0 = (blockIdx.x % parts) * 1024;
-    for (int c = c0 + threadIdx.x; c < min(c0 + 1024, p.VP / 8); c += 256) {
-        const float f = w * __builtin_amdgcn_exp2f((p.stats[(size_t)m * p.tiles + (c >> 5)].most - lse) * 1.4426950408889634f);
-        uint4 q = there ? row[c] : zero4();
-        uint32_t* u = reinterpret_cast<uint32_t*>(&q);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (there) u[i] = pack_bf16x2(bf16_bits_to_float(u[i] & 0xffffu) * f, __builtin_bit_cast(float, u[i] & 0xffff0000u) * f);
-        row[c] = q;
-    }
-}
-
-// ---- second product: 256 tokens (operand A: P) x 256 features (operand B: W, read across its rows) a workgroup, over a run of words
+// ---- second product, over a run of words: tokens (the exponentials) are the matrix instruction's rows, features its columns, W's operand read across its rows
+// (ds_read_b64_tr_b16).  2 x 4 wavefronts, each with AT x 2 tiles of 32 tokens x 32 features.
 __device__ __forceinline__ int wswz(int row, int c) { return row * 512 + ((c ^ (((row & 3) << 2) | ((row >> 2) & 3))) << 4); }
-__global__ __launch_bounds__(THREADS) void loss_grad_kernel(LossParams p) {
+template <int AT, int STAGES>
+struct Grad {
+    static constexpr int TOKENS = 2 * AT * 32, W0 = TOKENS * ROWB, D0 = W0 + DEPTH * 512, STAGE = D0 + TOKENS * 4, SMEM = STAGES * STAGE;      // tokens', words' rows, exponents
+};
+template <int AT, int STAGES>
+__global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
+    using S = Grad<AT, STAGES>;
+    constexpr int TOKENS = S::TOKENS, TP = TOKENS / 64, TW = 4;
     extern __shared__ __align__(16) uint8_t smem[];
     const uint32_t smem_lds = (uint32_t)(uintptr_t)(lptr_t)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tiles_k = (p.K + TILE - 1) / TILE, tiles_m = (p.M + TILE - 1) / TILE;
-    const int work = xcd_tile(blockIdx.x, gridDim.x), split = work / (tiles_k * tiles_m), tile = work % (tiles_k * tiles_m);
-    const int k0 = (tile % tiles_k) * TILE, m0 = (tile / tiles_k) * TILE;
-    const int w0 = split * p.words_per_split, w1 = min(w0 + p.words_per_split, p.VP);
-    const int steps = (w1 - w0) / DEPTH;
-    const bool tok = wave >= 4;
-    const int wq = wave & 3, last = p.M - 1 - m0;
-    const size_t step_bytes = tok ? DEPTH * 2 : (size_t)DEPTH * p.K * 2;
-    const uint8_t* base = tok ? reinterpret_cast<const uint8_t*>(p.P + (size_t)m0 * p.VP + w0) : reinterpret_cast<const uint8_t*>(p.W + (size_t)w0 * p.K + k0);
-    uint32_t voff[8];
-    int row[8];
+    const int tiles_k = (p.K + 255) / 256, tiles_m = (p.M + TOKENS - 1) / TOKENS;
+    const int work = xcd_tile(blockIdx.x, gridDim.x), split = __builtin_amdgcn_readfirstlane(work / (tiles_k * tiles_m));
+    int mt, kt;
+    tile_of(work - split * (tiles_k * tiles_m), tiles_m, tiles_k, 4, mt, kt);
+    const int k0 = kt * 256, m0 = mt * TOKENS, w0 = split * p.words_per_split, steps = (min(w0 + p.words_per_split, p.VP) - w0) / DEPTH;
+    const uint16_t* P = p.P + (size_t)m0 * p.VP + w0;
+    const uint16_t* W = p.W + (size_t)w0 * p.K + k0;
+    const bufdesc_t src_p = buffer_desc(P);
+    uint32_t off_p[TP], off_w[TW];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (tok) {                                       // 64 token rows of 128 bytes
-            row[i] = wq * 64 + 8 * i + (lane >> 3);
-            voff[i] = (uint32_t)min(row[i], last) * (uint32_t)p.VP * 2u + (uint32_t)((lane & 7) ^ ((row[i] >> 1) & 7)) * 16u;
-        } else {                                         // 16 words' rows of 512 bytes
-            row[i] = wq * 16 + 2 * i + (lane >> 5);
-            const int c = (lane & 31) ^ (((row[i] & 3) << 2) | ((row[i] >> 2) & 3));
-            voff[i] = k0 + 8 * c < p.K ? (uint32_t)row[i] * (uint32_t)p.K * 2u + (uint32_t)c * 16u : 0x80000000u;
-        }
+    for (int i = 0; i < TP; ++i) {                       // token rows of 128 bytes, eight a transfer
+        const int r = wave * (8 * TP) + 8 * i + (lane >> 3);
+        off_p[i] = (uint32_t)min(r, p.M - 1 - m0) * (uint32_t)p.VP * 2u + (uint32_t)((lane & 7) ^ ((r >> 1) & 7)) * 16u;
     }
-    auto fetch = [&](int s) __attribute__((always_inline)) {
-        const uint32_t dst = smem_lds + (uint32_t)(s & 1) * (2 * OPB) + (tok ? 0 : OPB) + (uint32_t)wq * 8192u;
-        const bufdesc_t src = buffer_desc(base + (size_t)s * step_bytes);
-        if (tok || w0 + (s + 1) * DEPTH <= p.V) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dma16_b(src, voff[i], 0, dst + i * 1024u);
-        } else {                                         // the words past V come as zeros
-#pragma unroll
-            for (int i = 0; i < 8; ++i) dma16_b(src, w0 + s * DEPTH + row[i] < p.V ? voff[i] : 0x80000000u, 0, dst + i * 1024u);
+    for (int i = 0; i < TW; ++i) {                       // words' rows of 512 bytes, two a transfer; features past K come as zeros
+        const int r = wave * 8 + 2 * i + (lane >> 5), c = (lane & 31) ^ (((r & 3) << 2) | ((r >> 2) & 3));
+        off_w[i] = k0 + 8 * c < p.K ? (uint32_t)r * (uint32_t)p.K * 2u + (uint32_t)c * 16u : 0x80000000u;
+    }
+    const uint32_t off_d = (uint32_t)min(m0 + wave * 64 + lane, p.M - 1) * 4u;
+    const int per = (1 << p.tile_shift) / DEPTH - 1;     // of a tile's steps the first has none of these bits
+    bool scaled = false;                                 // uniform
+    for (int i = m0 / 64; i <= (min(m0 + TOKENS, p.M) - 1) / 64; ++i) scaled = scaled || p.uneven[i] != 0;
+    scaled = __builtin_amdgcn_readfirstlane(scaled);
+    auto fetch = [&](int s, int i) __attribute__((always_inline)) {
+        const uint32_t stage = smem_lds + (uint32_t)(s % STAGES) * S::STAGE;
+        if (i == TP + TW) {                              // the exponents of a tile, with its first step (a transfer and four reads in every step: 818 -> 895 us)
+            if (scaled && wave < TP && (s & per) == 0)
+                dma4_b(buffer_desc(p.drop + (size_t)((w0 + s * DEPTH) >> p.tile_shift) * p.M), off_d, stage + S::D0 + (uint32_t)wave * 256u);
+        } else if (i < TP) dma16_b(src_p, off_p[i < TP ? i : 0], (uint32_t)s * (DEPTH * 2u), stage + (uint32_t)(wave * TP + i) * 1024u);
+        else {                                           // words past V come as zeros, too
+            const int r = wave * 8 + 2 * (i - TP) + (lane >> 5);
+            dma16_b(buffer_desc(W + (size_t)s * DEPTH * p.K), r < p.V - w0 - s * DEPTH ? off_w[i < TP ? 0 : i - TP] : 0x80000000u, 0, stage + S::W0 + (uint32_t)(wave * TW + i - TP) * 1024u);
         }
     };
-    const int wm = wave >> 2, wn = wave & 3, fi = lane & 31, half = lane >> 5, fsw = (fi >> 1) & 7;
-    int tr[2][2];                                        // lane -> (word 8 half + 4 e + L / 4, four features from 4 (L % 4))
+    const int wm = wave >> 2, wn = wave & 3, fi = lane & 31, half = lane >> 5;
+    int koff[4], tr[2][2];                               // tr: lane -> (word 8 half + 4 e + L / 4, four features from 4 (L % 4))
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) koff[kk] = ((2 * kk + half) ^ ((fi >> 1) & 7)) << 4;
     {
         const int L = lane & 15, grp = (lane >> 4) & 1;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) tr[e][b] = OPB + wswz(8 * half + 4 * e + (L >> 2), wn * 8 + b * 4 + grp * 2 + ((L & 3) >> 1)) + (L & 1) * 8;
+            for (int b = 0; b < 2; ++b) tr[e][b] = S::W0 + wswz(8 * half + 4 * e + (L >> 2), wn * 8 + b * 4 + grp * 2 + ((L & 3) >> 1)) + (L & 1) * 8;
     }
-    floatx16_t acc[4][2];
+    const int a0 = (wm * AT * 32 + fi) * ROWB;
+    floatx16_t acc[AT][2];
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int a = 0; a < AT; ++a)
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
-    if (steps > 0) fetch(0);
-    for (int s = 0; s < steps; ++s) {
-        dma_wait_all();
-        __syncthreads();
-        if (s + 1 < steps) fetch(s + 1);
-        const uint8_t* st = smem + (s & 1) * (2 * OPB);
-        const uint32_t sl = smem_lds + (uint32_t)(s & 1) * (2 * OPB);
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            bf16x8_t fa[4], fb[2];
-#pragma unroll
-            for (int a = 0; a < 4; ++a) fa[a] = *reinterpret_cast<const bf16x8_t*>(st + (wm * 128 + a * 32 + fi) * ROWB + (((2 * kk + half) ^ fsw) << 4));
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(uintptr_t)(sl + tr[0][b] + kk * 16 * 512));
-                const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(uintptr_t)(sl + tr[1][b] + kk * 16 * 512));
-                typedef short v8i16_t __attribute__((ext_vector_type(8)));
-                fb[b] = __builtin_bit_cast(bf16x8_t, v8i16_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    bf16x8_t fa[2][AT];
+    v4i16_t fb[2][2][2];
+    uint32_t drop[AT];                                   // exponents below the token's scale, of this step's tile
+    auto run = [&](auto SCALED_) __attribute__((always_inline)) {
+    constexpr bool SCALED = decltype(SCALED_)::value;
+    product_steps<STAGES, TP + TW + SCALED, TP + TW, AT + 4 + (SCALED ? AT : 0), AT * 2>(
+        steps, fetch,
+        [&](int s, int kk, int i) __attribute__((always_inline)) {
+            const uint32_t st = (uint32_t)(s % STAGES) * S::STAGE;
+            if (i < AT) fa[kk & 1][i < AT ? i : 0] = *reinterpret_cast<const bf16x8_t*>(smem + st + koff[kk] + a0 + i * 32 * ROWB);
+            else if (i >= AT + 4) {
+                const int a = i < AT + 4 ? 0 : i - AT - 4;
+                if (kk == 0 && (s & per) == 0) drop[a] = *reinterpret_cast<const uint32_t*>(smem + st + S::D0 + (wm * AT * 32 + a * 32 + fi) * 4);
+            } else {
+                const int q = i < AT || i >= AT + 4 ? 0 : i - AT, b = q >> 1, e = q & 1;
+                fb[kk & 1][b][e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(uintptr_t)(smem_lds + st + tr[e][b] + kk * 16 * 512));
             }
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[a], fb[b], acc[a][b], 0, 0, 0);
-        }
-    }
+        },
+        [&](int kk, int j) __attribute__((always_inline)) {
+            const int a = j >> 1, b = j & 1;
+            if (SCALED && b == 0) {                      // (an exponent that runs out leaves zero)
+                const v2u16_t d = __builtin_bit_cast(v2u16_t, drop[a]);
+                fa[kk & 1][a] = __builtin_bit_cast(bf16x8_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(v8u16_t, fa[kk & 1][a]), v8u16_t{d[0], d[1], d[0], d[1], d[0], d[1], d[0], d[1]}));
+            }
+            const v4i16_t lo = fb[kk & 1][b][0], hi = fb[kk & 1][b][1];
+            acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[kk & 1][a], __builtin_bit_cast(bf16x8_t, v8i16_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}),
+                                                                acc[a][b], 0, 0, 0);
+        });
+    };
+    if (scaled) run(std::true_type{});
+    else run(std::false_type{});
     float* out = p.part + (size_t)split * p.M * p.K;
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int a = 0; a < AT; ++a)
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int k = k0 + wn * 64 + b * 32 + fi;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const int m = m0 + wm * 128 + a * 32 + 8 * (v >> 2) + 4 * half + (v & 3);
+                const int m = m0 + wm * AT * 32 + a * 32 + 8 * (v >> 2) + 4 * half + (v & 3);
                 if (m < p.M && k < p.K) out[(size_t)m * p.K + k] = acc[a][b][v];
             }
         }
 }
 
-// ---- the splits' sums and the target's term
+// ---- the splits' sums times the token's factor, and the target's term
 __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
     const int runs = p.K / 8;
-    for (long long id = blockIdx.x * 256 + threadIdx.x; id < (long long)p.M * runs; id += gridDim.x * 256) {
+    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < (long long)p.M * runs; id += (long long)gridDim.x * 256) {
         const int m = (int)(id / runs), c = (int)(id % runs), t = p.targets[m];
+        const bool there = t >= 0 && t < p.V;
+        const float2 f = p.rows[m];
+        const uint4 q = reinterpret_cast<const uint4*>(p.W + (size_t)(there ? t : 0) * p.K)[c];
         float v[8] = {};
+#pragma unroll 4
         for (int s = 0; s < p.splits; ++s) {
-            const float4* q = reinterpret_cast<const float4*>(p.part + ((size_t)s * p.M + m) * p.K + 8 * c);
-            const float4 x = q[0], y = q[1];
-            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+            const float4* x = reinterpret_cast<const float4*>(p.part + ((size_t)s * p.M + m) * p.K + 8 * c);
+            const float4 lo = x[0], hi = x[1];
+            v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w; v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
         }
+        const uint32_t u[4] = {q.x, q.y, q.z, q.w};
         uint4 o = zero4();
-        if (t >= 0 && t < p.V) {
-            const uint4 q = reinterpret_cast<const uint4*>(p.W + (size_t)t * p.K)[c];
-            const float f = p.rows[m].y;
-            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+        if (there) {                                     // (nothing for a token without a target, whatever it holds)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __builtin_fmaf(f, bf16_bits_to_float(u[i] & 0xffffu), v[2 * i]);
-                v[2 * i + 1] = __builtin_fmaf(f, __builtin_bit_cast(float, u[i] & 0xffff0000u), v[2 * i + 1]);
+                v[2 * i] = __builtin_fmaf(f.y, bf16_bits_to_float(u[i] & 0xffffu), v[2 * i] * f.x);
+                v[2 * i + 1] = __builtin_fmaf(f.y, __builtin_bit_cast(float, u[i] & 0xffff0000u), v[2 * i + 1] * f.x);
             }
             o = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
         }
@@ -342,28 +445,52 @@ __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
 constexpr size_t kLossPiece = (size_t)256 << 20;         // bytes of a piece's exponentials
 constexpr size_t kLossPart = (size_t)64 << 20;           // bytes of the second product's partial sums beyond one of each
 
+// Microseconds of a round of tiles on all units: what does not depend on the steps, and a step (256 tiles of 1024 and 4096 features, or 2048 and 8192 words).
+// Lower tiles cost more per token, but leave less of a round empty.
+struct TileCost { int tokens; double fixed, step; };
+constexpr TileCost kLogitsCost[] = {{256, 11.0, 1.48}, {192, 8.0, 1.20}, {128, 6.0, 0.93}, {64, 3.0, 0.62}};
+constexpr TileCost kGradCost[] = {{256, 10.0, 1.55}, {192, 7.0, 1.23}, {128, 4.0, 1.03}, {64, 2.0, 0.78}};
+
 struct LossPlan {
-    int tiles, VP, rows, splits, words;                  // rows: tokens a piece
-    size_t stats0, zt0, rows0, part0, P0, bytes;
+    int tokens, shift, tiles, VP, rows, grad_tokens, splits, words;      // rows: tokens a piece
+    size_t stats0, zt0, drop0, uneven0, rows0, part0, P0, bytes;
 };
 LossPlan loss_plan(int M, int V, int K, bool grad) {
     LossPlan l{};
-    l.tiles = (V + TILE - 1) / TILE;
-    l.VP = l.tiles * TILE;
-    const size_t fits = std::min(kLossPiece / ((size_t)l.VP * 2), kLossPiece / ((size_t)K * 4)) / TILE * TILE;
-    l.rows = grad ? (int)std::min<size_t>(M, std::max<size_t>(fits, TILE)) : M;
-    l.rows = std::min(l.rows, std::max((1 << 24) / l.tiles, TILE));      // (statistics of a piece: 128 MB)
-    const long long out_tiles = (long long)((l.rows + TILE - 1) / TILE) * ((K + TILE - 1) / TILE);
+    const int units = device_compute_units();
+    const int V256 = (V + 255) / 256;
+    size_t rows = (size_t)M;
+    if (grad) rows = std::min(rows, std::max<size_t>(std::min(kLossPiece / ((size_t)V256 * 512), kLossPiece / 2 / ((size_t)K * 4)) / 256 * 256, 256));
+    rows = std::min<size_t>(rows, std::max((1 << 24) / V256, 256));      // (statistics of a piece: 128 MB)
+    l.rows = (int)rows;
+    l.shift = l.rows <= 64 ? 7 : 8;                      // few tokens: tiles of 128 words, so that more units read W
+    l.tiles = (V + (1 << l.shift) - 1) >> l.shift;
+    l.VP = l.tiles << l.shift;
+    auto rounds = [&](long long tiles) { return (double)((tiles + units - 1) / units); };
+    double least = 1e300;
+    for (const TileCost& c : kLogitsCost) {
+        const double t = rounds((long long)((l.rows + c.tokens - 1) / c.tokens) * l.tiles) * (c.fixed + c.step * ((K + DEPTH - 1) / DEPTH));
+        if (l.rows <= 64 ? c.tokens == 64 : t < least) { least = t; l.tokens = c.tokens; }
+    }
+    // The second product has few tiles, so that its words are split between workgroups, whose sums are written and read once more (at 4 MB a microsecond).
     const size_t out_bytes = (size_t)l.rows * K * 4;
-    const int steps = l.VP / DEPTH;
-    long long splits = std::max<long long>(1, std::min<long long>(device_compute_units() / out_tiles, steps / 8));
-    splits = std::max<long long>(1, std::min<long long>(splits, (long long)(kLossPart / out_bytes) + 1));
-    l.words = (int)((steps + splits - 1) / splits) * DEPTH;
+    const int most = (int)std::min<size_t>(std::min(l.tiles, 64), kLossPart / out_bytes + 1);
+    least = 1e300;
+    for (const TileCost& c : kGradCost) {
+        const long long out_tiles = (long long)((l.rows + c.tokens - 1) / c.tokens) * ((K + 255) / 256);
+        for (int splits = 1; splits <= most; ++splits) {
+            const int words = ((l.tiles + splits - 1) / splits) << l.shift;
+            const double t = rounds(out_tiles * splits) * (c.fixed + c.step * (words / DEPTH)) + (double)splits * (double)out_bytes / 2e6;
+            if (t < least) { least = t; l.grad_tokens = c.tokens; l.words = words; }
+        }
+    }
     l.splits = (l.VP + l.words - 1) / l.words;
     auto take = [&](size_t n) { const size_t at = l.bytes; l.bytes += (n + 255) / 256 * 256; return at; };
     l.stats0 = take((size_t)l.rows * l.tiles * sizeof(LossStat));
     l.zt0 = take((size_t)l.rows * 4);
     if (grad) {
+        l.drop0 = take((size_t)l.rows * l.tiles * 4);
+        l.uneven0 = take((size_t)(l.rows + 63) / 64 * 4);
         l.rows0 = take((size_t)l.rows * 8);
         l.part0 = take((size_t)l.splits * out_bytes);
         l.P0 = take((size_t)l.rows * l.VP * 2);
@@ -371,36 +498,58 @@ LossPlan loss_plan(int M, int V, int K, bool grad) {
     return l;
 }
 
+template <class K>
+hipError_t launch_tiles(K kernel, int smem, long long grid, const LossParams& p, hipStream_t st) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != hipSuccess) return e;
+    kernel<<<dim3((unsigned)grid), dim3(THREADS), smem, st>>>(p);
+    return hipGetLastError();
+}
+template <int WV, int AT, int BT, int STAGES>
+hipError_t launch_logits(const LossParams& p, hipStream_t st) {
+    using S = Logits<WV, AT, BT, STAGES>;
+    return launch_tiles(loss_logits_kernel<WV, AT, BT, STAGES>, S::SMEM, (long long)((p.M + S::TOKENS - 1) / S::TOKENS) * p.tiles, p, st);
+}
+template <int AT, int STAGES>
+hipError_t launch_grad(const LossParams& p, hipStream_t st) {
+    using S = Grad<AT, STAGES>;
+    return launch_tiles(loss_grad_kernel<AT, STAGES>, S::SMEM, (long long)((p.M + S::TOKENS - 1) / S::TOKENS) * ((p.K + 255) / 256) * p.splits, p, st);
+}
+
 }  // namespace
 
 size_t vocab_loss_workspace_bytes(int M, int V, int K, bool grad) { return loss_plan(M, V, K, grad).bytes; }
 
 hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t st) {
-    static const hipError_t attr[2] = {hipFuncSetAttribute(reinterpret_cast<const void*>(loss_logits_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, SMEM),
-                                       hipFuncSetAttribute(reinterpret_cast<const void*>(loss_grad_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, SMEM)};
-    if (attr[0] != hipSuccess) return attr[0];
-    if (attr[1] != hipSuccess) return attr[1];
     const bool grad = a.dH != nullptr;
     const LossPlan l = loss_plan(a.M, a.V, a.K, grad);
     uint8_t* ws = static_cast<uint8_t*>(a.workspace);
     for (int m0 = 0; m0 < a.M; m0 += l.rows) {
         LossParams p{};
-        p.M = std::min(l.rows, a.M - m0); p.V = a.V; p.K = a.K; p.VP = l.VP; p.tiles = l.tiles;
+        p.M = std::min(l.rows, a.M - m0); p.V = a.V; p.K = a.K; p.VP = l.VP; p.tiles = l.tiles; p.tile_shift = l.shift;
         p.h = a.h + (size_t)m0 * a.K; p.W = a.W; p.targets = a.targets + m0; p.weights = a.weights ? a.weights + m0 : nullptr;
         p.loss = a.loss + m0; p.lse = a.lse ? a.lse + m0 : nullptr; p.dH = grad ? a.dH + (size_t)m0 * a.K : nullptr;
         p.stats = reinterpret_cast<LossStat*>(ws + l.stats0); p.zt = reinterpret_cast<float*>(ws + l.zt0);
         if (grad) {
-            p.rows = reinterpret_cast<float2*>(ws + l.rows0); p.part = reinterpret_cast<float*>(ws + l.part0); p.P = reinterpret_cast<uint16_t*>(ws + l.P0);
+            p.drop = reinterpret_cast<uint32_t*>(ws + l.drop0); p.uneven = reinterpret_cast<uint32_t*>(ws + l.uneven0); p.rows = reinterpret_cast<float2*>(ws + l.rows0);
+            p.part = reinterpret_cast<float*>(ws + l.part0); p.P = reinterpret_cast<uint16_t*>(ws + l.P0);
             p.splits = l.splits; p.words_per_split = l.words;
         }
-        const int tiles_m = (p.M + TILE - 1) / TILE;
-        loss_logits_kernel<<<dim3((unsigned)(tiles_m * l.tiles)), dim3(THREADS), SMEM, st>>>(p);
-        loss_rows_kernel<<<dim3((unsigned)((p.M + 3) / 4)), dim3(256), 0, st>>>(p);
-        hipError_t e = hipGetLastError();
+        hipError_t e;
+        if (l.shift == 7) e = launch_logits<4, 1, 1, 6>(p, st);
+        else if (l.tokens == 256) e = launch_logits<2, 4, 2, 2>(p, st);
+        else if (l.tokens == 192) e = launch_logits<4, 2, 3, 2>(p, st);
+        else if (l.tokens == 128) e = launch_logits<4, 2, 2, 3>(p, st);
+        else e = launch_logits<4, 2, 1, 3>(p, st);
         if (e != hipSuccess) return e;
+        loss_rows_kernel<<<dim3((unsigned)((p.M + 63) / 64)), dim3(1024), 0, st>>>(p);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
         if (!grad) continue;
-        loss_scale_kernel<<<dim3((unsigned)p.M * (unsigned)((l.VP / 8 + 1023) / 1024)), dim3(256), 0, st>>>(p);
-        loss_grad_kernel<<<dim3((unsigned)(tiles_m * ((a.K + TILE - 1) / TILE) * l.splits)), dim3(THREADS), SMEM, st>>>(p);
+        if (l.grad_tokens == 256) e = launch_grad<4, 2>(p, st);
+        else if (l.grad_tokens == 192) e = launch_grad<3, 2>(p, st);
+        else if (l.grad_tokens == 128) e = launch_grad<2, 3>(p, st);
+        else e = launch_grad<1, 3>(p, st);
+        if (e != hipSuccess) return e;
         loss_sum_kernel<<<dim3((unsigned)std::min<long long>(((long long)p.M * (a.K / 8) + 255) / 256, 16 * device_compute_units())), dim3(256), 0, st>>>(p);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }

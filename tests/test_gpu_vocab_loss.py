@@ -48,7 +48,7 @@ def formulas(h, W, targets, weights):
 # exp: the difference of two logits, its product with log2 e and exp2 itself, 2^-23 of the exponent x (x e^-x < 0.4) and 2^-22; 64 terms a lane, a few joins, the
 # tiles' sums one after another in at most 64 lanes: 2^-17 of the sum of positive terms for up to 2^18 words.
 REL = 2.0 ** -17
-TINY = 2.0 ** -126        # an exponential below this is flushed to zero, so each of V words may be off by as much, in the loss and in its probability (times a weight below 1.25, |W| <= 1)
+TINY = 2.0 ** -126        # an exponential below this is flushed to zero (of the largest, where that is 2^0 to 2^64: here it is), so each of V words may be off by as much, in the loss and in its probability (times a weight below 1.25, |W| <= 1)
 
 
 def check(out, f):
