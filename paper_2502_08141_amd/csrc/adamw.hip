@@ -17,6 +17,8 @@ namespace lowra {
 namespace {
 
 constexpr int AW_THREADS = 256, AW_STEP = 4 * AW_THREADS;    // elements a workgroup takes at a time
+constexpr int AW_MOST = 4;                                   // and how often, with all loads of these in flight together
+constexpr int AW_AHEAD = 4;                                  // loads of codes in flight where they are only decoded
 
 __device__ __forceinline__ float m_value(int q, float A) {
     const float u = (float)q * (float)(1.0 / 127.0);
@@ -39,76 +41,103 @@ __device__ __forceinline__ float group_absmax(const float (&x)[4]) {
     b = dpp_umax<0x128>(b);                                  // row_ror:8
     return __builtin_bit_cast(float, b);
 }
-// The number of borders (k + 1/2)^P A below x MOST^P, P = 2 or 4.  In fp32 the count is right but next to a border (the quotient and the roots are
-// within 2^-22, so 255.5 of them within 2^-13.9); there both sides are compared in 64 bits.
+// The numbers of borders (k + 1/2)^P A below x MOST^P, P = 2 or 4.  In fp32 (quotient, roots and sum to one ulp) the count is right but next to a border:
+// 255.5 roots are less than 2^-14 off.  There both sides are compared in 64 bits; a wavefront has such a place in one of eight times.
 template <int P>
-__device__ __forceinline__ int code_of(float x, float A, float scale, float over) {
-    constexpr int MOST = P == 2 ? 127 : 255;
-    float u = sqrtf(x * scale * over);
-    if (P == 4) u = sqrtf(u);
-    const float t = u * (float)MOST + 0.5f;
-    const float whole = floorf(t), part = t - whole;
-    int q = (int)fminf(whole, (float)MOST);
-    if (part < 0x1p-12f || part > 1.0f - 0x1p-12f) {
-        const double full = (double)x * (double)(P == 2 ? 127ll * 127 : 255ll * 255 * 255 * 255);
-        auto border = [&](double k) __attribute__((always_inline)) { return (P == 2 ? k * k : (k * k) * (k * k)) * (double)A; };
-        if (q > 0 && full <= border(q - 0.5)) --q;
-        else if (q < MOST && full > border(q + 0.5)) ++q;
+__device__ __forceinline__ void codes_of(const float (&x)[4], float A, float (&q)[4]) {
+    constexpr float MOST = P == 2 ? 127.0f : 255.0f;
+    const bool tiny = A < 0x1p-120f;                         // (the reciprocal would be none)
+    float over = A > 0.0f ? __builtin_amdgcn_rcpf(tiny ? A * 0x1p30f : A) : 0.0f, worst = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float u = __builtin_fabsf(x[i]) * over;
+        if (__any(tiny)) u = tiny ? __builtin_fabsf(x[i]) * 0x1p30f * over : u;
+        u = __builtin_amdgcn_sqrtf(u);
+        if (P == 4) u = __builtin_amdgcn_sqrtf(u);
+        const float t = __builtin_fmaf(u, MOST, 0.5f), part = __builtin_amdgcn_fractf(t);
+        q[i] = t - part;
+        worst = fmaxf(worst, __builtin_fabsf(part - 0.5f));
     }
-    return P == 4 && x > 0.0f ? max(q, 1) : q;
+    if (worst > 0.5f - 0x1p-12f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const double full = (double)__builtin_fabsf(x[i]) * (double)(P == 2 ? 127ll * 127 : 255ll * 255 * 255 * 255);
+            auto border = [&](double k) __attribute__((always_inline)) { return (P == 2 ? k * k : (k * k) * (k * k)) * (double)A; };
+            if (q[i] > 0.0f && full <= border((double)q[i] - 0.5)) q[i] -= 1.0f;
+            else if (q[i] < MOST && full > border((double)q[i] + 0.5)) q[i] += 1.0f;
+        }
+    }
+}
+
+// The root to one ulp, of subnormal numbers as well (v_sqrt_f32 takes those for zero); the IEEE one is fifteen instructions.
+__device__ __forceinline__ float root_of(float x) {
+    const bool tiny = x < 0x1p-96f;
+    return __builtin_amdgcn_sqrtf(tiny ? x * 0x1p64f : x) * (tiny ? 0x1p-32f : 1.0f);
 }
 
 template <bool FULL>
 __device__ __forceinline__ float4 get4(const float* p, long long left) {
-    if (FULL) return *reinterpret_cast<const float4*>(p);
+    if (FULL) return load16_stream(reinterpret_cast<const float4*>(p));
     return make_float4(left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f, left > 2 ? p[2] : 0.0f, left > 3 ? p[3] : 0.0f);
 }
 template <bool FULL>
 __device__ __forceinline__ void put4(float* p, long long left, const float (&v)[4]) {
-    if (FULL) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); return; }
+    if (FULL) { store16_stream(p, make_float4(v[0], v[1], v[2], v[3])); return; }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (left > i) p[i] = v[i];
 }
 
-// Four elements of an item; all 16 lanes of a group come here together.
+// Four elements of an item as they lie in memory
+struct Quad { float4 g, w, m, v; uint32_t mq, vq; float mA, vA; };
 template <bool EIGHT, bool FULL>
-__device__ __forceinline__ void adamw_four(const AdamwItem& it, const AdamwStep& s, float clip, long long at) {
+__device__ __forceinline__ void adamw_load(const AdamwItem& it, long long at, Quad& q) {
     const long long left = it.count - at;
-    const float4 g4 = get4<FULL>(it.grad + at, left), w4 = get4<FULL>(it.weight + at, left);
+    q.g = get4<FULL>(it.grad + at, left);
+    q.w = get4<FULL>(it.weight + at, left);
+    if (!EIGHT) {
+        q.m = get4<FULL>(static_cast<const float*>(it.m) + at, left);
+        q.v = get4<FULL>(static_cast<const float*>(it.v) + at, left);
+        return;
+    }
+    const uint8_t *m = static_cast<const uint8_t*>(it.m) + at, *v = static_cast<const uint8_t*>(it.v) + at;
+    if (FULL) {
+        q.mq = *reinterpret_cast<const uint32_t*>(m);
+        q.vq = *reinterpret_cast<const uint32_t*>(v);
+    } else {
+        q.mq = q.vq = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (left > i) { q.mq |= (uint32_t)m[i] << (8 * i); q.vq |= (uint32_t)v[i] << (8 * i); }
+    }
+    q.mA = FULL || left > 0 ? it.m_absmax[at >> 6] : 0.0f;
+    q.vA = FULL || left > 0 ? it.v_absmax[at >> 6] : 0.0f;
+}
+
+// All 16 lanes of a group come here together.
+template <bool EIGHT, bool FULL>
+__device__ __forceinline__ void adamw_four(const AdamwItem& it, const AdamwStep& s, float clip, long long at, const Quad& r) {
+    const long long left = it.count - at;
     float m[4], v[4];
     if (EIGHT) {
-        uint32_t mq = 0, vq = 0;
-        if (FULL) {
-            mq = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(it.m) + at);
-            vq = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(it.v) + at);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (left > i) {
-                    mq |= (uint32_t)static_cast<const uint8_t*>(it.m)[at + i] << (8 * i);
-                    vq |= (uint32_t)static_cast<const uint8_t*>(it.v)[at + i] << (8 * i);
-                }
-        }
-        const float mA = FULL || left > 0 ? it.m_absmax[at >> 6] : 0.0f, vA = FULL || left > 0 ? it.v_absmax[at >> 6] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            m[i] = m_value((int)(int8_t)(mq >> (8 * i)), mA);
-            v[i] = v_value((vq >> (8 * i)) & 0xffu, vA);
+            m[i] = m_value((int)(int8_t)(r.mq >> (8 * i)), r.mA);
+            v[i] = v_value((r.vq >> (8 * i)) & 0xffu, r.vA);
         }
     } else {
-        const float4 m4 = get4<FULL>(static_cast<const float*>(it.m) + at, left), v4 = get4<FULL>(static_cast<const float*>(it.v) + at, left);
-        m[0] = m4.x; m[1] = m4.y; m[2] = m4.z; m[3] = m4.w;
-        v[0] = v4.x; v[1] = v4.y; v[2] = v4.z; v[3] = v4.w;
+        m[0] = r.m.x; m[1] = r.m.y; m[2] = r.m.z; m[3] = r.m.w;
+        v[0] = r.v.x; v[1] = r.v.y; v[2] = r.v.z; v[3] = r.v.w;
     }
-    const float g[4] = {g4.x * clip, g4.y * clip, g4.z * clip, g4.w * clip};
-    float w[4] = {w4.x, w4.y, w4.z, w4.w};
-    const float lr = s.lr * it.lr_scale, decay = s.decay * it.decay_scale;
+    const float g[4] = {r.g.x * clip, r.g.y * clip, r.g.z * clip, r.g.w * clip};
+    float w[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
+    const float lr = s.lr * it.lr_scale, lr_m = lr * s.over_bias1, lr_w = lr * (s.decay * it.decay_scale);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         m[i] = s.b1 * m[i] + s.c1 * g[i];
         v[i] = s.b2 * v[i] + s.c2 * (g[i] * g[i]);
-        w[i] -= lr * (m[i] / s.bias1 / (sqrtf(v[i] / s.bias2) + s.eps) + decay * w[i]);
+        const float root = s.eps >= 1e-12f ? __builtin_amdgcn_sqrtf(v[i] * s.over_bias2) : root_of(v[i] * s.over_bias2);      // (uniform; the root of what is subnormal is below 1e-19)
+        w[i] = __builtin_fmaf(-lr_w, w[i], w[i]) - lr_m * m[i] * __builtin_amdgcn_rcpf(root + s.eps);
     }
     put4<FULL>(it.weight_out + at, left, w);
     if (it.weight_bf16) {                                    // uniform
@@ -130,14 +159,14 @@ __device__ __forceinline__ void adamw_four(const AdamwItem& it, const AdamwStep&
             if (left <= i) m[i] = v[i] = 0.0f;
     }
     const float mA = group_absmax(m), vA = group_absmax(v);
-    const float ms = mA < 0x1p-60f ? 0x1p64f : 1.0f, vs = vA < 0x1p-60f ? 0x1p64f : 1.0f;         // (the quotient of small numbers: both times a power of two)
-    const float mo = mA > 0.0f ? 1.0f / (mA * ms) : 0.0f, vo = vA > 0.0f ? 1.0f / (vA * vs) : 0.0f;
+    float mc[4], vc[4];
+    codes_of<2>(m, mA, mc);
+    codes_of<4>(v, vA, vc);
     uint32_t mq = 0, vq = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int q = code_of<2>(__builtin_fabsf(m[i]), mA, ms, mo);
-        mq |= (uint32_t)((m[i] < 0.0f ? -q : q) & 0xff) << (8 * i);
-        vq |= (uint32_t)(code_of<4>(v[i], vA, vs, vo) & 0xff) << (8 * i);
+        mq |= ((uint32_t)(int)(m[i] < 0.0f ? -mc[i] : mc[i]) & 0xffu) << (8 * i);
+        vq |= ((uint32_t)(int)fmaxf(vc[i], v[i] > 0.0f ? 1.0f : 0.0f) & 0xffu) << (8 * i);
     }
     if (FULL) {
         *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(it.m_out) + at) = mq;
@@ -157,28 +186,50 @@ __device__ __forceinline__ void adamw_four(const AdamwItem& it, const AdamwStep&
 }
 
 template <bool EIGHT>
-__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwItem* __restrict__ items, const AdamwChunk* __restrict__ chunks, int chunk, AdamwStep s) {
+__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwItem* __restrict__ items, const AdamwChunk* __restrict__ chunks, int steps, AdamwStep s) {
     const AdamwChunk c = chunks[blockIdx.x];
     const AdamwItem it = items[c.item];
     const float clip = s.grad_scale ? *s.grad_scale : 1.0f;
-    const long long first = c.first, last = min(first + chunk, it.count);
-    const long long whole = first + (last - first) / AW_STEP * AW_STEP;
-    for (long long at = first; at < whole; at += AW_STEP) adamw_four<EIGHT, true>(it, s, clip, at + 4 * threadIdx.x);
-    if (whole < last) adamw_four<EIGHT, false>(it, s, clip, whole + 4 * threadIdx.x);
+    const long long first = (long long)c.first + 4 * threadIdx.x;
+    if ((long long)c.first + steps * AW_STEP <= it.count && steps == AW_MOST) {          // uniform; all loads together
+        Quad q[AW_MOST];
+#pragma unroll
+        for (int k = 0; k < AW_MOST; ++k) adamw_load<EIGHT, true>(it, first + k * AW_STEP, q[k]);
+#pragma unroll
+        for (int k = 0; k < AW_MOST; ++k) adamw_four<EIGHT, true>(it, s, clip, first + k * AW_STEP, q[k]);
+        return;
+    }
+    for (int k = 0; k < steps && (long long)c.first + k * AW_STEP < it.count; ++k) {
+        Quad q;
+        if ((long long)c.first + (k + 1) * AW_STEP <= it.count) {
+            adamw_load<EIGHT, true>(it, first + k * AW_STEP, q);
+            adamw_four<EIGHT, true>(it, s, clip, first + k * AW_STEP, q);
+        } else {
+            adamw_load<EIGHT, false>(it, first + k * AW_STEP, q);
+            adamw_four<EIGHT, false>(it, s, clip, first + k * AW_STEP, q);
+        }
+    }
 }
 
 template <bool SIGNED>
 __global__ __launch_bounds__(256) void adamw_state_kernel(long long count, const uint8_t* codes, const float* absmax, float* out) {
-    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (at >= count) return;
-    const float A = absmax[at >> 6];
-    auto value = [&](uint32_t q) __attribute__((always_inline)) { return SIGNED ? m_value((int)(int8_t)q, A) : v_value(q & 0xffu, A); };
-    if (at + 4 <= count) {
-        const uint32_t q = *reinterpret_cast<const uint32_t*>(codes + at);
-        *reinterpret_cast<float4*>(out + at) = make_float4(value(q), value(q >> 8), value(q >> 16), value(q >> 24));
-        return;
+    const long long first = (long long)blockIdx.x * (1024 * AW_AHEAD) + 4 * threadIdx.x;
+    auto value = [](uint32_t q, float A) __attribute__((always_inline)) { return SIGNED ? m_value((int)(int8_t)q, A) : v_value(q & 0xffu, A); };
+    uint32_t q[AW_AHEAD];
+    float A[AW_AHEAD];
+#pragma unroll
+    for (int k = 0; k < AW_AHEAD; ++k) {
+        const long long at = first + 1024 * k;
+        q[k] = at + 4 <= count ? *reinterpret_cast<const uint32_t*>(codes + at) : 0u;
+        A[k] = at < count ? absmax[at >> 6] : 0.0f;
     }
-    for (int i = 0; at + i < count; ++i) out[at + i] = value(codes[at + i]);
+#pragma unroll
+    for (int k = 0; k < AW_AHEAD; ++k) {
+        const long long at = first + 1024 * k;
+        if (at + 4 <= count) store16_stream(out + at, make_float4(value(q[k], A[k]), value(q[k] >> 8, A[k]), value(q[k] >> 16, A[k]), value(q[k] >> 24, A[k])));
+        else
+            for (int i = 0; at + i < count; ++i) out[at + i] = value(codes[at + i], A[k]);
+    }
 }
 
 template <class T>
@@ -193,11 +244,12 @@ hipError_t adamw_build(const std::vector<AdamwItem>& items, bool eight, AdamwGro
     if (items.empty()) return hipSuccess;
     long long total = 0;
     for (const AdamwItem& it : items) total += it.count;
-    // enough workgroups to fill the chip several times, and no more than 16 rounds each
-    g.chunk = AW_STEP * (int)std::max(1ll, std::min(16ll, total / AW_STEP / (16 * device_compute_units())));
+    // as many elements as a workgroup asks for together, unless that leaves units without any
+    g.steps = (int)std::max(1ll, std::min((long long)AW_MOST, total / AW_STEP / (4 * device_compute_units())));
+    const int chunk = g.steps * AW_STEP;
     std::vector<AdamwChunk> chunks;
     for (size_t i = 0; i < items.size(); ++i)
-        for (long long at = 0; at < items[i].count; at += g.chunk) chunks.push_back(AdamwChunk{(int)i, (uint32_t)at});
+        for (long long at = 0; at < items[i].count; at += chunk) chunks.push_back(AdamwChunk{(int)i, (uint32_t)at});
     if (chunks.size() > 0x7fffffffu) return hipErrorInvalidValue;
     g.nchunks = (int)chunks.size();
     hipError_t e = upload(items, g.d_items);
@@ -205,10 +257,10 @@ hipError_t adamw_build(const std::vector<AdamwItem>& items, bool eight, AdamwGro
 }
 
 hipError_t adamw_run(const AdamwGroup (&groups)[2], const AdamwStep& s, hipStream_t st) {
-    if (groups[0].nchunks) adamw_kernel<false><<<dim3((unsigned)groups[0].nchunks), dim3(AW_THREADS), 0, st>>>(groups[0].d_items, groups[0].d_chunks, groups[0].chunk, s);
+    if (groups[0].nchunks) adamw_kernel<false><<<dim3((unsigned)groups[0].nchunks), dim3(AW_THREADS), 0, st>>>(groups[0].d_items, groups[0].d_chunks, groups[0].steps, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !groups[1].nchunks) return e;
-    adamw_kernel<true><<<dim3((unsigned)groups[1].nchunks), dim3(AW_THREADS), 0, st>>>(groups[1].d_items, groups[1].d_chunks, groups[1].chunk, s);
+    adamw_kernel<true><<<dim3((unsigned)groups[1].nchunks), dim3(AW_THREADS), 0, st>>>(groups[1].d_items, groups[1].d_chunks, groups[1].steps, s);
     return hipGetLastError();
 }
 
@@ -220,7 +272,7 @@ void adamw_free(AdamwGroup (&groups)[2]) {
 }
 
 hipError_t launch_adamw_state(long long count, bool is_signed, const void* codes, const float* absmax, float* out, hipStream_t st) {
-    const dim3 grid((unsigned)((count + 1023) / 1024)), block(256);
+    const dim3 grid((unsigned)((count + 1024 * AW_AHEAD - 1) / (1024 * AW_AHEAD))), block(256);
     if (is_signed) adamw_state_kernel<true><<<grid, block, 0, st>>>(count, static_cast<const uint8_t*>(codes), absmax, out);
     else adamw_state_kernel<false><<<grid, block, 0, st>>>(count, static_cast<const uint8_t*>(codes), absmax, out);
     return hipGetLastError();

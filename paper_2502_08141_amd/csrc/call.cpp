@@ -401,10 +401,224 @@ PyObject* init_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// ---- the operators of a training step beside the linear
+typedef int (*norm_fwd_fn)(int, int, int, const void*, const void*, const void*, float, void*, void*);
+typedef int (*norm_bwd_fn)(int, int, int, const void*, const void*, const void*, float, const void*, void*, void*, void*, void*, size_t, void*);
+struct RopeTensor { const void* x; void* y; int heads; int64_t x_token, x_head, y_token, y_head; };      // as include/lowra.h lays it out
+typedef int (*rope_fn)(int, const RopeTensor*, int, int, int, int, const void*, const void*, float, int, void*);
+typedef int (*vocab_loss_fn)(int, int, int, const void*, const void*, const void*, const void*, void*, void*, void*, void*, size_t, void*);
+norm_fwd_fn lib_norm_fwd;
+norm_bwd_fn lib_norm_bwd;
+rope_fn lib_rope;
+vocab_loss_fn lib_vocab_loss;
+
+bool here(const at::Tensor& t) { return t.get_device() == c10::hip::current_device(); }
+bool small_int(PyObject* o, int& v) {
+    if (!PyLong_CheckExact(o)) return false;
+    const long x = PyLong_AsLong(o);
+    v = (int)x;
+    return !PyErr_Occurred() && x == v;
+}
+// a tuple of the tensors that are wanted, None for the others
+template <size_t N>
+PyObject* tuple_of(at::Tensor (&out)[N], const bool (&want)[N]) {
+    PyObject* res = PyTuple_New(N);
+    for (size_t i = 0; i < N && res; ++i) {
+        PyObject* v = Py_None;
+        if (want[i]) {
+            try {
+                v = THPVariable_Wrap(std::move(out[i]));
+            } catch (...) {
+                Py_DECREF(res);
+                throw;
+            }
+        } else {
+            Py_INCREF(v);
+        }
+        if (v) PyTuple_SET_ITEM(res, i, v);
+        else Py_CLEAR(res);
+    }
+    return res;
+}
+
+// norm_fwd(x, weight, bias, kind, eps) -> y
+PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 5) return none();
+    try {
+        if (modes()) return none();
+        const at::Tensor* x = plain(a[0], at::kBFloat16);
+        int kind;
+        const void *weight, *bias;
+        if (!x || x->dim() != 2 || !here(*x) || !small_int(a[3], kind) || !PyFloat_CheckExact(a[4])) return none();
+        const int64_t M = x->size(0), N = x->size(1);
+        if (M > INT32_MAX || N > INT32_MAX || !operand(a[1], -1, N, *x, weight) || !operand(a[2], -1, N, *x, bias)) return none();
+        at::Tensor y = empty({M, N}, x->options());
+        const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
+        const void* px = x->data_ptr();
+        void *py = y.data_ptr(), *st = current_stream();
+        PyObject* res = THPVariable_Wrap(std::move(y));
+        if (!res) return none();
+        int status;
+        {
+            Unlocked u;
+            status = lib_norm_fwd((int)M, (int)N, kind, px, weight, bias, eps, py, st);
+        }
+        return done(status, res);
+    } catch (...) {
+        return none();
+    }
+}
+
+// norm_bwd(dY, x, weight, kind, eps, residual, input_grad, weight_grad, bias_grad, workspace) -> (dX or None, dweight or None, dbias or None)
+PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 10) return none();
+    try {
+        if (modes()) return none();
+        const at::Tensor *dY = plain(a[0], at::kBFloat16), *ws = plain(a[9], at::kByte);
+        int kind;
+        if (!dY || !ws || dY->dim() != 2 || !here(*dY) || ws->device() != dY->device() || !small_int(a[3], kind) || !PyFloat_CheckExact(a[4])) return none();
+        for (int i = 6; i < 9; ++i)
+            if (!PyBool_Check(a[i])) return none();
+        const int64_t M = dY->size(0), N = dY->size(1);
+        const void *x, *weight, *residual;
+        if (M > INT32_MAX || N > INT32_MAX || a[1] == Py_None || !operand(a[1], M, N, *dY, x) || !operand(a[2], -1, N, *dY, weight) || !operand(a[5], M, N, *dY, residual))
+            return none();
+        const bool want[3] = {a[6] == Py_True, a[7] == Py_True, a[8] == Py_True};
+        at::Tensor out[3];
+        void* p[3] = {nullptr, nullptr, nullptr};
+        for (int i = 0; i < 3; ++i) {
+            if (!want[i]) continue;
+            out[i] = i == 0 ? empty({M, N}, dY->options()) : empty({N}, dY->options().dtype(at::kFloat));
+            p[i] = out[i].data_ptr();
+        }
+        const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
+        const void* py = dY->data_ptr();
+        void *wp = ws->data_ptr(), *st = current_stream();
+        const size_t ws_bytes = (size_t)ws->numel();
+        PyObject* res = tuple_of(out, want);
+        if (!res) return none();
+        int status;
+        {
+            Unlocked u;
+            status = lib_norm_bwd((int)M, (int)N, kind, py, x, weight, eps, residual, p[0], p[1], p[2], wp, ws_bytes, st);
+        }
+        return done(status, res);
+    } catch (...) {
+        return none();
+    }
+}
+
+// rope(x or list of x, positions, turns, layout, inverse, magnitude) -> y or list of y
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 6) return none();
+    PyObject* res = nullptr;
+    try {
+        if (modes()) return none();
+        const bool many = PyList_CheckExact(a[0]) || PyTuple_CheckExact(a[0]);
+        const Py_ssize_t count = many ? PySequence_Fast_GET_SIZE(a[0]) : 1;
+        const at::Tensor *positions = plain(a[1], at::kInt), *turns = plain(a[2], at::kLong);
+        int layout;
+        if (count < 1 || count > 4 || !positions || !turns || positions->dim() != 1 || turns->dim() != 1 || !small_int(a[3], layout) || !PyBool_Check(a[4]) ||
+            !PyFloat_CheckExact(a[5]))
+            return none();
+        RopeTensor t[4];
+        at::Tensor out[4];
+        const int64_t M = positions->size(0);
+        int64_t D = -1;
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            PyObject* o = many ? PySequence_Fast_GET_ITEM(a[0], i) : a[0];
+            if (!THPVariable_CheckExact(o)) return none();
+            const at::Tensor& x = THPVariable_Unpack(o);
+            if (x.scalar_type() != at::kBFloat16 || !x.is_cuda() || x.dim() != 3 || (x.stride(2) != 1 && x.size(2) != 1) || x.size(0) != M || !here(x)) return none();
+            if (D < 0) D = x.size(2);
+            if (x.size(2) != D || x.size(1) > INT32_MAX) return none();
+            t[i] = RopeTensor{x.data_ptr(), nullptr, (int)x.size(1), x.stride(0), x.stride(1), x.size(1) * D, D};
+        }
+        if (M > INT32_MAX || D > INT32_MAX || turns->size(0) > INT32_MAX / 2 || !here(*positions) || !here(*turns)) return none();
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            out[i] = empty({M, t[i].heads, D}, turns->options().dtype(at::kBFloat16));
+            t[i].y = out[i].data_ptr();
+        }
+        const float magnitude = (float)PyFloat_AS_DOUBLE(a[5]);
+        const int inverse = a[4] == Py_True, rot = 2 * (int)turns->size(0);
+        const void *pp = positions->data_ptr(), *pt = turns->data_ptr();
+        void* st = current_stream();
+        if (many) {
+            res = PyList_New(count);
+            for (Py_ssize_t i = 0; i < count && res; ++i) {
+                PyObject* v = THPVariable_Wrap(std::move(out[i]));
+                if (v) PyList_SET_ITEM(res, i, v);
+                else Py_CLEAR(res);
+            }
+        } else {
+            res = THPVariable_Wrap(std::move(out[0]));
+        }
+        if (!res) return none();
+        int status;
+        {
+            Unlocked u;
+            status = lib_rope((int)count, t, (int)M, (int)D, rot, layout, pp, pt, magnitude, inverse, st);
+        }
+        return done(status, res);
+    } catch (...) {
+        Py_XDECREF(res);
+        return none();
+    }
+}
+
+// vocab_loss(h, W, targets, weights, grad, workspace) -> (loss, lse, dH or None)
+PyObject* vocab_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 6) return none();
+    try {
+        if (modes()) return none();
+        const at::Tensor *h = plain(a[0], at::kBFloat16), *W = plain(a[1], at::kBFloat16), *targets = plain(a[2], at::kInt), *ws = plain(a[5], at::kByte);
+        const at::Tensor* weights = a[3] == Py_None ? nullptr : plain(a[3], at::kFloat);
+        if (!h || !W || !targets || !ws || (!weights && a[3] != Py_None) || !PyBool_Check(a[4]) || h->dim() != 2 || W->dim() != 2 || !here(*h)) return none();
+        const int64_t M = h->size(0), K = h->size(1), V = W->size(0);
+        if (M > INT32_MAX || K > INT32_MAX || V > INT32_MAX || W->size(1) != K || targets->dim() != 1 || targets->size(0) != M) return none();
+        if (weights && (weights->dim() != 1 || weights->size(0) != M)) return none();
+        for (const at::Tensor* t : {W, targets, ws, weights})
+            if (t && t->device() != h->device()) return none();
+        const bool want[3] = {true, true, a[4] == Py_True};
+        at::Tensor out[3];
+        out[0] = empty({M}, h->options().dtype(at::kFloat));
+        out[1] = empty({M}, h->options().dtype(at::kFloat));
+        if (want[2]) out[2] = empty({M, K}, h->options());
+        const void *ph = h->data_ptr(), *pw = W->data_ptr(), *pt = targets->data_ptr(), *pf = weights ? weights->data_ptr() : nullptr;
+        void *p0 = out[0].data_ptr(), *p1 = out[1].data_ptr(), *p2 = want[2] ? out[2].data_ptr() : nullptr, *wp = ws->data_ptr(), *st = current_stream();
+        const size_t ws_bytes = (size_t)ws->numel();
+        PyObject* res = tuple_of(out, want);
+        if (!res) return none();
+        int status;
+        {
+            Unlocked u;
+            status = lib_vocab_loss((int)M, (int)V, (int)K, ph, pw, pt, pf, p0, p1, p2, wp, ws_bytes, st);
+        }
+        return done(status, res);
+    } catch (...) {
+        return none();
+    }
+}
+
+// init_step(addresses): those of the operators beside the linear
+PyObject* init_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 4) { PyErr_SetString(PyExc_TypeError, "init_step: four addresses"); return nullptr; }
+    void* f[4];
+    for (int i = 0; i < 4; ++i) f[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+    lib_norm_fwd = (norm_fwd_fn)f[0]; lib_norm_bwd = (norm_bwd_fn)f[1]; lib_rope = (rope_fn)f[2]; lib_vocab_loss = (vocab_loss_fn)f[3];
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)())init, METH_FASTCALL, nullptr},
                          {"init_act", (PyCFunction)(void (*)())init_act, METH_FASTCALL, nullptr},
                          {"linear_act", (PyCFunction)(void (*)())linear_act, METH_FASTCALL, nullptr},
                          {"act_bwd", (PyCFunction)(void (*)())act_bwd, METH_FASTCALL, nullptr},
+                         {"init_step", (PyCFunction)(void (*)())init_step, METH_FASTCALL, nullptr},
+                         {"norm_fwd", (PyCFunction)(void (*)())norm_fwd, METH_FASTCALL, nullptr},
+                         {"norm_bwd", (PyCFunction)(void (*)())norm_bwd, METH_FASTCALL, nullptr},
+                         {"rope", (PyCFunction)(void (*)())rope, METH_FASTCALL, nullptr},
+                         {"vocab_loss", (PyCFunction)(void (*)())vocab_loss, METH_FASTCALL, nullptr},
                          {"linear", (PyCFunction)(void (*)())linear, METH_FASTCALL, nullptr},
                          {"side_product", (PyCFunction)(void (*)())side_product, METH_FASTCALL, nullptr},
                          {"grads", (PyCFunction)(void (*)())grads, METH_FASTCALL, nullptr},

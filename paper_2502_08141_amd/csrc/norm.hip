@@ -47,7 +47,7 @@ __device__ __forceinline__ void row_sums(float (&v)[S], float (*red)[W][4], int&
 #pragma unroll
     for (int s = 0; s < S; ++s) v[s] = wave_sum_f32(v[s]);
     if constexpr (W > 1) {
-        const int wave = threadIdx.x >> 6;
+        const int wave = (threadIdx.x >> 6) % W;                  // of the row
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
             for (int s = 0; s < S; ++s) red[turn][wave][s] = v[s];
@@ -119,28 +119,37 @@ __global__ __launch_bounds__(norm_threads(W)) void norm_fwd_kernel(NormArgs a) {
     }
 }
 
-// Workgroups take rows in turn; sums: [workgroup][2][N] (dweight, dbias), or null
-template <int W, int C, bool RMS>
-__global__ __launch_bounds__(norm_threads(W)) void norm_bwd_kernel(NormArgs a, float* sums) {
-    constexpr int ROWS = W == 1 ? 4 : 1;
-    __shared__ float red[2][W][4];
-    const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x, first = (int)blockIdx.x * ROWS + (W == 1 ? threadIdx.x >> 6 : 0), step = (int)gridDim.x * ROWS;
-    const int runs = a.N >> 3;
+// A workgroup has G rows side by side, each W wavefronts', and takes rows in turn; sums: [dweight, dbias][workgroup][N], or null.  BIAS: dbias is asked for.
+template <int W, int C, int G, bool RMS, bool BIAS>
+__global__ __launch_bounds__(64 * W * G) void norm_bwd_kernel(NormArgs a, float* sums) {
+    __shared__ float red_of[G][2][W][4];
+    extern __shared__ __align__(16) float join[];                 // [G][N]
+    const int t = threadIdx.x % (64 * W), group = threadIdx.x / (64 * W), step = (int)gridDim.x * G;
+    float(*red)[W][4] = red_of[group];
     const float inv = 1.0f / (float)a.N;
     int turn = 0;
-    float dw[C][8], db[C][8];
+    float dw[C][8], db[BIAS ? C : 1][8];
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dw[c][i] = db[c][i] = 0.0f;
-    for (int row = first; row < a.M; row += step) {
-        const size_t at = (size_t)row * a.N;
-        uint4 xq[C], gq[C];
+        for (int i = 0; i < 8; ++i) {
+            dw[c][i] = 0.0f;
+            if (BIAS) db[BIAS ? c : 0][i] = 0.0f;
+        }
+    for (int first = (int)blockIdx.x * G; first < a.M; first += step) {              // (uniform: the sums of a row of several wavefronts meet at barriers)
+        const int runs = first + group < a.M ? a.N >> 3 : 0;
+        const size_t at = (size_t)min(first + group, a.M - 1) * a.N;
+        // (asking for the next row's operands here as well took longer: 16384 x 1024 26 -> 30 us, 4096 x 4096 31 -> 37 to 43)
+        uint4 xq[C], gq[C], rq[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int run = c * (64 * W) + t;
             xq[c] = run < runs ? reinterpret_cast<const uint4*>(a.x + at)[run] : zero4();
             gq[c] = run < runs ? reinterpret_cast<const uint4*>(a.dY + at)[run] : zero4();
+        }
+        if (a.residual) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) rq[c] = c * (64 * W) + t < runs ? reinterpret_cast<const uint4*>(a.residual + at)[c * (64 * W) + t] : zero4();
         }
         float mean = 0.0f;
         if (!RMS) {
@@ -184,12 +193,12 @@ __global__ __launch_bounds__(norm_threads(W)) void norm_bwd_kernel(NormArgs a, f
             unpack8(xq[c], d);
             unpack8(gq[c], g);
             if (a.weight) unpack8(reinterpret_cast<const uint4*>(a.weight)[run], w);
-            if (a.residual) unpack8(reinterpret_cast<const uint4*>(a.residual + at)[run], r);
+            if (a.residual) unpack8(rq[c], r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 d[i] -= mean;
                 dw[c][i] += g[i] * (d[i] * rstd);
-                db[c][i] += g[i];
+                if (BIAS) db[BIAS ? c : 0][i] += g[i];
                 if (a.weight) g[i] *= w[i];
                 g[i] = rstd * (g[i] - gmean - d[i] * along);
                 if (a.residual) g[i] += r[i];
@@ -198,59 +207,59 @@ __global__ __launch_bounds__(norm_threads(W)) void norm_bwd_kernel(NormArgs a, f
         }
     }
     if (!sums) return;                                            // uniform
-    float* out = sums + (size_t)blockIdx.x * 2 * a.N;
-    if constexpr (W == 1) {
-        __shared__ float join[4][64][8];
-        const int wave = threadIdx.x >> 6;
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) join[wave][t][i] = half ? db[c][i] : dw[c][i];
-                __syncthreads();
-                for (int o = threadIdx.x; o < 512; o += 256) {
-                    const int col = c * 512 + o;
-                    if (col < a.N) out[(size_t)half * a.N + col] = ((join[0][o >> 3][o & 7] + join[1][o >> 3][o & 7]) + join[2][o >> 3][o & 7]) + join[3][o >> 3][o & 7];
-                }
-            }
-    } else {
+    for (int half = 0; half < (BIAS ? 2 : 1); ++half) {
+        float* out = sums + ((size_t)half * gridDim.x + blockIdx.x) * a.N;
+        float* to = G > 1 ? join + group * a.N : out;
+        if (G > 1 && half) __syncthreads();
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int run = c * (64 * W) + t;
-            if (run >= runs) continue;
+            if (run >= a.N >> 3) continue;
+            const float(&v)[8] = half ? db[BIAS ? c : 0] : dw[c];
+            float4* p = reinterpret_cast<float4*>(to) + 2 * run;
+            p[0] = make_float4(v[0], v[1], v[2], v[3]);
+            p[1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+        if (G == 1) continue;
+        __syncthreads();
+        for (int q = threadIdx.x; q < a.N / 4; q += 64 * W * G) {
+            float4 s = reinterpret_cast<const float4*>(join)[q];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float4* p = reinterpret_cast<float4*>(out + (size_t)half * a.N) + 2 * run;
-                const float(&v)[8] = half ? db[c] : dw[c];
-                p[0] = make_float4(v[0], v[1], v[2], v[3]);
-                p[1] = make_float4(v[4], v[5], v[6], v[7]);
+            for (int r = 1; r < G; ++r) {
+                const float4 u = reinterpret_cast<const float4*>(join + r * a.N)[q];
+                s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
             }
+            reinterpret_cast<float4*>(out)[q] = s;
         }
     }
 }
 
-// 32 columns a workgroup, the chunks dealt to eight groups of threads, each with up to eight loads under way; blockIdx.y: dweight, dbias
-__global__ __launch_bounds__(256) void norm_sum_kernel(const float* __restrict__ sums, int chunks, int N, float* dweight, float* dbias) {
-    __shared__ float red[8][32];
+// 32 columns a workgroup, the chunks dealt to 32 groups of threads, each with up to eight loads under way; blockIdx.y: dweight, dbias
+__global__ __launch_bounds__(1024) void norm_sum_kernel(const float* __restrict__ sums, int chunks, int N, float* dweight, float* dbias) {
+    __shared__ float red[32][33];
     float* out = blockIdx.y ? dbias : dweight;
     if (!out) return;                                             // uniform
-    const float* in = sums + (size_t)blockIdx.y * N;
+    const float* in = sums + (size_t)blockIdx.y * chunks * N;
     const int c = threadIdx.x & 31, grp = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
     float v = 0.0f;
-    for (int k = grp; k < chunks; k += 64) {
+    for (int k = grp; k < chunks; k += 256) {
         float x[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = in[(size_t)min(k + 8 * u, chunks - 1) * 2 * N + min(col, N - 1)];
+        for (int u = 0; u < 8; ++u) x[u] = in[(size_t)min(k + 32 * u, chunks - 1) * N + min(col, N - 1)];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v += k + 8 * u < chunks ? x[u] : 0.0f;
+        for (int u = 0; u < 8; ++u) v += k + 32 * u < chunks ? x[u] : 0.0f;
     }
     red[grp][c] = v;
     __syncthreads();
-    if (grp != 0 || col >= N) return;
-    for (int g = 1; g < 8; ++g) v += red[g][c];
-    out[col] = v;
+    if (threadIdx.x >= 64) return;
+    // a wavefront adds up the 32 groups, half of them a lane
+    const int half = threadIdx.x >> 5;
+    v = red[16 * half][c];
+#pragma unroll
+    for (int g = 1; g < 16; ++g) v += red[16 * half + g][c];
+    v += __shfl_xor(v, 32);
+    if (half == 0 && col < N) out[col] = v;
 }
 
 // Calls f with the wavefronts that share a row and the runs of eight columns a thread
@@ -265,9 +274,26 @@ hipError_t with_shape(int N, F f) {
     if (runs <= 1024) return f(integral_constant<int, 8>{}, integral_constant<int, 2>{});
     return f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
 }
+template <int W_, int C_, int G_> struct BwdShape { static constexpr int W = W_, C = C_, G = G_; };
+// Two runs a thread and two workgroups of 512 threads a unit, so that few partial sums are left (4096 x 4096, rms, with residual: 44 us with one row to a workgroup
+// and 1024 of those, 28.8 now; a wavefront to a row 35).  Up to 1024 columns few rows are done sooner with two wavefronts each (64 and 777 rows of 1024 7.1
+// and 7.7 -> 6.2 and 7.2 us), many with one (16384: 28.8 -> 26.4).
+template <class F>
+auto with_bwd_shape(int M, int N, F f) {
+    const int runs = N / 8;
+    if (runs <= 64) return f(BwdShape<1, 1, 8>{});
+    if (runs <= 128 && M > 8192) return f(BwdShape<1, 2, 8>{});
+    if (runs <= 128) return f(BwdShape<2, 1, 4>{});
+    if (runs <= 256) return f(BwdShape<2, 2, 4>{});
+    if (runs <= 512) return f(BwdShape<4, 2, 2>{});
+    if (runs <= 1024) return f(BwdShape<8, 2, 1>{});
+    return f(BwdShape<8, 4, 1>{});
+}
 int norm_blocks(int M, int N) {
-    const int rows = N <= 1024 ? 4 : 1;
-    return std::min((M + rows - 1) / rows, (N <= 4096 ? 4 : N <= 8192 ? 2 : 1) * device_compute_units());
+    return with_bwd_shape(M, N, [&](auto S_) {
+        constexpr int G = decltype(S_)::G;
+        return std::min((M + G - 1) / G, 2 * device_compute_units());
+    });
 }
 
 }  // namespace
@@ -287,14 +313,20 @@ hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t st) {
 hipError_t launch_norm_bwd(const NormArgs& a, float* dweight, float* dbias, void* workspace, hipStream_t st) {
     const int blocks = norm_blocks(a.M, a.N);
     float* sums = dweight || dbias ? static_cast<float*>(workspace) : nullptr;
-    const hipError_t e = with_shape(a.N, [&](auto W_, auto C_) {
-        constexpr int W = decltype(W_)::value, C = decltype(C_)::value;
-        if (a.rms) norm_bwd_kernel<W, C, true><<<dim3((unsigned)blocks), dim3(norm_threads(W)), 0, st>>>(a, sums);
-        else norm_bwd_kernel<W, C, false><<<dim3((unsigned)blocks), dim3(norm_threads(W)), 0, st>>>(a, sums);
-        return hipGetLastError();
+    const hipError_t e = with_bwd_shape(a.M, a.N, [&](auto S_) {
+        constexpr int W = decltype(S_)::W, C = decltype(S_)::C, G = decltype(S_)::G;
+        const int smem = G > 1 && sums ? G * a.N * (int)sizeof(float) : 0;
+        auto go = [&](auto kernel) {
+            const hipError_t e = smem > 65536 ? hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, smem) : hipSuccess;
+            if (e != hipSuccess) return e;
+            kernel<<<dim3((unsigned)blocks), dim3(64 * W * G), smem, st>>>(a, sums);
+            return hipGetLastError();
+        };
+        if (dbias) return a.rms ? go(norm_bwd_kernel<W, C, G, true, true>) : go(norm_bwd_kernel<W, C, G, false, true>);
+        return a.rms ? go(norm_bwd_kernel<W, C, G, true, false>) : go(norm_bwd_kernel<W, C, G, false, false>);
     });
     if (e != hipSuccess || !sums) return e;
-    norm_sum_kernel<<<dim3((unsigned)((a.N + 31) / 32), 2), dim3(256), 0, st>>>(sums, blocks, a.N, dweight, dbias);
+    norm_sum_kernel<<<dim3((unsigned)((a.N + 31) / 32), dbias ? 2u : 1u), dim3(1024), 0, st>>>(sums, blocks, a.N, dweight, dbias);
     return hipGetLastError();
 }
 

@@ -62,12 +62,12 @@ __device__ __forceinline__ float hi16(uint32_t w) { return __builtin_bit_cast(fl
 // V columns to an access.  A unit is what a thread has of a head: V pairs of columns V apart from each other by rot / 2, or V neighbours that
 // are V / 2 pairs (V = 1: a pair by itself), or V columns behind the rotated ones.  Threads: units fastest, then head slots, then tokens.
 template <int V, bool INTER>
-__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int units, int rot_units, int slots, long long total) {
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int units, int rot_units, int slots, uint32_t total) {
+    const uint32_t id = blockIdx.x * 256u + threadIdx.x;
     if (id >= total) return;
-    const int unit = (int)(id % units);
-    const long long rest = id / units;
-    const int slot = (int)(rest % slots), m = (int)(rest / slots);
+    const uint32_t rest = id / (uint32_t)units;
+    const int unit = (int)(id - rest * (uint32_t)units);
+    const int m = (int)(rest / (uint32_t)slots), slot = (int)(rest - (uint32_t)m * (uint32_t)slots);
     if (unit >= rot_units) {                                     // columns that stay
         const int col = a.rot + (unit - rot_units) * V;
         int h0 = 0;
@@ -144,7 +144,7 @@ hipError_t run(const RopeArgs& a, hipStream_t st) {
     const long long want = 4ll * 256 * device_compute_units();
     const int slots = (int)std::max<long long>(1, std::min<long long>(heads, std::max<long long>((heads + 7) / 8, want / std::max<long long>(1, (long long)a.M * units))));
     const long long total = (long long)a.M * slots * units;
-    rope_kernel<V, INTER><<<dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st>>>(a, units, rot_units, slots, total);
+    rope_kernel<V, INTER><<<dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st>>>(a, units, rot_units, slots, (uint32_t)total);
     return hipGetLastError();
 }
 

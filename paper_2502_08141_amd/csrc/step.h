@@ -41,12 +41,12 @@ struct AdamwItem {
     long long count;
     float lr_scale, decay_scale;
 };
-struct AdamwChunk { int item; uint32_t first; };             // elements [first, first + the launch's chunk) of an item
+struct AdamwChunk { int item; uint32_t first; };             // elements of an item from this one on, as many as a workgroup of the launch takes
 struct AdamwGroup {                                          // the items whose states have the same width
     AdamwItem* d_items = nullptr; AdamwChunk* d_chunks = nullptr;
-    int nchunks = 0, chunk = 0;
+    int nchunks = 0, steps = 0;
 };
-struct AdamwStep { float lr, b1, c1, b2, c2, bias1, bias2, eps, decay; const float* grad_scale; };   // c = 1 - b; bias = 1 - b^t
+struct AdamwStep { float lr, b1, c1, b2, c2, over_bias1, over_bias2, eps, decay; const float* grad_scale; };   // c = 1 - b; over_bias = 1 / (1 - b^t)
 hipError_t adamw_build(const std::vector<AdamwItem>& items, bool eight, AdamwGroup& g);
 hipError_t adamw_run(const AdamwGroup (&groups)[2], const AdamwStep& s, hipStream_t st);
 void adamw_free(AdamwGroup (&groups)[2]);

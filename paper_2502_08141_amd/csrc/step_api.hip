@@ -238,8 +238,8 @@ lowra_status lowra_adamw_batch_run(const lowra_adamw_batch* b, const lowra_adamw
     if (hipGetDevice(&dev) != hipSuccess) return LOWRA_HIP_ERROR;
     if (dev != b->device) return LOWRA_INVALID_ARG;
     // (1 - beta^t by expm1 and log: a beta next to one keeps its digits)
-    auto bias = [&](double beta) { return beta > 0.0 ? (float)-std::expm1((double)s->step * std::log(beta)) : 1.0f; };
-    const lowra::AdamwStep a{(float)s->lr, (float)s->beta_one, (float)(1.0 - s->beta_one), (float)s->beta_two, (float)(1.0 - s->beta_two), bias(s->beta_one), bias(s->beta_two),
+    auto over_bias = [&](double beta) { return beta > 0.0 ? (float)(-1.0 / std::expm1((double)s->step * std::log(beta))) : 1.0f; };
+    const lowra::AdamwStep a{(float)s->lr, (float)s->beta_one, (float)(1.0 - s->beta_one), (float)s->beta_two, (float)(1.0 - s->beta_two), over_bias(s->beta_one), over_bias(s->beta_two),
                              (float)s->eps, (float)s->weight_decay, grad_scale};
     return launched(lowra::adamw_run(b->groups, a, static_cast<hipStream_t>(stream)));
 }

@@ -193,6 +193,7 @@ def lib() -> C.CDLL:
         call.init(*(C.cast(f, C.c_void_p).value for f in (L.lowra_linear_fwd, L.lowra_linear_bwd_input, L.lowra_linear_side_product,
                                                           L.lowra_adapter_grads, L.lowra_adapter_grads_from_side, L.lowra_dequantize)))
         call.init_act(*(C.cast(f, C.c_void_p).value for f in (L.lowra_linear_fwd_act, L.lowra_linear_bwd_input_act, L.lowra_act_bwd)))
+        call.init_step(*(C.cast(f, C.c_void_p).value for f in (L.lowra_norm_fwd, L.lowra_norm_bwd, L.lowra_rope, L.lowra_vocab_loss)))
         _lib, _call = L, call
     return _lib
 
@@ -846,6 +847,10 @@ def _typed(t, dtype, shape, name: str, device):
 def lowra_norm_fwd(x, weight=None, bias=None, kind: int = NORM_LAYER, eps: float = 1e-5, y=None):
     """y [M,N] bf16 = (x - mean) / sqrt(mean((x - mean)^2) + eps) weight + bias over the rows of x [M,N] bf16; NORM_RMS: mean = 0.  weight, bias:
     [N] bf16 or None; y may be x."""
+    if y is None and _lib is not None:
+        res = _call.norm_fwd(x, weight, bias, kind, eps)
+        if res is not None:
+            return _native(res, "lowra_norm_fwd")
     M, N = _rows(x, "x")
     _operand(weight, (N,), "weight", x.device); _operand(bias, (N,), "bias", x.device)
     if y is None:
@@ -863,6 +868,10 @@ def lowra_norm_bwd(dY, x, weight=None, kind: int = NORM_LAYER, eps: float = 1e-5
                    bias_grad: bool = False, dX=None, dweight=None, dbias=None, workspace=None):
     """The way back of lowra_norm_fwd for dY [M,N] bf16 -> (dX, dweight, dbias): dX bf16 with `residual` [M,N] bf16 added (None without `input_grad`),
     dweight and dbias fp32 [N] (None without `weight_grad`, `bias_grad`).  What is given of the three is written there; dX may be residual."""
+    if dX is None and dweight is None and dbias is None and workspace is not None and _lib is not None:
+        res = _call.norm_bwd(dY, x, weight, kind, eps, residual, input_grad, weight_grad, bias_grad, workspace)
+        if res is not None:
+            return _native(res, "lowra_norm_bwd")
     M, N = _rows(dY, "dY")
     device = dY.device
     _operand(x, (M, N), "x", device); _operand(weight, (N,), "weight", device); _operand(residual, (M, N), "residual", device)
@@ -898,6 +907,10 @@ def lowra_rope(x, positions, turns, layout: int = ROPE_HALF, inverse: bool = Fal
     """Rotary positions of x [M, heads, D] bf16, or of a list of up to four of those (queries and keys) with the same M and D, by positions [M]
     int32 and the plan `turns` (lowra_rope_frequencies), whose length says how many columns are turned.  Tokens and heads may have any stride, the
     columns are contiguous.  `out`: where to write, of the same shapes (x itself: in place); new tensors without it.  `inverse`: the way back."""
+    if out is None and _lib is not None:
+        res = _call.rope(x, positions, turns, layout, inverse, magnitude)
+        if res is not None:
+            return _native(res, "lowra_rope")
     many = isinstance(x, (list, tuple))
     xs = list(x) if many else [x]
     if not xs or len(xs) > 4:
@@ -935,6 +948,10 @@ def lowra_vocab_loss(h, W, targets, weights=None, grad: bool = True, loss=None, 
     """Cross entropy of h [M,K] bf16 through the frozen head W [V,K] bf16 against targets [M] int32 (outside 0..V-1: no target, loss 0) ->
     (loss fp32 [M], lse fp32 [M], dH bf16 [M,K]): dH is the gradient of the sum of weights loss with respect to h (weights: [M] fp32, None: ones), None
     without `grad`."""
+    if loss is None and lse is None and dH is None and workspace is not None and _lib is not None:
+        res = _call.vocab_loss(h, W, targets, weights, grad, workspace)
+        if res is not None:
+            return _native(res, "lowra_vocab_loss")
     M, K = _rows(h, "h")
     V, _ = _rows(W, "W")
     device = h.device

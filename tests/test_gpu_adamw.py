@@ -222,6 +222,33 @@ def test_many_items_of_both_widths():
             assert bool((pool[i, k][:e] == 77).all() and (pool[i, k][e + a[k].numel():] == 77).all()), (i, k)
 
 
+def test_past_32_bit_offsets():
+    """An item whose tensors are larger than 4 GB, and whose last groups are short: as the same elements in a batch of their own."""
+    count = (1 << 30) + 4099
+    for eight in (False, True):
+        g = torch.Generator(device="cuda").manual_seed(7)
+        d = {"grad": torch.empty(count, device="cuda").normal_(generator=g), "weight": torch.empty(count, device="cuda").normal_(generator=g)}
+        if eight:
+            d |= {"m": torch.randint(-127, 128, (count,), generator=g, device="cuda", dtype=torch.int8), "v": torch.randint(0, 256, (count,), generator=g, device="cuda", dtype=torch.uint8),
+                  "m_absmax": torch.rand((count + 63) // 64, generator=g, device="cuda"), "v_absmax": torch.rand((count + 63) // 64, generator=g, device="cuda")}
+        else:
+            d |= {"m": torch.empty(count, device="cuda").normal_(generator=g), "v": torch.rand(count, generator=g, device="cuda")}
+        spans = [(0, 3000), ((1 << 30) - 64, (1 << 30) + 4099)]
+        parts = [{k: (t[a // 64:(b + 63) // 64] if "absmax" in k else t[a:b]).clone() for k, t in d.items()} for a, b in spans]
+        lowra.AdamWBatch([lowra.AdamWItem(**d)]).run(**HYPER)
+        for (a, b), q in zip(spans, parts):
+            lowra.AdamWBatch([lowra.AdamWItem(**q)]).run(**HYPER)
+            whole = b - a if b == count else (b - a) // 64 * 64                     # (a group that the part cuts has another largest magnitude)
+            for k, t in q.items():
+                n = (whole + 63) // 64 if "absmax" in k else whole
+                first = a // 64 if "absmax" in k else a
+                assert torch.equal(d[k][first:first + n], t[:n]), k
+        if eight:
+            values = lowra.lowra_adamw_state(d["m"], d["m_absmax"])
+            assert torch.equal(values[-4099:], lowra.lowra_adamw_state(d["m"][-4099:].clone(), d["m_absmax"][-65:].clone()))
+        del d
+
+
 def test_not_finite_stays_where_it_is():
     for eight in (False, True):
         s = make(256, eight, 3)

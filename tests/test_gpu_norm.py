@@ -171,6 +171,31 @@ def test_large_mean_keeps_its_digits():
     near(y, f["y"], 2.0 ** -17 * 300 * f["rstd"] * i["weight"].double().abs() * (1 + f["xh"].abs()) , "y", 2.0 ** -8)
 
 
+def test_past_32_bit_offsets():
+    M, N = 530000, 4104
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dY = (torch.empty(M, N, dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(2))
+    w = torch.randn(N, generator=g, device="cuda").bfloat16()
+    y = lowra.lowra_norm_fwd(x, w)
+    dX, dw, db = lowra.lowra_norm_bwd(dY, x, w, weight_grad=True, bias_grad=True)
+    for a, b in ((0, 20), (M - 20, M)):
+        assert torch.equal(y[a:b], lowra.lowra_norm_fwd(x[a:b].contiguous(), w))
+        assert torch.equal(dX[a:b], lowra.lowra_norm_bwd(dY[a:b].contiguous(), x[a:b].contiguous(), w)[0])
+    total = sum(dY[i:i + 50000].double().sum(0) for i in range(0, M, 50000))
+    # a workgroup's 1000 rows one after another: 2^-13 of the sum of magnitudes at worst, far less for these
+    assert float((db.double() - total).norm() / total.norm()) <= 1e-4
+
+
+def test_more_rows_than_workgroups():
+    """Rows that a launch's workgroups take in turn."""
+    M, N = (1 << 22) + 5, 8
+    x = torch.randn(M, N, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").bfloat16()
+    y, dX = lowra.lowra_norm_fwd(x), lowra.lowra_norm_bwd(x, x)[0]
+    for a, b in ((0, 64), ((1 << 22) - 7, M)):
+        assert torch.equal(y[a:b], lowra.lowra_norm_fwd(x[a:b].contiguous()))
+        assert torch.equal(dX[a:b], lowra.lowra_norm_bwd(x[a:b].contiguous(), x[a:b].contiguous())[0])
+
+
 def test_no_tokens():
     e = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
     assert lowra.lowra_norm_fwd(e).shape == (0, 64)

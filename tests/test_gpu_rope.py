@@ -122,6 +122,15 @@ def test_way_back_is_the_gradient():
         assert y.shape == x.shape
 
 
+def test_past_32_bit_offsets():
+    M, heads, D = 70000, 256, 128
+    x = torch.empty(M, heads, D, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    p, turns = places(M, 1 << 20), lowra.lowra_rope_frequencies(D)
+    y = lowra.lowra_rope(x, p, turns)
+    for a, b in ((0, 8), (M // 2, M // 2 + 8), (M - 8, M)):
+        assert torch.equal(y[a:b], lowra.lowra_rope(x[a:b], p[a:b].contiguous(), turns))
+
+
 def test_no_tokens_streams_and_graphs():
     turns = lowra.lowra_rope_frequencies(64)
     assert lowra.lowra_rope(make(0, 4, 64), places(0, 5), turns).shape == (0, 4, 64)

@@ -142,6 +142,35 @@ def test_large_logits_and_infinities():
     assert bool(a[0][2].isnan()) and bool(a[2][2].isnan().all()) and float(a[0][11]) == 0.0 and not a[2][11].any()
 
 
+def test_scales_of_a_tokens_tiles():
+    """A token's exponentials are on scales that go by the largest logit of each tile of words; where these differ (a last column of h and W makes the logits of
+    one tile larger or smaller than another's by hundreds) the gradient brings them together.  All tokens of a group alike, and one among others."""
+    for M in (3, 70, 300):
+        h, W, targets, weights = make(M, 1500, 72, 11, known=0.3)
+        h[:, -1], W[:, -1] = 0.0, 0.0
+        W[:256, -1], W[256:512, -1], W[512:600, -1] = 1.0, -1.0, 0.5
+        for rows in (slice(None), slice(M // 2, M // 2 + 1)):
+            for lift in (16.0, 48.0, 64.0, -64.0, 128.0, 256.0):
+                h2 = h.clone()
+                h2[rows, -1] = lift
+                out, f = call(h2, W, targets, weights), formulas(h2, W, targets, weights)
+                check(out, f)
+    # the same logits all moved by a constant: nothing changes but lse
+    h, W, targets, weights = make(100, 700, 72, 12)
+    h[:, -1], W[:, -1] = 0.0, 1.0
+    base = call(h, W, targets, weights)
+    for lift in (-256.0, -64.0, -16.0, 32.0, 128.0):
+        h2 = h.clone()
+        h2[:, -1] = lift
+        out, f = call(h2, W, targets, weights), formulas(h2, W, targets, weights)
+        # (from 2^-32 of the largest on down to 2^-94 a probability may be lost: the loss of the surest tokens by V of those)
+        f["V"] = max(f["V"], f["V"] * 2.0 ** 32 if lift < 0 else 0)
+        check(out[:2] + (None,), f)
+        f["V"] = 700
+        check(out[:0] + (f["loss"].float(), f["lse"].float(), out[2]), f)
+    assert torch.equal(base[0], call(h, W, targets, weights)[0])
+
+
 def test_all_padding_and_extreme_targets():
     h, W, _, weights = make(20, 300, 64, 4)
     for t in (-1, -100, 300, 511, 512, 2 ** 31 - 1, -2 ** 31):
@@ -162,6 +191,37 @@ def test_pieces_of_tokens():
     for a, b in ((0, 512), (512, 1100)):
         f = formulas(h[a:b], W, targets[a:b], weights[a:b])
         check([t[a:b] for t in out], f)
+
+
+def test_past_32_bit_offsets():
+    """Rows of h and dH behind 2^32 bytes, and words of W: as the same rows and words in calls of their own."""
+    M, V, K = 530000, 40, 4104
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, M, 100000):
+        h[i:i + 100000].normal_(generator=g)
+    W = (torch.randn(V, K, generator=g, device="cuda") * 0.05).bfloat16()
+    targets = torch.randint(0, V, (M,), generator=g, device="cuda").int()
+    out = lowra.lowra_vocab_loss(h, W, targets)
+    for a, b in ((0, 300), (M - 300, M)):
+        part = lowra.lowra_vocab_loss(h[a:b].contiguous(), W, targets[a:b].contiguous())
+        for x, y, tol in zip(out, part, (1e-5, 1e-5, 2.0 ** -7)):                     # (other tiles and splits: sums in another order)
+            assert bool(((x[a:b].double() - y.double()).abs() <= tol * (1 + y.double().abs())).all())
+    del h, out
+    V, K, M = 300000, 8192, 20
+    W = torch.empty(V, K, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, V, 50000):
+        W[i:i + 50000].normal_(std=0.01, generator=g)
+    h = torch.randn(M, K, generator=g, device="cuda").bfloat16()
+    targets = torch.tensor([V - 1 - i for i in range(M)], dtype=torch.int32, device="cuda")
+    loss, lse, dH = lowra.lowra_vocab_loss(h, W, targets)
+    z = torch.cat([h.double() @ W[i:i + 20000].double().T for i in range(0, V, 20000)], 1)
+    ref = torch.logsumexp(z, 1)
+    assert float((lse.double() - ref).abs().max()) <= 1e-4 and float((loss.double() - (ref - z[torch.arange(M), targets.long()])).abs().max()) <= 1e-4
+    p = torch.exp(z - ref[:, None])
+    p[torch.arange(M), targets.long()] -= 1
+    want = sum(p[:, i:i + 20000] @ W[i:i + 20000].double() for i in range(0, V, 20000))
+    assert float((dH.double() - want).norm() / want.norm()) <= 2.0 ** -8
 
 
 def test_workspace_of_anything_and_guards():
