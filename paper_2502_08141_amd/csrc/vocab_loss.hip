@@ -44,7 +44,7 @@ struct LossParams {
     LossStat* stats;                                     // [tiles][M]
     float* zt;                                           // [M]
     uint32_t* drop;                                      // [tiles][M]: exponents below the token's scale, as both halves' bits
-    uint32_t* uneven;                                    // [M / 64]: some token of these has such a tile
+    uint32_t* uneven;                                    // [M / 16]: some token of these has such a tile
     float2* rows;                                        // [M]: weight / sum, weight (p_t - 1)
     uint16_t* P;                                         // [M][VP]
     float* part;                                         // [splits][M][K]
@@ -261,33 +261,39 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
     }
 }
 
-// ---- 64 tokens a workgroup, a lane each; the tiles dealt to sixteen wavefronts
+// ---- 16 tokens a workgroup, the tiles dealt to 64 threads each (64 tokens and 16 threads: 777 tokens of 197 tiles 9.8 us)
+constexpr int ROWS_TOKENS = 16;
 __global__ __launch_bounds__(1024) void loss_rows_kernel(LossParams p) {
-    __shared__ float join[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = blockIdx.x * 64 + lane, at = min(m, p.M - 1);
+    __shared__ float join[16][ROWS_TOKENS];
+    const int tok = threadIdx.x % ROWS_TOKENS, group = threadIdx.x / ROWS_TOKENS, wave = threadIdx.x >> 6, m = blockIdx.x * ROWS_TOKENS + tok, at = min(m, p.M - 1);
+    const bool first = (threadIdx.x & 63) < ROWS_TOKENS;
     float most = kLeast * kLog2e;
-#pragma unroll 8
-    for (int i = wave; i < p.tiles; i += 16) most = fmaxf(most, p.stats[(size_t)i * p.M + at].shift);
-    join[wave][lane] = most;
+#pragma unroll 4
+    for (int i = group; i < p.tiles; i += 64) most = fmaxf(most, p.stats[(size_t)i * p.M + at].shift);
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    if (first) join[wave][tok] = most;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 16; ++w) most = fmaxf(most, join[w][lane]);
+    for (int w = 0; w < 16; ++w) most = fmaxf(most, join[w][tok]);
     __syncthreads();
     float others = 0.0f;
     bool uneven = false;
-#pragma unroll 8
-    for (int i = wave; i < p.tiles; i += 16) {
+#pragma unroll 4
+    for (int i = group; i < p.tiles; i += 64) {
         const LossStat st = p.stats[(size_t)i * p.M + at];
         others += ldexpf(st.sum, (int)fmaxf(st.shift - most, -1000.0f));      // (2^-128 by itself is none in fp32)
         // an exponential times 2^-d: bf16 has its exponent from bit 7 on, and 255 leaves nothing of any
         uneven = uneven || st.shift != most;
         if (p.drop && m < p.M) p.drop[(size_t)i * p.M + m] = ((uint32_t)fminf(most - st.shift, 255.0f) << 7) * 0x10001u;
     }
-    join[wave][lane] = others;
+    others += __shfl_xor(others, 16);
+    others += __shfl_xor(others, 32);
+    if (first) join[wave][tok] = others;
     const int any = __syncthreads_or(uneven);
     if (p.uneven && threadIdx.x == 0) p.uneven[blockIdx.x] = (uint32_t)(any != 0);
-    if (wave != 0 || m >= p.M) return;
-    for (int w = 1; w < 16; ++w) others += join[w][lane];
+    if (threadIdx.x >= ROWS_TOKENS || m >= p.M) return;
+    for (int w = 1; w < 16; ++w) others += join[w][tok];
     const int t = p.targets[m];
     const bool there = t >= 0 && t < p.V;
     const float xt = there ? __builtin_fmaf(p.zt[m], kLog2e, -most) : -INFINITY, et = exp2f(xt), total = others + et, log_total = logf(total);
@@ -336,7 +342,7 @@ __global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
     const uint32_t off_d = (uint32_t)min(m0 + wave * 64 + lane, p.M - 1) * 4u;
     const int per = (1 << p.tile_shift) / DEPTH - 1;     // of a tile's steps the first has none of these bits
     bool scaled = false;                                 // uniform
-    for (int i = m0 / 64; i <= (min(m0 + TOKENS, p.M) - 1) / 64; ++i) scaled = scaled || p.uneven[i] != 0;
+    for (int i = m0 / ROWS_TOKENS; i <= (min(m0 + TOKENS, p.M) - 1) / ROWS_TOKENS; ++i) scaled |= p.uneven[i] != 0;
     scaled = __builtin_amdgcn_readfirstlane(scaled);
     auto fetch = [&](int s, int i) __attribute__((always_inline)) {
         const uint32_t stage = smem_lds + (uint32_t)(s % STAGES) * S::STAGE;
@@ -449,7 +455,7 @@ constexpr size_t kLossPart = (size_t)64 << 20;           // bytes of the second 
 // Lower tiles cost more per token, but leave less of a round empty.
 struct TileCost { int tokens; double fixed, step; };
 constexpr TileCost kLogitsCost[] = {{256, 11.0, 1.48}, {192, 8.0, 1.20}, {128, 6.0, 0.93}, {64, 3.0, 0.62}};
-constexpr TileCost kGradCost[] = {{256, 10.0, 1.55}, {192, 7.0, 1.23}, {128, 4.0, 1.03}, {64, 2.0, 0.78}};
+constexpr TileCost kGradCost[] = {{256, 10.0, 1.55}, {192, 7.0, 1.23}, {128, 4.0, 1.08}, {64, 2.0, 0.78}};
 
 struct LossPlan {
     int tokens, shift, tiles, VP, rows, grad_tokens, splits, words;      // rows: tokens a piece
@@ -472,7 +478,7 @@ LossPlan loss_plan(int M, int V, int K, bool grad) {
         const double t = rounds((long long)((l.rows + c.tokens - 1) / c.tokens) * l.tiles) * (c.fixed + c.step * ((K + DEPTH - 1) / DEPTH));
         if (l.rows <= 64 ? c.tokens == 64 : t < least) { least = t; l.tokens = c.tokens; }
     }
-    // The second product has few tiles, so that its words are split between workgroups, whose sums are written and read once more (at 4 MB a microsecond).
+    // The second product has few tiles, so that its words are split between workgroups, whose sums are written and read once more (3.3 MB of them a microsecond).
     const size_t out_bytes = (size_t)l.rows * K * 4;
     const int most = (int)std::min<size_t>(std::min(l.tiles, 64), kLossPart / out_bytes + 1);
     least = 1e300;
@@ -480,7 +486,7 @@ LossPlan loss_plan(int M, int V, int K, bool grad) {
         const long long out_tiles = (long long)((l.rows + c.tokens - 1) / c.tokens) * ((K + 255) / 256);
         for (int splits = 1; splits <= most; ++splits) {
             const int words = ((l.tiles + splits - 1) / splits) << l.shift;
-            const double t = rounds(out_tiles * splits) * (c.fixed + c.step * (words / DEPTH)) + (double)splits * (double)out_bytes / 2e6;
+            const double t = rounds(out_tiles * splits) * (c.fixed + c.step * (words / DEPTH)) + (double)splits * (double)out_bytes / 3.3e6;
             if (t < least) { least = t; l.grad_tokens = c.tokens; l.words = words; }
         }
     }
@@ -490,7 +496,7 @@ LossPlan loss_plan(int M, int V, int K, bool grad) {
     l.zt0 = take((size_t)l.rows * 4);
     if (grad) {
         l.drop0 = take((size_t)l.rows * l.tiles * 4);
-        l.uneven0 = take((size_t)(l.rows + 63) / 64 * 4);
+        l.uneven0 = take((size_t)(l.rows + ROWS_TOKENS - 1) / ROWS_TOKENS * 4);
         l.rows0 = take((size_t)l.rows * 8);
         l.part0 = take((size_t)l.splits * out_bytes);
         l.P0 = take((size_t)l.rows * l.VP * 2);
@@ -542,7 +548,7 @@ hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t st) {
         else if (l.tokens == 128) e = launch_logits<4, 2, 2, 3>(p, st);
         else e = launch_logits<4, 2, 1, 3>(p, st);
         if (e != hipSuccess) return e;
-        loss_rows_kernel<<<dim3((unsigned)((p.M + 63) / 64)), dim3(1024), 0, st>>>(p);
+        loss_rows_kernel<<<dim3((unsigned)((p.M + ROWS_TOKENS - 1) / ROWS_TOKENS)), dim3(1024), 0, st>>>(p);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (!grad) continue;
         if (l.grad_tokens == 256) e = launch_grad<4, 2>(p, st);
