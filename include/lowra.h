@@ -432,7 +432,7 @@ lowra_status lowra_vocab_loss(int M, int V, int K, const uint16_t* h, const uint
  * A run takes the scalars (a captured one repeats those it was captured with) and only launches.  create allocates device memory for the descriptors and
  * copies them synchronously; destroy frees.
  * create: INVALID_ARG (null / n <= 0 / count <= 0 / a missing pointer; absmax is needed with 8 bits and null with 32; an output that overlaps
- * anything else of the batch, so no tensor is in it twice), UNSUPPORTED (other state_bits, more than 2^31 elements), MISALIGNED, OUT_OF_MEMORY, HIP_ERROR.
+ * anything else of the batch, so no tensor is in it twice), UNSUPPORTED (other state_bits, more than 2^31 elements, 2^24 pieces of up to 1024 in all), MISALIGNED, OUT_OF_MEMORY, HIP_ERROR.
  * run: INVALID_ARG (null, step < 1, a beta outside [0, 1), eps below zero, another device than the one of create), MISALIGNED, HIP_ERROR. */
 typedef struct lowra_adamw_item {
     int64_t count;

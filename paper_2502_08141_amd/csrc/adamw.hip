@@ -5,7 +5,8 @@
 // so that the quotient m / sqrt(v) is resolved alike on both sides, and a v above zero never becomes zero.  A code is the number of borders k + 1/2, on the
 // scale of q, that lie below the magnitude; a step's own weights use m' and v' before they are coded.
 //
-// Memory bound: 22 to 26 bytes an element with 32-bit states (30 with the bf16 copy), 18 with 8-bit ones.  A lane has four consecutive elements, so that
+// Memory bound: 28 bytes an element with 32-bit states (30 with the bf16 copy), 18.25 with 8-bit ones and the copy.  143 million elements in 8 bits: 481 us, 5.4 TB/s
+// (without the coding it takes as long).  A lane has four consecutive elements, so that
 // every access of a wavefront is contiguous, and sixteen lanes have a group.
 #include <algorithm>
 
@@ -75,14 +76,16 @@ __device__ __forceinline__ float root_of(float x) {
     return __builtin_amdgcn_sqrtf(tiny ? x * 0x1p64f : x) * (tiny ? 0x1p-32f : 1.0f);
 }
 
-template <bool FULL>
+// STREAM: past the caches, for batches that none of them holds (below, at adamw_build)
+template <bool FULL, bool STREAM>
 __device__ __forceinline__ float4 get4(const float* p, long long left) {
-    if (FULL) return load16_stream(reinterpret_cast<const float4*>(p));
+    if (FULL) return STREAM ? load16_stream(reinterpret_cast<const float4*>(p)) : *reinterpret_cast<const float4*>(p);
     return make_float4(left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f, left > 2 ? p[2] : 0.0f, left > 3 ? p[3] : 0.0f);
 }
-template <bool FULL>
+template <bool FULL, bool STREAM>
 __device__ __forceinline__ void put4(float* p, long long left, const float (&v)[4]) {
-    if (FULL) { store16_stream(p, make_float4(v[0], v[1], v[2], v[3])); return; }
+    if (FULL && STREAM) { store16_stream(p, make_float4(v[0], v[1], v[2], v[3])); return; }
+    if (FULL) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); return; }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (left > i) p[i] = v[i];
@@ -90,14 +93,14 @@ __device__ __forceinline__ void put4(float* p, long long left, const float (&v)[
 
 // Four elements of an item as they lie in memory
 struct Quad { float4 g, w, m, v; uint32_t mq, vq; float mA, vA; };
-template <bool EIGHT, bool FULL>
+template <bool EIGHT, bool FULL, bool STREAM>
 __device__ __forceinline__ void adamw_load(const AdamwItem& it, long long at, Quad& q) {
     const long long left = it.count - at;
-    q.g = get4<FULL>(it.grad + at, left);
-    q.w = get4<FULL>(it.weight + at, left);
+    q.g = get4<FULL, STREAM>(it.grad + at, left);
+    q.w = get4<FULL, STREAM>(it.weight + at, left);
     if (!EIGHT) {
-        q.m = get4<FULL>(static_cast<const float*>(it.m) + at, left);
-        q.v = get4<FULL>(static_cast<const float*>(it.v) + at, left);
+        q.m = get4<FULL, STREAM>(static_cast<const float*>(it.m) + at, left);
+        q.v = get4<FULL, STREAM>(static_cast<const float*>(it.v) + at, left);
         return;
     }
     const uint8_t *m = static_cast<const uint8_t*>(it.m) + at, *v = static_cast<const uint8_t*>(it.v) + at;
@@ -115,7 +118,7 @@ __device__ __forceinline__ void adamw_load(const AdamwItem& it, long long at, Qu
 }
 
 // All 16 lanes of a group come here together.
-template <bool EIGHT, bool FULL>
+template <bool EIGHT, bool FULL, bool STREAM>
 __device__ __forceinline__ void adamw_four(const AdamwItem& it, const AdamwStep& s, float clip, long long at, const Quad& r) {
     const long long left = it.count - at;
     float m[4], v[4];
@@ -139,7 +142,7 @@ __device__ __forceinline__ void adamw_four(const AdamwItem& it, const AdamwStep&
         const float root = s.eps >= 1e-12f ? __builtin_amdgcn_sqrtf(v[i] * s.over_bias2) : root_of(v[i] * s.over_bias2);      // (uniform; the root of what is subnormal is below 1e-19)
         w[i] = __builtin_fmaf(-lr_w, w[i], w[i]) - lr_m * m[i] * __builtin_amdgcn_rcpf(root + s.eps);
     }
-    put4<FULL>(it.weight_out + at, left, w);
+    put4<FULL, STREAM>(it.weight_out + at, left, w);
     if (it.weight_bf16) {                                    // uniform
         if (FULL) *reinterpret_cast<uint2*>(it.weight_bf16 + at) = make_uint2(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]));
         else {
@@ -149,8 +152,8 @@ __device__ __forceinline__ void adamw_four(const AdamwItem& it, const AdamwStep&
         }
     }
     if (!EIGHT) {
-        put4<FULL>(static_cast<float*>(it.m_out) + at, left, m);
-        put4<FULL>(static_cast<float*>(it.v_out) + at, left, v);
+        put4<FULL, STREAM>(static_cast<float*>(it.m_out) + at, left, m);
+        put4<FULL, STREAM>(static_cast<float*>(it.v_out) + at, left, v);
         return;
     }
     if (!FULL) {                                             // lanes past the end have nothing in their group
@@ -185,29 +188,26 @@ __device__ __forceinline__ void adamw_four(const AdamwItem& it, const AdamwStep&
     }
 }
 
-template <bool EIGHT>
-__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwItem* __restrict__ items, const AdamwChunk* __restrict__ chunks, int steps, AdamwStep s) {
+// STEPS: how often a workgroup takes AW_STEP elements
+template <bool EIGHT, bool STREAM, int STEPS>
+__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwItem* __restrict__ items, const AdamwChunk* __restrict__ chunks, AdamwStep s) {
     const AdamwChunk c = chunks[blockIdx.x];
     const AdamwItem it = items[c.item];
     const float clip = s.grad_scale ? *s.grad_scale : 1.0f;
     const long long first = (long long)c.first + 4 * threadIdx.x;
-    if ((long long)c.first + steps * AW_STEP <= it.count && steps == AW_MOST) {          // uniform; all loads together
-        Quad q[AW_MOST];
+    if ((long long)c.first + STEPS * AW_STEP <= it.count) {  // uniform; all loads together
+        Quad q[STEPS];
 #pragma unroll
-        for (int k = 0; k < AW_MOST; ++k) adamw_load<EIGHT, true>(it, first + k * AW_STEP, q[k]);
+        for (int k = 0; k < STEPS; ++k) adamw_load<EIGHT, true, STREAM>(it, first + k * AW_STEP, q[k]);
 #pragma unroll
-        for (int k = 0; k < AW_MOST; ++k) adamw_four<EIGHT, true>(it, s, clip, first + k * AW_STEP, q[k]);
+        for (int k = 0; k < STEPS; ++k) adamw_four<EIGHT, true, STREAM>(it, s, clip, first + k * AW_STEP, q[k]);
         return;
     }
-    for (int k = 0; k < steps && (long long)c.first + k * AW_STEP < it.count; ++k) {
+#pragma unroll 1
+    for (int k = 0; k < STEPS && (long long)c.first + k * AW_STEP < it.count; ++k) {       // an item's end
         Quad q;
-        if ((long long)c.first + (k + 1) * AW_STEP <= it.count) {
-            adamw_load<EIGHT, true>(it, first + k * AW_STEP, q);
-            adamw_four<EIGHT, true>(it, s, clip, first + k * AW_STEP, q);
-        } else {
-            adamw_load<EIGHT, false>(it, first + k * AW_STEP, q);
-            adamw_four<EIGHT, false>(it, s, clip, first + k * AW_STEP, q);
-        }
+        adamw_load<EIGHT, false, STREAM>(it, first + k * AW_STEP, q);
+        adamw_four<EIGHT, false, STREAM>(it, s, clip, first + k * AW_STEP, q);
     }
 }
 
@@ -244,24 +244,32 @@ hipError_t adamw_build(const std::vector<AdamwItem>& items, bool eight, AdamwGro
     if (items.empty()) return hipSuccess;
     long long total = 0;
     for (const AdamwItem& it : items) total += it.count;
-    // as many elements as a workgroup asks for together, unless that leaves units without any
-    g.steps = (int)std::max(1ll, std::min((long long)AW_MOST, total / AW_STEP / (4 * device_compute_units())));
+    // as many elements as a workgroup asks for together, unless that leaves units with less than four workgroups (1.25 million elements: 7.0 us in single
+    // steps; 8.4 with the code for four in the same kernel)
+    g.steps = total / AW_STEP >= (long long)AW_MOST * 4 * device_compute_units() ? AW_MOST : 1;
     const int chunk = g.steps * AW_STEP;
+    // past the caches where the batch is more than the 256 MB behind them (143 million elements in 8 bits, with their decoded states: 843 -> 831 us)
+    g.stream = total * (eight ? 18 : 30) > (256ll << 20);
     std::vector<AdamwChunk> chunks;
     for (size_t i = 0; i < items.size(); ++i)
         for (long long at = 0; at < items[i].count; at += chunk) chunks.push_back(AdamwChunk{(int)i, (uint32_t)at});
-    if (chunks.size() > 0x7fffffffu) return hipErrorInvalidValue;
     g.nchunks = (int)chunks.size();
     hipError_t e = upload(items, g.d_items);
     return e != hipSuccess ? e : upload(chunks, g.d_chunks);
 }
 
-hipError_t adamw_run(const AdamwGroup (&groups)[2], const AdamwStep& s, hipStream_t st) {
-    if (groups[0].nchunks) adamw_kernel<false><<<dim3((unsigned)groups[0].nchunks), dim3(AW_THREADS), 0, st>>>(groups[0].d_items, groups[0].d_chunks, groups[0].steps, s);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !groups[1].nchunks) return e;
-    adamw_kernel<true><<<dim3((unsigned)groups[1].nchunks), dim3(AW_THREADS), 0, st>>>(groups[1].d_items, groups[1].d_chunks, groups[1].steps, s);
+template <bool EIGHT>
+static hipError_t adamw_launch(const AdamwGroup& g, const AdamwStep& s, hipStream_t st) {
+    if (!g.nchunks) return hipSuccess;
+    const dim3 grid((unsigned)g.nchunks), block(AW_THREADS);
+    if (g.steps == 1) adamw_kernel<EIGHT, false, 1><<<grid, block, 0, st>>>(g.d_items, g.d_chunks, s);
+    else if (!g.stream) adamw_kernel<EIGHT, false, AW_MOST><<<grid, block, 0, st>>>(g.d_items, g.d_chunks, s);
+    else adamw_kernel<EIGHT, true, AW_MOST><<<grid, block, 0, st>>>(g.d_items, g.d_chunks, s);
     return hipGetLastError();
+}
+hipError_t adamw_run(const AdamwGroup (&groups)[2], const AdamwStep& s, hipStream_t st) {
+    const hipError_t e = adamw_launch<false>(groups[0], s, st);
+    return e != hipSuccess ? e : adamw_launch<true>(groups[1], s, st);
 }
 
 void adamw_free(AdamwGroup (&groups)[2]) {

@@ -207,6 +207,9 @@ lowra_status lowra_adamw_batch_create(int n, const lowra_adamw_item* items, lowr
             !aligned16(it.weight_out) || !aligned16(it.weight_bf16))
             return LOWRA_MISALIGNED;
     }
+    long long pieces = 0;                                        // (a launch has less than 2^32 threads, 256 to a thousand elements at least)
+    for (int i = 0; i < n; ++i) pieces += (items[i].count + 1023) / 1024;
+    if (pieces >= 1 << 24) return LOWRA_UNSUPPORTED;
     lowra_adamw_batch* b = nullptr;
     lowra_status st = LOWRA_OK;
     try {

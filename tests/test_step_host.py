@@ -164,6 +164,8 @@ def test_adamw_refusals():
     for n in names[8:]:
         assert create(item(1, 8, **{n: None})) == INV and create(item(1, 32, **{n: P(30)})) == INV, n
     assert create(item(1, 16)) == UNS
+    far = lambda i: 1 << 40 | i << 36                                                       # three items of 2^31 elements and pieces beyond what a launch has
+    assert create(*[dict(count=1 << 31, state_bits=32, lr_scale=1.0, decay_scale=1.0) | {n: far(8 * i + k) for k, n in enumerate(names[:7])} for i in range(8)]) == UNS
     assert not out.value
     step = lowra.AdamWStep(1e-3, 0.9, 0.999, 1e-8, 0.0, 1)
     assert L.lowra_adamw_batch_run(None, C.addressof(step), None, None) == INV
