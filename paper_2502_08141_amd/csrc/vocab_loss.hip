@@ -8,7 +8,7 @@
 // than 2^-94 of the largest may be lost.  A pass over these numbers gives loss and lse, and
 // how far each tile's n is below the token's largest.  The second product multiplies the exponentials with W.  Where tiles of a token differ in n,
 // it brings them to the token's scale on the way into the matrix unit, a subtraction from their exponents and exact; for tokens whose n are all the same
-// it has a loop without (4096 x 32000 x 4096: 895 us with the subtraction, 818 without; a pass over the exponentials before it 90).  The token's factor
+// it has a loop without (4096 x 32000 x 4096 by itself: 895 us with the subtraction, 818 without; a pass over the exponentials before it 90).  The token's factor
 // weight / sum meets the fp32 sums.  So a probability is rounded once, to bf16.  The target's own term, weight (p_t - 1) W_t, is added in fp32: p_t is near
 // one for most tokens of a trained model, and its rounding would be the gradient's error.  p_t - 1 and the loss come from the sum without the target, so
 // that they keep their digits there.
@@ -51,8 +51,8 @@ struct LossParams {
     int splits, words_per_split;
 };
 
-// The tile of a workgroup: runs of `group` tiles of one operand against all of the other, so that the workgroups of an L2 share both (4096 x 32768 x
-// 4096: 880 us; one operand's tiles all against two of the other's 955).
+// The tile of a workgroup: `group` tiles of one operand against all of the other in turn, so that the workgroups of an L2 share both (4096 x 32768 x 4096 by
+// itself: four or eight 884 us, one 955, with the loop as it was then).
 __device__ __forceinline__ void tile_of(int tile, int major, int minor, int group, int& a, int& b) {
     const int g = tile / (group * minor), r = tile - g * group * minor, n = min(group, major - g * group);
     a = g * group + r % n;
@@ -62,11 +62,13 @@ __device__ __forceinline__ void tile_of(int tile, int major, int minor, int grou
 template <int N>
 __device__ __forceinline__ void wait_transfers() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 
-// The steps of a product.  A step's operands are two tiles of one of STAGES stages in LDS.  fetch(s, i) asks for transfer i of T of step s (of which some steps may leave
-// out all but WT); read(s, kk, i)
-// for operand registers i of R of slice kk (16 deep) of step s; mul(kk, j) is matrix instruction j of N of a slice.  The only barrier of a step stands before its last
-// slice, when that slice's operands are in registers: the stage is free from there on for step s + STAGES, whose transfers are dealt over two slices (back to back
-// they hold up the issue: 900 -> 850 us), and step s + 1 is there, so that its first operands are read under the last slice's products.
+// The steps of a product.  A step's operands are two tiles in one of STAGES stages of LDS.  fetch(s, i) asks for transfer i of T of step s, of which some steps
+// leave out all but the first WT; read(s, kk, i) for operand registers i of R of slice kk (16 deep) of step s; mul(kk, j) is matrix instruction j of N of a slice.
+// The only barrier of a step stands before its last slice, when that slice's operands are in registers: from there on the stage is free for step s + STAGES, whose
+// transfers are dealt over two slices, and step s + 1 is there, so that its first operands are read under the last slice's products.  4096 x 32768 x 4096 by
+// itself: 838 us; a barrier and all transfers at the beginning of a step 1042, all transfers in one slice 862, in three 5 % more than in two, without the
+// priority over the other wavefront while transfers are issued 2 % more; four wavefronts with 128 x 128 outputs each 846 to 950, and 900 with the transfers in
+// one slice; two workgroups of 256 x 128 outputs a unit 1117.  The matrix units are busy for 76 % of the first product's time and 82 % of the second's.
 template <int STAGES, int T, int WT, int R, int N, class Fetch, class Read, class Mul>
 __device__ __forceinline__ void product_steps(int steps, Fetch fetch, Read read, Mul mul) {
     constexpr int H = (T + 1) / 2;                       // transfers in the first of the two slices
@@ -346,7 +348,7 @@ __global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
     scaled = __builtin_amdgcn_readfirstlane(scaled);
     auto fetch = [&](int s, int i) __attribute__((always_inline)) {
         const uint32_t stage = smem_lds + (uint32_t)(s % STAGES) * S::STAGE;
-        if (i == TP + TW) {                              // the exponents of a tile, with its first step (a transfer and four reads in every step: 818 -> 895 us)
+        if (i == TP + TW) {                              // the exponents of a tile, with its first step
             if (scaled && wave < TP && (s & per) == 0)
                 dma4_b(buffer_desc(p.drop + (size_t)((w0 + s * DEPTH) >> p.tile_shift) * p.M), off_d, stage + S::D0 + (uint32_t)wave * 256u);
         } else if (i < TP) dma16_b(src_p, off_p[i < TP ? i : 0], (uint32_t)s * (DEPTH * 2u), stage + (uint32_t)(wave * TP + i) * 1024u);
@@ -378,30 +380,30 @@ __global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
     v4i16_t fb[2][2][2];
     uint32_t drop[AT];                                   // exponents below the token's scale, of this step's tile
     auto run = [&](auto SCALED_) __attribute__((always_inline)) {
-    constexpr bool SCALED = decltype(SCALED_)::value;
-    product_steps<STAGES, TP + TW + SCALED, TP + TW, AT + 4 + (SCALED ? AT : 0), AT * 2>(
-        steps, fetch,
-        [&](int s, int kk, int i) __attribute__((always_inline)) {
-            const uint32_t st = (uint32_t)(s % STAGES) * S::STAGE;
-            if (i < AT) fa[kk & 1][i < AT ? i : 0] = *reinterpret_cast<const bf16x8_t*>(smem + st + koff[kk] + a0 + i * 32 * ROWB);
-            else if (i >= AT + 4) {
-                const int a = i < AT + 4 ? 0 : i - AT - 4;
-                if (kk == 0 && (s & per) == 0) drop[a] = *reinterpret_cast<const uint32_t*>(smem + st + S::D0 + (wm * AT * 32 + a * 32 + fi) * 4);
-            } else {
-                const int q = i < AT || i >= AT + 4 ? 0 : i - AT, b = q >> 1, e = q & 1;
-                fb[kk & 1][b][e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(uintptr_t)(smem_lds + st + tr[e][b] + kk * 16 * 512));
-            }
-        },
-        [&](int kk, int j) __attribute__((always_inline)) {
-            const int a = j >> 1, b = j & 1;
-            if (SCALED && b == 0) {                      // (an exponent that runs out leaves zero)
-                const v2u16_t d = __builtin_bit_cast(v2u16_t, drop[a]);
-                fa[kk & 1][a] = __builtin_bit_cast(bf16x8_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(v8u16_t, fa[kk & 1][a]), v8u16_t{d[0], d[1], d[0], d[1], d[0], d[1], d[0], d[1]}));
-            }
-            const v4i16_t lo = fb[kk & 1][b][0], hi = fb[kk & 1][b][1];
-            acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[kk & 1][a], __builtin_bit_cast(bf16x8_t, v8i16_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}),
-                                                                acc[a][b], 0, 0, 0);
-        });
+        constexpr bool SCALED = decltype(SCALED_)::value;
+        product_steps<STAGES, TP + TW + SCALED, TP + TW, AT + 4 + (SCALED ? AT : 0), AT * 2>(
+            steps, fetch,
+            [&](int s, int kk, int i) __attribute__((always_inline)) {
+                const uint32_t st = (uint32_t)(s % STAGES) * S::STAGE;
+                if (i < AT) fa[kk & 1][i < AT ? i : 0] = *reinterpret_cast<const bf16x8_t*>(smem + st + koff[kk] + a0 + i * 32 * ROWB);
+                else if (i >= AT + 4) {
+                    const int a = i < AT + 4 ? 0 : i - AT - 4;
+                    if (kk == 0 && (s & per) == 0) drop[a] = *reinterpret_cast<const uint32_t*>(smem + st + S::D0 + (wm * AT * 32 + a * 32 + fi) * 4);
+                } else {
+                    const int q = i < AT || i >= AT + 4 ? 0 : i - AT, b = q >> 1, e = q & 1;
+                    fb[kk & 1][b][e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(uintptr_t)(smem_lds + st + tr[e][b] + kk * 16 * 512));
+                }
+            },
+            [&](int kk, int j) __attribute__((always_inline)) {
+                const int a = j >> 1, b = j & 1;
+                if (SCALED && b == 0) {                      // (an exponent that runs out leaves zero)
+                    const v2u16_t d = __builtin_bit_cast(v2u16_t, drop[a]);
+                    fa[kk & 1][a] = __builtin_bit_cast(bf16x8_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(v8u16_t, fa[kk & 1][a]), v8u16_t{d[0], d[1], d[0], d[1], d[0], d[1], d[0], d[1]}));
+                }
+                const v4i16_t lo = fb[kk & 1][b][0], hi = fb[kk & 1][b][1];
+                acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[kk & 1][a], __builtin_bit_cast(bf16x8_t, v8i16_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}),
+                                                                    acc[a][b], 0, 0, 0);
+            });
     };
     if (scaled) run(std::true_type{});
     else run(std::false_type{});
