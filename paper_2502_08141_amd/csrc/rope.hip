@@ -5,7 +5,8 @@
 // Memory bound: 2 bytes in and 2 out per element.  The angle is position x turns mod 2^64 in whole numbers, 2^-64 of a full turn a unit: exact
 // at any position, where fp32 is off by 0.03 at 2^20 and a table of cosines would be read beside the data.  What is left is at most an eighth of a turn, where
 // the Taylor polynomials of degree 9 and 10 are exact to fp32 rounding (remainders pi/4^11 / 11! = 2e-9 and pi/4^12 / 12! = 1e-10).  A thread keeps
-// the angles of its columns for several heads.
+// the angles of its columns for several heads.  Graph replays: 4096 tokens of 32 + 32 heads of 128 columns 22.8 us (5.9 TB/s), 32 + 8 heads of neighbours 15.4,
+// four tokens of 32 + 8 heads 3.2.
 #include <algorithm>
 
 #include "gemm_common.h"
