@@ -235,7 +235,8 @@ __global__ __launch_bounds__(64 * W * G, C <= 2 ? 4 : 2) void norm_bwd_kernel(No
     }
 }
 
-// 32 columns a workgroup, the chunks dealt to 32 groups of threads, each with up to eight loads under way; blockIdx.y: dweight, dbias
+// 32 columns a workgroup, a cache line of each chunk, the chunks dealt to 32 groups of threads, each with up to eight loads under way; blockIdx.y: dweight, dbias
+// (4096 x 4096 rms with residual, both launches: 29.0 us; 16 columns 30.1, 64 29.6)
 __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* __restrict__ sums, int chunks, int N, float* dweight, float* dbias) {
     __shared__ float red[32][33];
     float* out = blockIdx.y ? dbias : dweight;

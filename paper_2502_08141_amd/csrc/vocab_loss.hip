@@ -5,17 +5,17 @@
 // does not depend on the other words: per token a whole number n not far from log2 e times the tile's largest z, the sum of 2^(z log2 e - n) over the words but
 // the target, z_t where the tile has it, and, for the gradient, the exponentials themselves in bf16 (the target's as zero).  fp32 and bf16 reach from
 // 2^-126 to 2^127, so n is zero where the largest is between 2^-32 and 2^64 (z from -22 to 44) and the multiple of 64 below elsewhere; what is less
-// than 2^-94 of the largest may be lost.  A pass over these numbers gives loss and lse, and
-// how far each tile's n is below the token's largest.  The second product multiplies the exponentials with W.  Where tiles of a token differ in n,
-// it brings them to the token's scale on the way into the matrix unit, a subtraction from their exponents and exact; for tokens whose n are all the same
-// it has a loop without (4096 x 32000 x 4096 by itself: 895 us with the subtraction, 818 without; a pass over the exponentials before it 90).  The token's factor
+// than 2^-94 of the largest may be lost.  A small pass over these numbers gives loss and lse.  The second product multiplies the exponentials with W and
+// does not wait for that pass, whose workgroups stand behind its own.  Where n is not zero for every tile and every token with a target, it takes the tokens' largest n
+// first and brings a tile's exponentials to that scale on the way into the matrix unit, a subtraction from their exponents and exact; else its loop is without
+// (4096 x 32000 x 4096 by itself: 895 us with the subtraction, 818 without; a pass over the exponentials before it 90).  The token's factor
 // weight / sum meets the fp32 sums.  So a probability is rounded once, to bf16.  The target's own term, weight (p_t - 1) W_t, is added in fp32: p_t is near
 // one for most tokens of a trained model, and its rounding would be the gradient's error.  p_t - 1 and the loss come from the sum without the target, so
 // that they keep their digits there.
 // Tokens go in pieces whose exponentials fit kLossPiece bytes, so that neither the logits nor anything else of size M x V is ever there at once.
 // (Pieces of the vocabulary would have to form z a second time for the gradient: 6 M V K operations in place of 4.)
 // Graph replays: 4096 tokens of 32000 words, K 4096, 1636 to 1674 us by the card (1.28 to 1.31 PFLOP/s; the matrix unit busy for 76 % of the first product and 82 % of the
-// second), 777 of 50265, K 1024, 220; 333 of 32000 without the gradient 121, of which W from memory is 44; 19 of 1003, K 512, 17.8, four launches' latencies.
+// second), 777 of 50265, K 1024, 220; 333 of 32000 without the gradient 121, of which W from memory is 44; 19 of 1003, K 512, 14.6, three launches' latencies.
 #include <algorithm>
 
 #include "gemm_common.h"
@@ -45,12 +45,13 @@ struct LossParams {
     int M, V, K, VP, tiles, tile_shift;                  // this piece's tokens; VP: words in whole tiles of 2^tile_shift
     LossStat* stats;                                     // [tiles][M]
     float* zt;                                           // [M]
-    uint32_t* drop;                                      // [tiles][M]: exponents below the token's scale, as both halves' bits
-    uint32_t* uneven;                                    // [M / 16]: some token of these has such a tile
+    uint32_t* apart;                                     // [M / apart_tokens][tiles]: a target's token of these has a shift that is not zero
+    int apart_tokens;
     float2* rows;                                        // [M]: weight / sum, weight (p_t - 1)
     uint16_t* P;                                         // [M][VP]
     float* part;                                         // [splits][M][K]
     int splits, words_per_split;
+    bool rows_inside;                                    // the tokens' numbers come with the second product's launch
 };
 
 // The tile of a workgroup: `group` tiles of one operand against all of the other in turn, so that the workgroups of an L2 share both (4096 x 32768 x 4096 by
@@ -187,6 +188,7 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
                 }
     }
     float shift[BT], sum[BT];
+    bool there[BT];
 #pragma unroll
     for (int b = 0; b < BT; ++b) {
         float most = kLeast;
@@ -199,6 +201,7 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
         // the target leaves the sum
         const int m = m0 + t0 + 32 * b;
         const uint32_t target = m < p.M ? (uint32_t)p.targets[m] : ~0u, mine = target < (uint32_t)p.V ? target - (uint32_t)(v0 + w0) : ~0u;
+        there[b] = target < (uint32_t)p.V;
         if (__any(mine < AT * 32)) {
 #pragma unroll
             for (int a = 0; a < AT; ++a)
@@ -218,6 +221,14 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
         for (int w = 1; w < WV; ++w) most = fmaxf(most, join[w][t0 + 32 * b]);
         const float n = most * kLog2e;
         shift[b] = n >= -32.0f && n <= 64.0f ? 0.0f : 64.0f * floorf(n * (1.0f / 64.0f));
+    }
+    if (p.P && wv == 0) {                                // uniform
+        bool apart = false;
+#pragma unroll
+        for (int b = 0; b < BT; ++b) apart |= there[b] && shift[b] != 0.0f;
+        const int of = mt * (WAVES / WV) + wt;
+        const bool any = __any(apart);
+        if (lane == 0 && of * (BT * 32) < p.M) p.apart[(size_t)of * p.tiles + vt] = any;
     }
     __syncthreads();
 #pragma unroll
@@ -265,38 +276,40 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
     }
 }
 
-// ---- 16 tokens a workgroup, the tiles dealt to 64 threads each (64 tokens and 16 threads: 777 tokens of 197 tiles 9.8 us)
+// ---- loss, lse and what the gradient needs of a token, 16 tokens a workgroup, the tiles dealt to 64 groups of threads (16 groups and 64 tokens: 777 tokens of 197 tiles
+// 9.8 us for 7.4).  N wavefronts: 16, or 8 that have two groups' sums each, so that the order is the same.
 constexpr int ROWS_TOKENS = 16;
-__global__ __launch_bounds__(1024) void loss_rows_kernel(LossParams p) {
-    __shared__ float join[16][ROWS_TOKENS];
-    const int tok = threadIdx.x % ROWS_TOKENS, group = threadIdx.x / ROWS_TOKENS, wave = threadIdx.x >> 6, m = blockIdx.x * ROWS_TOKENS + tok, at = min(m, p.M - 1);
+template <int N>
+__device__ __forceinline__ void loss_rows(const LossParams& p, int block, float (*join)[ROWS_TOKENS]) {
+    constexpr int SETS = 16 / N;
+    const int tok = threadIdx.x % ROWS_TOKENS, group = threadIdx.x / ROWS_TOKENS, wave = threadIdx.x >> 6, m = block * ROWS_TOKENS + tok, at = min(m, p.M - 1);
     const bool first = (threadIdx.x & 63) < ROWS_TOKENS;
     float most = kLeast * kLog2e;
 #pragma unroll 4
-    for (int i = group; i < p.tiles; i += 64) most = fmaxf(most, p.stats[(size_t)i * p.M + at].shift);
+    for (int i = group; i < p.tiles; i += 4 * N) most = fmaxf(most, p.stats[(size_t)i * p.M + at].shift);
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
     if (first) join[wave][tok] = most;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 16; ++w) most = fmaxf(most, join[w][tok]);
+    for (int w = 0; w < N; ++w) most = fmaxf(most, join[w][tok]);
     __syncthreads();
     float others = 0.0f;
-    bool uneven = false;
+#pragma unroll
+    for (int q = 0; q < SETS; ++q) {
+        others = 0.0f;
 #pragma unroll 4
-    for (int i = group; i < p.tiles; i += 64) {
-        const LossStat st = p.stats[(size_t)i * p.M + at];
-        others += ldexpf(st.sum, (int)fmaxf(st.shift - most, -1000.0f));      // (2^-128 by itself is none in fp32)
-        // an exponential times 2^-d: bf16 has its exponent from bit 7 on, and 255 leaves nothing of any
-        uneven = uneven || st.shift != most;
-        if (p.drop && m < p.M) p.drop[(size_t)i * p.M + m] = ((uint32_t)fminf(most - st.shift, 255.0f) << 7) * 0x10001u;
+        for (int i = group + 4 * N * q; i < p.tiles; i += 64) {
+            const LossStat st = p.stats[(size_t)i * p.M + at];
+            others += ldexpf(st.sum, (int)fmaxf(st.shift - most, -1000.0f));      // (2^-128 by itself is none in fp32)
+        }
+        others += __shfl_xor(others, 16);
+        others += __shfl_xor(others, 32);
+        if (first) join[N * q + wave][tok] = others;
     }
-    others += __shfl_xor(others, 16);
-    others += __shfl_xor(others, 32);
-    if (first) join[wave][tok] = others;
-    const int any = __syncthreads_or(uneven);
-    if (p.uneven && threadIdx.x == 0) p.uneven[blockIdx.x] = (uint32_t)(any != 0);
+    __syncthreads();
     if (threadIdx.x >= ROWS_TOKENS || m >= p.M) return;
+    others = join[0][tok];
     for (int w = 1; w < 16; ++w) others += join[w][tok];
     const int t = p.targets[m];
     const bool there = t >= 0 && t < p.V;
@@ -309,13 +322,17 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(LossParams p) {
         p.rows[m] = make_float2(w / total, -w * (others / total));
     }
 }
+__global__ __launch_bounds__(1024) void loss_rows_kernel(LossParams p) {
+    __shared__ float join[16][ROWS_TOKENS];
+    loss_rows<16>(p, blockIdx.x, join);
+}
 
 // ---- second product, over a run of words: tokens (the exponentials) are the matrix instruction's rows, features its columns, W's operand read across its rows
 // (ds_read_b64_tr_b16).  2 x 4 wavefronts, each with AT x 2 tiles of 32 tokens x 32 features.
 __device__ __forceinline__ int wswz(int row, int c) { return row * 512 + ((c ^ (((row & 3) << 2) | ((row >> 2) & 3))) << 4); }
 template <int AT, int STAGES>
 struct Grad {
-    static constexpr int TOKENS = 2 * AT * 32, W0 = TOKENS * ROWB, D0 = W0 + DEPTH * 512, STAGE = D0 + TOKENS * 4, SMEM = STAGES * STAGE;      // tokens', words' rows, exponents
+    static constexpr int TOKENS = 2 * AT * 32, W0 = TOKENS * ROWB, D0 = W0 + DEPTH * 512, STAGE = D0 + TOKENS * 4, SMEM = STAGES * STAGE;      // tokens', words' rows, shifts
 };
 template <int AT, int STAGES>
 __global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
@@ -325,7 +342,9 @@ __global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
     const uint32_t smem_lds = (uint32_t)(uintptr_t)(lptr_t)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tiles_k = (p.K + 255) / 256, tiles_m = (p.M + TOKENS - 1) / TOKENS;
-    const int work = xcd_tile(blockIdx.x, gridDim.x), split = __builtin_amdgcn_readfirstlane(work / (tiles_k * tiles_m));
+    const int tiles = tiles_k * tiles_m * p.splits;
+    if ((int)blockIdx.x >= tiles) { loss_rows<WAVES>(p, blockIdx.x - tiles, reinterpret_cast<float(*)[ROWS_TOKENS]>(smem)); return; }
+    const int work = xcd_tile(blockIdx.x, tiles), split = __builtin_amdgcn_readfirstlane(work / (tiles_k * tiles_m));
     int mt, kt;
     tile_of(work - split * (tiles_k * tiles_m), tiles_m, tiles_k, 4, mt, kt);
     const int k0 = kt * 256, m0 = mt * TOKENS, w0 = split * p.words_per_split, steps = (min(w0 + p.words_per_split, p.VP) - w0) / DEPTH;
@@ -343,16 +362,19 @@ __global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
         const int r = wave * 8 + 2 * i + (lane >> 5), c = (lane & 31) ^ (((r & 3) << 2) | ((r >> 2) & 3));
         off_w[i] = k0 + 8 * c < p.K ? (uint32_t)r * (uint32_t)p.K * 2u + (uint32_t)c * 16u : 0x80000000u;
     }
-    const uint32_t off_d = (uint32_t)min(m0 + wave * 64 + lane, p.M - 1) * 4u;
+    const uint32_t off_d = (uint32_t)min(m0 + wave * 64 + lane, p.M - 1) * (uint32_t)sizeof(LossStat);
     const int per = (1 << p.tile_shift) / DEPTH - 1;     // of a tile's steps the first has none of these bits
-    bool scaled = false;                                 // uniform
-    for (int i = m0 / ROWS_TOKENS; i <= (min(m0 + TOKENS, p.M) - 1) / ROWS_TOKENS; ++i) scaled |= p.uneven[i] != 0;
-    scaled = __builtin_amdgcn_readfirstlane(scaled);
+    uint32_t apart = 0;
+    {
+        const int first = m0 / p.apart_tokens, n = ((min(m0 + TOKENS, p.M) - 1) / p.apart_tokens + 1 - first) * p.tiles;
+        for (int i = tid; i < n; i += THREADS) apart |= p.apart[(size_t)first * p.tiles + i];
+    }
+    const bool scaled = __builtin_amdgcn_readfirstlane(__syncthreads_or((int)apart)) != 0;
     auto fetch = [&](int s, int i) __attribute__((always_inline)) {
         const uint32_t stage = smem_lds + (uint32_t)(s % STAGES) * S::STAGE;
-        if (i == TP + TW) {                              // the exponents of a tile, with its first step
+        if (i == TP + TW) {                              // the shifts of a tile, with its first step
             if (scaled && wave < TP && (s & per) == 0)
-                dma4_b(buffer_desc(p.drop + (size_t)((w0 + s * DEPTH) >> p.tile_shift) * p.M), off_d, stage + S::D0 + (uint32_t)wave * 256u);
+                dma4_b(buffer_desc(p.stats + (size_t)((w0 + s * DEPTH) >> p.tile_shift) * p.M), off_d, stage + S::D0 + (uint32_t)wave * 256u);
         } else if (i < TP) dma16_b(src_p, off_p[i < TP ? i : 0], (uint32_t)s * (DEPTH * 2u), stage + (uint32_t)(wave * TP + i) * 1024u);
         else {                                           // words past V come as zeros, too
             const int r = wave * 8 + 2 * (i - TP) + (lane >> 5);
@@ -380,7 +402,27 @@ __global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
             for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
     bf16x8_t fa[2][AT];
     v4i16_t fb[2][2][2];
-    uint32_t drop[AT];                                   // exponents below the token's scale, of this step's tile
+    float most[AT];                                      // the tokens' largest shifts, which their scale is
+    uint32_t drop[AT];                                   // how far this step's tile is below: exponents of both halves
+    if (scaled) {
+        constexpr int PARTS = THREADS / TOKENS;
+        float* join = reinterpret_cast<float*>(smem);
+        if (tid < PARTS * TOKENS) {
+            const LossStat* of = p.stats + min(m0 + tid % TOKENS, p.M - 1);
+            float l = kLeast * kLog2e;
+#pragma unroll 8
+            for (int i = tid / TOKENS; i < p.tiles; i += PARTS) l = fmaxf(l, of[(size_t)i * p.M].shift);
+            join[tid] = l;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int a = 0; a < AT; ++a) {
+            most[a] = kLeast * kLog2e;
+#pragma unroll
+            for (int r = 0; r < PARTS; ++r) most[a] = fmaxf(most[a], join[r * TOKENS + wm * AT * 32 + a * 32 + fi]);
+        }
+        __syncthreads();
+    }
     auto run = [&](auto SCALED_) __attribute__((always_inline)) {
         constexpr bool SCALED = decltype(SCALED_)::value;
         product_steps<STAGES, TP + TW + SCALED, TP + TW, AT + 4 + (SCALED ? AT : 0), AT * 2>(
@@ -390,7 +432,9 @@ __global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
                 if (i < AT) fa[kk & 1][i < AT ? i : 0] = *reinterpret_cast<const bf16x8_t*>(smem + st + koff[kk] + a0 + i * 32 * ROWB);
                 else if (i >= AT + 4) {
                     const int a = i < AT + 4 ? 0 : i - AT - 4;
-                    if (kk == 0 && (s & per) == 0) drop[a] = *reinterpret_cast<const uint32_t*>(smem + st + S::D0 + (wm * AT * 32 + a * 32 + fi) * 4);
+                    // an exponential times 2^-d: bf16 has its exponent from bit 7 on, and 255 leaves nothing of any
+                    if (kk == 0 && (s & per) == 0)
+                        drop[a] = ((uint32_t)fminf(most[a] - *reinterpret_cast<const float*>(smem + st + S::D0 + (wm * AT * 32 + a * 32 + fi) * 4), 255.0f) << 7) * 0x10001u;
                 } else {
                     const int q = i < AT || i >= AT + 4 ? 0 : i - AT, b = q >> 1, e = q & 1;
                     fb[kk & 1][b][e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(uintptr_t)(smem_lds + st + tr[e][b] + kk * 16 * 512));
@@ -463,7 +507,7 @@ constexpr TileCost kGradCost[] = {{256, 10.0, 1.55}, {192, 7.0, 1.23}, {128, 4.0
 
 struct LossPlan {
     int tokens, shift, tiles, VP, rows, grad_tokens, splits, words;      // rows: tokens a piece
-    size_t stats0, zt0, drop0, uneven0, rows0, part0, P0, bytes;
+    size_t stats0, zt0, apart0, rows0, part0, P0, bytes;
 };
 LossPlan loss_plan(int M, int V, int K, bool grad) {
     LossPlan l{};
@@ -499,8 +543,7 @@ LossPlan loss_plan(int M, int V, int K, bool grad) {
     l.stats0 = take((size_t)l.rows * l.tiles * sizeof(LossStat));
     l.zt0 = take((size_t)l.rows * 4);
     if (grad) {
-        l.drop0 = take((size_t)l.rows * l.tiles * 4);
-        l.uneven0 = take((size_t)(l.rows + ROWS_TOKENS - 1) / ROWS_TOKENS * 4);
+        l.apart0 = take((size_t)((l.rows + 31) / 32) * l.tiles * 4);
         l.rows0 = take((size_t)l.rows * 8);
         l.part0 = take((size_t)l.splits * out_bytes);
         l.P0 = take((size_t)l.rows * l.VP * 2);
@@ -508,6 +551,7 @@ LossPlan loss_plan(int M, int V, int K, bool grad) {
     return l;
 }
 
+int loss_rows_blocks(int M) { return (M + ROWS_TOKENS - 1) / ROWS_TOKENS; }
 template <class K>
 hipError_t launch_tiles(K kernel, int smem, long long grid, const LossParams& p, hipStream_t st) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -516,14 +560,15 @@ hipError_t launch_tiles(K kernel, int smem, long long grid, const LossParams& p,
     return hipGetLastError();
 }
 template <int WV, int AT, int BT, int STAGES>
-hipError_t launch_logits(const LossParams& p, hipStream_t st) {
+hipError_t launch_logits(LossParams& p, hipStream_t st) {
     using S = Logits<WV, AT, BT, STAGES>;
+    p.apart_tokens = BT * 32;
     return launch_tiles(loss_logits_kernel<WV, AT, BT, STAGES>, S::SMEM, (long long)((p.M + S::TOKENS - 1) / S::TOKENS) * p.tiles, p, st);
 }
 template <int AT, int STAGES>
 hipError_t launch_grad(const LossParams& p, hipStream_t st) {
     using S = Grad<AT, STAGES>;
-    return launch_tiles(loss_grad_kernel<AT, STAGES>, S::SMEM, (long long)((p.M + S::TOKENS - 1) / S::TOKENS) * ((p.K + 255) / 256) * p.splits, p, st);
+    return launch_tiles(loss_grad_kernel<AT, STAGES>, S::SMEM, (long long)((p.M + S::TOKENS - 1) / S::TOKENS) * ((p.K + 255) / 256) * p.splits + (p.rows_inside ? loss_rows_blocks(p.M) : 0), p, st);
 }
 
 }  // namespace
@@ -541,7 +586,7 @@ hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t st) {
         p.loss = a.loss + m0; p.lse = a.lse ? a.lse + m0 : nullptr; p.dH = grad ? a.dH + (size_t)m0 * a.K : nullptr;
         p.stats = reinterpret_cast<LossStat*>(ws + l.stats0); p.zt = reinterpret_cast<float*>(ws + l.zt0);
         if (grad) {
-            p.drop = reinterpret_cast<uint32_t*>(ws + l.drop0); p.uneven = reinterpret_cast<uint32_t*>(ws + l.uneven0); p.rows = reinterpret_cast<float2*>(ws + l.rows0);
+            p.apart = reinterpret_cast<uint32_t*>(ws + l.apart0); p.rows = reinterpret_cast<float2*>(ws + l.rows0);
             p.part = reinterpret_cast<float*>(ws + l.part0); p.P = reinterpret_cast<uint16_t*>(ws + l.P0);
             p.splits = l.splits; p.words_per_split = l.words;
         }
@@ -552,8 +597,13 @@ hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t st) {
         else if (l.tokens == 128) e = launch_logits<4, 2, 2, 3>(p, st);
         else e = launch_logits<4, 2, 1, 3>(p, st);
         if (e != hipSuccess) return e;
-        loss_rows_kernel<<<dim3((unsigned)((p.M + ROWS_TOKENS - 1) / ROWS_TOKENS)), dim3(1024), 0, st>>>(p);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        // A launch less for few tokens (64 of 50265 words, K 1024, 64.0 -> 59.0 us, of 1003, K 512, 19.5 -> 16.0; 4096 of 1003 36.9 -> 35.2; 8192 level).  Beside the
+        // second product's LDS a unit holds one such workgroup, so that many take longer (65536 tokens of 1003 words 257 us, in a launch of their own 251).
+        p.rows_inside = grad && loss_rows_blocks(p.M) <= device_compute_units();
+        if (!p.rows_inside) {
+            loss_rows_kernel<<<dim3((unsigned)loss_rows_blocks(p.M)), dim3(1024), 0, st>>>(p);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
         if (!grad) continue;
         if (l.grad_tokens == 256) e = launch_grad<4, 2>(p, st);
         else if (l.grad_tokens == 192) e = launch_grad<3, 2>(p, st);

@@ -283,3 +283,25 @@ def test_binding_refusals():
     with pytest.raises(lowra.LowraError) as e:
         lowra.lowra_vocab_loss(b[:, :60].contiguous(), v[:, :60].contiguous(), targets)
     assert e.value.status == lowra.UNSUPPORTED
+
+
+@pytest.mark.parametrize("M", [4096, 4097])
+def test_many_tokens(M):
+    """The tokens' numbers beside the second product, and in a launch of their own."""
+    h, W, targets, weights = make(M, 300, 64, 2)
+    check(call(h, W, targets, weights), formulas(h, W, targets, weights))
+
+
+@pytest.mark.parametrize("M,V,K", [(40, 700, 64), (600, 2049, 128)])
+def test_padding_of_any_size_beside_ordinary_tokens(M, V, K):
+    h, W, targets, weights = make(M, V, K, 3)
+    f = formulas(h, W, targets, weights)
+    out = call(h, W, targets, weights)
+    there = f["there"]
+    pads = (~there).nonzero()[:, 0]
+    assert pads.numel() >= 4
+    filled = h.clone()
+    for i, v in enumerate((1e4, -1e30, float("inf"), float("nan"))):
+        filled[pads[i::4]] = v
+    got = call(filled, W, targets, weights)
+    assert torch.equal(got[0], out[0]) and torch.equal(got[2], out[2]) and torch.equal(got[1][there], out[1][there])
