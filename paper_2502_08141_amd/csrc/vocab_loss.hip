@@ -147,8 +147,13 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
     uint32_t past[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) past[i] = (steps - 1) * DEPTH + 8 * ((lane & 7) ^ ((4 * i + (lane >> 4)) & 7)) < p.K ? 0u : 0x80000000u;
+    // A tile of few tokens is the only one to read its rows of W, and workgroups that all read the same columns of rows that lie 2^n bytes apart meet in a part of the memory's
+    // channels: each begins with another step (16 and 128 tokens of 128256 words, K 2048, 120 and 132 -> 103 and 104 us, 16 of 32000, K 4096, 61 -> 52; 16 steps level).
+    // Where tiles share rows, they do so because they read them together: 4096 tokens 826 us, with this 840 to 890.
+    int at = __builtin_amdgcn_readfirstlane(p.M <= TOKENS && steps >= 32 ? vt % steps : 0) - 1;
     auto fetch = [&](int s, int i) __attribute__((always_inline)) {
-        const uint32_t stage = smem_lds + (uint32_t)(s % STAGES) * S::STAGE, soff = (uint32_t)s * (DEPTH * 2u), end = s == steps - 1 ? ~0u : 0u;
+        if (i == 0) at = at + 1 == steps ? 0 : at + 1;   // (transfers are asked for in order)
+        const uint32_t stage = smem_lds + (uint32_t)(s % STAGES) * S::STAGE, soff = (uint32_t)at * (DEPTH * 2u), end = at == steps - 1 ? ~0u : 0u;
         if (i < TW) dma16_b(src_w, off_w[i < TW ? i : 0] | (past[(wave * TW + i) & 1] & end), soff, stage + (uint32_t)(wave * TW + i) * 1024u);
         else dma16_b(src_h, off_h[i < TW ? 0 : i - TW] | (past[(wave * TT + i - TW) & 1] & end), soff, stage + WORDS * ROWB + (uint32_t)(wave * TT + i - TW) * 1024u);
     };
@@ -517,14 +522,16 @@ LossPlan loss_plan(int M, int V, int K, bool grad) {
     if (grad) rows = std::min(rows, std::max<size_t>(std::min(kLossPiece / ((size_t)V256 * 512), kLossPiece / 2 / ((size_t)K * 4)) / 256 * 256, 256));
     rows = std::min<size_t>(rows, std::max((1 << 24) / V256, 256));      // (statistics of a piece: 128 MB)
     l.rows = (int)rows;
-    l.shift = l.rows <= 64 ? 7 : 8;                      // few tokens: tiles of 128 words, so that more units read W
+    // Few tokens: tiles of 128 words, so that more units read W; up to 128 tokens only where a unit has no more than one of them (128 tokens, K 4096, 32000 words 71 -> 60 us,
+    // K 8192, 16000 words 105 -> 82; K 1024, 50265 words would be 32 -> 41).
+    l.shift = l.rows <= 64 || (l.rows <= 128 && (V + 127) / 128 <= units) ? 7 : 8;
     l.tiles = (V + (1 << l.shift) - 1) >> l.shift;
     l.VP = l.tiles << l.shift;
     auto rounds = [&](long long tiles) { return (double)((tiles + units - 1) / units); };
     double least = 1e300;
     for (const TileCost& c : kLogitsCost) {
         const double t = rounds((long long)((l.rows + c.tokens - 1) / c.tokens) * l.tiles) * (c.fixed + c.step * ((K + DEPTH - 1) / DEPTH));
-        if (l.rows <= 64 ? c.tokens == 64 : t < least) { least = t; l.tokens = c.tokens; }
+        if (l.shift == 7 ? c.tokens == (l.rows <= 64 ? 64 : 128) : t < least) { least = t; l.tokens = c.tokens; }
     }
     // The second product has few tiles, so that its words are split between workgroups, whose sums are written and read once more (3.3 MB of them a microsecond).
     const size_t out_bytes = (size_t)l.rows * K * 4;
@@ -591,7 +598,10 @@ hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t st) {
             p.splits = l.splits; p.words_per_split = l.words;
         }
         hipError_t e;
-        if (l.shift == 7) e = launch_logits<4, 1, 1, 6>(p, st);
+        // 64 tokens: two workgroups of three stages a unit where there are more tiles than units (K 640, 100000 words 42 -> 35 us), else one of six (K 8192, 16000 words 76 -> 71)
+        if (l.shift == 7 && l.tokens == 128) e = launch_logits<4, 1, 2, 4>(p, st);
+        else if (l.shift == 7 && l.tiles > device_compute_units()) e = launch_logits<4, 1, 1, 3>(p, st);
+        else if (l.shift == 7) e = launch_logits<4, 1, 1, 6>(p, st);
         else if (l.tokens == 256) e = launch_logits<2, 4, 2, 2>(p, st);
         else if (l.tokens == 192) e = launch_logits<4, 2, 3, 2>(p, st);
         else if (l.tokens == 128) e = launch_logits<4, 2, 2, 3>(p, st);

@@ -305,3 +305,10 @@ def test_padding_of_any_size_beside_ordinary_tokens(M, V, K):
         filled[pads[i::4]] = v
     got = call(filled, W, targets, weights)
     assert torch.equal(got[0], out[0]) and torch.equal(got[2], out[2]) and torch.equal(got[1][there], out[1][there])
+
+
+@pytest.mark.parametrize("M,V,K", [(1, 32897, 64), (64, 33000, 72), (100, 1000, 2056), (128, 257, 2112), (64, 300, 4168), (40, 129, 2048)])
+def test_few_tokens(M, V, K):
+    """More tiles of words than units, and contractions that begin in their middle."""
+    h, W, targets, weights = make(M, V, K, 4)
+    check(call(h, W, targets, weights), formulas(h, W, targets, weights))
