@@ -14,8 +14,8 @@
 // that they keep their digits there.
 // Tokens go in pieces whose exponentials fit kLossPiece bytes, so that neither the logits nor anything else of size M x V is ever there at once.
 // (Pieces of the vocabulary would have to form z a second time for the gradient: 6 M V K operations in place of 4.)
-// Graph replays: 4096 tokens of 32000 words, K 4096, 1636 to 1674 us by the card (1.28 to 1.31 PFLOP/s; the matrix unit busy for 76 % of the first product and 82 % of the
-// second), 777 of 50265, K 1024, 220; 333 of 32000 without the gradient 121, of which W from memory is 44; 19 of 1003, K 512, 14.6, three launches' latencies.
+// Graph replays: 4096 tokens of 32000 words, K 4096, 1636 to 1690 us by the card (1.27 to 1.31 PFLOP/s; the matrix unit busy for 76 % of the first product and 82 % of the
+// second), 777 of 50265, K 1024, 215; 333 of 32000, K 4096, without the gradient 112, 90 with W in a cache; 16 of 32000, K 4096, 95 and without 53 (W at 5.6 and 5.0 TB/s); 19 of 1003, K 512, 14.6, three launches' latencies.
 #include <algorithm>
 
 #include "gemm_common.h"
