@@ -244,12 +244,11 @@ hipError_t adamw_build(const std::vector<AdamwItem>& items, bool eight, AdamwGro
     if (items.empty()) return hipSuccess;
     long long total = 0;
     for (const AdamwItem& it : items) total += it.count;
-    // as many elements as a workgroup asks for together, unless that leaves units with less than four workgroups (1.25 million elements: 7.0 us in single
-    // steps; 8.4 with the code for four in the same kernel)
-    g.steps = total / AW_STEP >= (long long)AW_MOST * 4 * device_compute_units() ? AW_MOST : 1;
-    const int chunk = g.steps * AW_STEP;
-    // past the caches where the batch is more than the 256 MB behind them (143 million elements in 8 bits, with their decoded states: 843 -> 831 us)
-    g.stream = total * (eight ? 18 : 30) > (256ll << 20);
+    // A batch of which the 256 MB behind the caches hold less than half of what it reads and writes goes past the caches, and a workgroup asks for AW_MOST rounds together: 32-bit
+    // states of 201 MB 47 us through the caches and 43.5 in single rounds, 40.3 so; of 268 MB 57.6 in single rounds, 53.2 so; 8-bit states of 327 MB, two decodings with them, 98 and 91.
+    // Below, workgroups of one round are as soon done or sooner (8-bit states of 82 MB 30.0 -> 27.4, 32-bit ones of 37 MB 8.4 -> 7.0).
+    g.large = total * (eight ? 18 : 30) > (128ll << 20);
+    const int chunk = (g.large ? AW_MOST : 1) * AW_STEP;
     std::vector<AdamwChunk> chunks;
     for (size_t i = 0; i < items.size(); ++i)
         for (long long at = 0; at < items[i].count; at += chunk) chunks.push_back(AdamwChunk{(int)i, (uint32_t)at});
@@ -262,9 +261,8 @@ template <bool EIGHT>
 static hipError_t adamw_launch(const AdamwGroup& g, const AdamwStep& s, hipStream_t st) {
     if (!g.nchunks) return hipSuccess;
     const dim3 grid((unsigned)g.nchunks), block(AW_THREADS);
-    if (g.steps == 1) adamw_kernel<EIGHT, false, 1><<<grid, block, 0, st>>>(g.d_items, g.d_chunks, s);
-    else if (!g.stream) adamw_kernel<EIGHT, false, AW_MOST><<<grid, block, 0, st>>>(g.d_items, g.d_chunks, s);
-    else adamw_kernel<EIGHT, true, AW_MOST><<<grid, block, 0, st>>>(g.d_items, g.d_chunks, s);
+    if (g.large) adamw_kernel<EIGHT, true, AW_MOST><<<grid, block, 0, st>>>(g.d_items, g.d_chunks, s);
+    else adamw_kernel<EIGHT, false, 1><<<grid, block, 0, st>>>(g.d_items, g.d_chunks, s);
     return hipGetLastError();
 }
 hipError_t adamw_run(const AdamwGroup (&groups)[2], const AdamwStep& s, hipStream_t st) {

@@ -44,7 +44,7 @@ struct AdamwItem {
 struct AdamwChunk { int item; uint32_t first; };             // elements of an item from this one on, as many as a workgroup of the launch takes
 struct AdamwGroup {                                          // the items whose states have the same width
     AdamwItem* d_items = nullptr; AdamwChunk* d_chunks = nullptr;
-    int nchunks = 0, steps = 0; bool stream = false;
+    int nchunks = 0; bool large = false;
 };
 struct AdamwStep { float lr, b1, c1, b2, c2, over_bias1, over_bias2, eps, decay; const float* grad_scale; };   // c = 1 - b; over_bias = 1 / (1 - b^t)
 hipError_t adamw_build(const std::vector<AdamwItem>& items, bool eight, AdamwGroup& g);

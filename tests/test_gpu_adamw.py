@@ -320,3 +320,27 @@ def test_binding_refusals():
         b.run(lr=0.1, grad_scale=torch.ones(2, device="cuda"))
     with pytest.raises(ValueError):
         lowra.lowra_adamw_state(eight["m"], torch.zeros(3, device="cuda"))
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_large_batch_is_its_items(eight):
+    """A batch past the caches, in pieces of four rounds with ragged ends, gives the bits of its items in batches of their own."""
+    counts = [1200003, 64, 1, 4095, 4096, 4097, 1000000, 63, 1023, 8193, 1300000, 900001, 1100032, 1250000, 777777, 1000001]
+    items = [cuda(make(1000, eight, seed=i)) for i in range(len(counts))]
+    for s, n in zip(items, counts):                                     # the same thousand elements over and over (960: whole groups)
+        for k, t in list(s.items()):
+            if "absmax" in k:
+                s[k] = t[:15].repeat((n + 959) // 960)[:(n + 63) // 64].contiguous()
+            else:
+                s[k] = t[:960].repeat((n + 959) // 960)[:n].contiguous()
+    def run(which):
+        sets = [{k: v.clone() for k, v in items[i].items()} for i in which]
+        copies = [torch.empty(counts[i], dtype=torch.bfloat16, device="cuda") for i in which]
+        batch = lowra.AdamWBatch([lowra.AdamWItem(weight_bf16=c, **s) for s, c in zip(sets, copies)])
+        batch.run(**HYPER)
+        torch.cuda.synchronize()
+        return [dict(s, copy=c) for s, c in zip(sets, copies)]
+    assert sum(counts) * (18 if eight else 30) > 1 << 27 and max(counts) * 30 < 1 << 27
+    for i, out in enumerate(run(range(len(counts)))):
+        alone, = run([i])
+        assert all(torch.equal(out[k], alone[k]) for k in out), (i, counts[i])
