@@ -320,8 +320,9 @@ __device__ __forceinline__ void loss_rows(const LossParams& p, int block, float 
     const bool there = t >= 0 && t < p.V;
     const float xt = there ? __builtin_fmaf(p.zt[m], kLog2e, -most) : -INFINITY, et = exp2f(xt), total = others + et, log_total = logf(total);
     if (p.lse) p.lse[m] = __builtin_fmaf(most, kLn2, log_total);
-    const float ratio = others / et;                     // (past fp32 where the target is 2^-126 of the others)
-    p.loss[m] = !there ? 0.0f : ratio < 3e38f ? log1pf(ratio) : log_total - xt * kLn2;
+    // From 2^24 on the target is nothing in the total, and et may be too small to have all its digits (the others are 2^-32 at least, so below it has them).
+    const float ratio = others / et;
+    p.loss[m] = !there ? 0.0f : ratio < 0x1p24f ? log1pf(ratio) : log_total - xt * kLn2;
     if (p.rows) {
         const float w = !there ? 0.0f : p.weights ? p.weights[m] : 1.0f;
         p.rows[m] = make_float2(w / total, -w * (others / total));
