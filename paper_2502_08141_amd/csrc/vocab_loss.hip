@@ -9,9 +9,10 @@
 // does not wait for that pass, whose workgroups stand behind its own.  Where n is not zero for every tile and every token with a target, it takes the tokens' largest n
 // first and brings a tile's exponentials to that scale on the way into the matrix unit, a subtraction from their exponents and exact; else its loop is without
 // (4096 x 32000 x 4096 by itself: 895 us with the subtraction, 818 without; a pass over the exponentials before it 90).  The token's factor
-// weight / sum meets the fp32 sums.  So a probability is rounded once, to bf16.  The target's own term, weight (p_t - 1) W_t, is added in fp32: p_t is near
-// one for most tokens of a trained model, and its rounding would be the gradient's error.  p_t - 1 and the loss come from the sum without the target, so
-// that they keep their digits there.
+// weight / sum meets the fp32 sums.  So a probability is rounded once, to bf16; the factor also takes the rounded exponentials' sum back to that of the exact ones, so
+// that a word's rounding counts by how far its row of W is from the others' mean, and not at all where one word has all that the target leaves.  The target's own term,
+// weight (p_t - 1) W_t, is added in fp32: p_t is near one for most tokens of a trained model, and its rounding would be the gradient's error.  p_t - 1 and the loss come from
+// the sum without the target, so that they keep their digits there.
 // Tokens go in pieces whose exponentials fit kLossPiece bytes, so that neither the logits nor anything else of size M x V is ever there at once.
 // (Pieces of the vocabulary would have to form z a second time for the gradient: 6 M V K operations in place of 4.)
 // Graph replays: 4096 tokens of 32000 words, K 4096, 1636 to 1690 us by the card (1.27 to 1.31 PFLOP/s; the matrix unit busy for 76 % of the first product and 82 % of the
@@ -26,6 +27,7 @@ namespace lowra {
 namespace {
 
 constexpr int THREADS = 512, WAVES = 8, DEPTH = 64;      // a step of either product: 64 features or words
+typedef __bf16 v2bf16_t __attribute__((ext_vector_type(2)));
 typedef short v4i16_t __attribute__((ext_vector_type(4)));
 typedef short v8i16_t __attribute__((ext_vector_type(8)));
 typedef unsigned short v2u16_t __attribute__((ext_vector_type(2)));
@@ -44,10 +46,11 @@ struct LossParams {
     uint16_t* dH;
     int M, V, K, VP, tiles, tile_shift;                  // this piece's tokens; VP: words in whole tiles of 2^tile_shift
     LossStat* stats;                                     // [tiles][M]
+    float* rounded;                                      // [tiles][M]: the sum again, of the exponentials as they are in P
     float* zt;                                           // [M]
     uint32_t* apart;                                     // [M / apart_tokens][tiles]: a target's token of these has a shift that is not zero
     int apart_tokens;
-    float2* rows;                                        // [M]: weight / sum, weight (p_t - 1)
+    float2* rows;                                        // [M]: weight / sum (of rounded exponentials), weight (p_t - 1)
     uint16_t* P;                                         // [M][VP]
     float* part;                                         // [splits][M][K]
     int splits, words_per_split;
@@ -118,6 +121,11 @@ __device__ __forceinline__ void product_steps(int steps, Fetch fetch, Read read,
     }
 }
 
+// sum + both halves
+__device__ __forceinline__ float sum_bf16x2(uint32_t e, float sum) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf16_t, e), __builtin_bit_cast(v2bf16_t, 0x3f803f80u), sum, false);
+}
+
 // ---- first product.  Words are the matrix instruction's rows, tokens its columns, so that a token's words lie in one lane and its other half: WV x (8 / WV)
 // wavefronts, each with AT x BT tiles of 32 words x 32 tokens.
 template <int WV, int AT, int BT, int STAGES>
@@ -130,7 +138,7 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
     using S = Logits<WV, AT, BT, STAGES>;
     constexpr int WORDS = S::WORDS, TOKENS = S::TOKENS, TW = WORDS / 64, TT = TOKENS / 64;       // transfers of a wavefront: eight rows each
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ float join[WV][TOKENS];
+    __shared__ float join[WV][TOKENS], join_rounded[WV][TOKENS];
     const uint32_t smem_lds = (uint32_t)(uintptr_t)(lptr_t)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int vt, mt;
@@ -251,15 +259,22 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
     }
     if (p.P) {                                           // the exponentials to LDS: a row a token, 16-byte chunks in another order for each of 32 tokens
 #pragma unroll
-        for (int b = 0; b < BT; ++b)
+        for (int b = 0; b < BT; ++b) {
+            float held = 0.0f, more = 0.0f;
 #pragma unroll
             for (int a = 0; a < AT; ++a)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int c = wv * AT * 4 + a * 4 + q;
-                    *reinterpret_cast<uint2*>(smem + (t0 + 32 * b) * (WORDS * 2) + ((c ^ (fi & (WORDS / 8 - 1))) << 4) + 8 * half) =
-                        make_uint2(pack_bf16x2(acc[a][b][4 * q], acc[a][b][4 * q + 1]), pack_bf16x2(acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]));
+                    const uint2 e = make_uint2(pack_bf16x2(acc[a][b][4 * q], acc[a][b][4 * q + 1]), pack_bf16x2(acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]));
+                    *reinterpret_cast<uint2*>(smem + (t0 + 32 * b) * (WORDS * 2) + ((c ^ (fi & (WORDS / 8 - 1))) << 4) + 8 * half) = e;
+                    held = sum_bf16x2(e.x, held);
+                    more = sum_bf16x2(e.y, more);
                 }
+            held += more;
+            held += __shfl_xor(held, 32);
+            if (half == 0) join_rounded[wv][t0 + 32 * b] = held;
+        }
     }
     __syncthreads();
     if (wv == 0 && half == 0) {
@@ -270,6 +285,11 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
 #pragma unroll
             for (int w = 1; w < WV; ++w) s += join[w][t];
             if (m0 + t < p.M) p.stats[(size_t)vt * p.M + m0 + t] = LossStat{shift[b], s};
+            if (!p.P) continue;
+            s = join_rounded[0][t];
+#pragma unroll
+            for (int w = 1; w < WV; ++w) s += join_rounded[w][t];
+            if (m0 + t < p.M) p.rounded[(size_t)vt * p.M + m0 + t] = s;
         }
     }
     if (!p.P) return;                                    // uniform
@@ -284,9 +304,9 @@ __global__ __launch_bounds__(THREADS, 2) void loss_logits_kernel(LossParams p) {
 // ---- loss, lse and what the gradient needs of a token, 16 tokens a workgroup, the tiles dealt to 64 groups of threads (16 groups and 64 tokens: 777 tokens of 197 tiles
 // 9.8 us for 7.4).  N wavefronts: 16, or 8 that have two groups' sums each, so that the order is the same.
 constexpr int ROWS_TOKENS = 16;
-template <int N>
-__device__ __forceinline__ void loss_rows(const LossParams& p, int block, float (*join)[ROWS_TOKENS]) {
-    constexpr int SETS = 16 / N;
+template <int N, bool GRAD>
+__device__ __forceinline__ void loss_rows(const LossParams& p, int block, float (*join)[2][ROWS_TOKENS]) {
+    constexpr int SETS = 16 / N, SUMS = GRAD ? 2 : 1;    // of the exponentials, and of those that the gradient has
     const int tok = threadIdx.x % ROWS_TOKENS, group = threadIdx.x / ROWS_TOKENS, wave = threadIdx.x >> 6, m = block * ROWS_TOKENS + tok, at = min(m, p.M - 1);
     const bool first = (threadIdx.x & 63) < ROWS_TOKENS;
     float most = kLeast * kLog2e;
@@ -294,28 +314,40 @@ __device__ __forceinline__ void loss_rows(const LossParams& p, int block, float 
     for (int i = group; i < p.tiles; i += 4 * N) most = fmaxf(most, p.stats[(size_t)i * p.M + at].shift);
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
-    if (first) join[wave][tok] = most;
+    if (first) join[wave][0][tok] = most;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < N; ++w) most = fmaxf(most, join[w][tok]);
+    for (int w = 0; w < N; ++w) most = fmaxf(most, join[w][0][tok]);
     __syncthreads();
-    float others = 0.0f;
+    float sum[SUMS];
 #pragma unroll
     for (int q = 0; q < SETS; ++q) {
-        others = 0.0f;
+#pragma unroll
+        for (float& v : sum) v = 0.0f;
 #pragma unroll 4
         for (int i = group + 4 * N * q; i < p.tiles; i += 64) {
             const LossStat st = p.stats[(size_t)i * p.M + at];
-            others += ldexpf(st.sum, (int)fmaxf(st.shift - most, -1000.0f));      // (2^-128 by itself is none in fp32)
+            const float of[2] = {st.sum, GRAD ? p.rounded[(size_t)i * p.M + at] : 0.0f};
+            const int by = (int)fmaxf(st.shift - most, -1000.0f);                  // (2^-128 by itself is none in fp32)
+#pragma unroll
+            for (int k = 0; k < SUMS; ++k) sum[k] += ldexpf(of[k], by);
         }
-        others += __shfl_xor(others, 16);
-        others += __shfl_xor(others, 32);
-        if (first) join[N * q + wave][tok] = others;
+#pragma unroll
+        for (int k = 0; k < SUMS; ++k) {
+            sum[k] += __shfl_xor(sum[k], 16);
+            sum[k] += __shfl_xor(sum[k], 32);
+            if (first) join[N * q + wave][k][tok] = sum[k];
+        }
     }
     __syncthreads();
     if (threadIdx.x >= ROWS_TOKENS || m >= p.M) return;
-    others = join[0][tok];
-    for (int w = 1; w < 16; ++w) others += join[w][tok];
+#pragma unroll
+    for (int k = 0; k < SUMS; ++k) {
+        sum[k] = join[0][k][tok];
+#pragma unroll
+        for (int w = 1; w < 16; ++w) sum[k] += join[w][k][tok];
+    }
+    const float others = sum[0];
     const int t = p.targets[m];
     const bool there = t >= 0 && t < p.V;
     const float xt = there ? __builtin_fmaf(p.zt[m], kLog2e, -most) : -INFINITY, et = exp2f(xt), total = others + et, log_total = logf(total);
@@ -323,14 +355,15 @@ __device__ __forceinline__ void loss_rows(const LossParams& p, int block, float 
     // From 2^24 on the target is nothing in the total, and et may be too small to have all its digits (the others are 2^-32 at least, so below it has them).
     const float ratio = others / et;
     p.loss[m] = !there ? 0.0f : ratio < 0x1p24f ? log1pf(ratio) : log_total - xt * kLn2;
-    if (p.rows) {
+    if constexpr (GRAD) {
         const float w = !there ? 0.0f : p.weights ? p.weights[m] : 1.0f;
-        p.rows[m] = make_float2(w / total, -w * (others / total));
+        p.rows[m] = make_float2(w / total * (sum[1] > 0.0f ? others / sum[1] : 1.0f), -w * (others / total));
     }
 }
+template <bool GRAD>
 __global__ __launch_bounds__(1024) void loss_rows_kernel(LossParams p) {
-    __shared__ float join[16][ROWS_TOKENS];
-    loss_rows<16>(p, blockIdx.x, join);
+    __shared__ float join[16][2][ROWS_TOKENS];
+    loss_rows<16, GRAD>(p, blockIdx.x, join);
 }
 
 // ---- second product, over a run of words: tokens (the exponentials) are the matrix instruction's rows, features its columns, W's operand read across its rows
@@ -349,7 +382,7 @@ __global__ __launch_bounds__(THREADS, 2) void loss_grad_kernel(LossParams p) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tiles_k = (p.K + 255) / 256, tiles_m = (p.M + TOKENS - 1) / TOKENS;
     const int tiles = tiles_k * tiles_m * p.splits;
-    if ((int)blockIdx.x >= tiles) { loss_rows<WAVES>(p, blockIdx.x - tiles, reinterpret_cast<float(*)[ROWS_TOKENS]>(smem)); return; }
+    if ((int)blockIdx.x >= tiles) { loss_rows<WAVES, true>(p, blockIdx.x - tiles, reinterpret_cast<float(*)[2][ROWS_TOKENS]>(smem)); return; }
     const int work = xcd_tile(blockIdx.x, tiles), split = __builtin_amdgcn_readfirstlane(work / (tiles_k * tiles_m));
     int mt, kt;
     tile_of(work - split * (tiles_k * tiles_m), tiles_m, tiles_k, 4, mt, kt);
@@ -513,7 +546,7 @@ constexpr TileCost kGradCost[] = {{256, 10.0, 1.55}, {192, 7.0, 1.23}, {128, 4.0
 
 struct LossPlan {
     int tokens, shift, tiles, VP, rows, grad_tokens, splits, words;      // rows: tokens a piece
-    size_t stats0, zt0, apart0, rows0, part0, P0, bytes;
+    size_t stats0, zt0, rounded0, apart0, rows0, part0, P0, bytes;
 };
 LossPlan loss_plan(int M, int V, int K, bool grad) {
     LossPlan l{};
@@ -551,6 +584,7 @@ LossPlan loss_plan(int M, int V, int K, bool grad) {
     l.stats0 = take((size_t)l.rows * l.tiles * sizeof(LossStat));
     l.zt0 = take((size_t)l.rows * 4);
     if (grad) {
+        l.rounded0 = take((size_t)l.rows * l.tiles * sizeof(float));
         l.apart0 = take((size_t)((l.rows + 31) / 32) * l.tiles * 4);
         l.rows0 = take((size_t)l.rows * 8);
         l.part0 = take((size_t)l.splits * out_bytes);
@@ -594,7 +628,7 @@ hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t st) {
         p.loss = a.loss + m0; p.lse = a.lse ? a.lse + m0 : nullptr; p.dH = grad ? a.dH + (size_t)m0 * a.K : nullptr;
         p.stats = reinterpret_cast<LossStat*>(ws + l.stats0); p.zt = reinterpret_cast<float*>(ws + l.zt0);
         if (grad) {
-            p.apart = reinterpret_cast<uint32_t*>(ws + l.apart0); p.rows = reinterpret_cast<float2*>(ws + l.rows0);
+            p.rounded = reinterpret_cast<float*>(ws + l.rounded0); p.apart = reinterpret_cast<uint32_t*>(ws + l.apart0); p.rows = reinterpret_cast<float2*>(ws + l.rows0);
             p.part = reinterpret_cast<float*>(ws + l.part0); p.P = reinterpret_cast<uint16_t*>(ws + l.P0);
             p.splits = l.splits; p.words_per_split = l.words;
         }
@@ -612,7 +646,8 @@ hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t st) {
         // second product's LDS a unit holds one such workgroup, so that many take longer (65536 tokens of 1003 words 257 us, in a launch of their own 251).
         p.rows_inside = grad && loss_rows_blocks(p.M) <= device_compute_units();
         if (!p.rows_inside) {
-            loss_rows_kernel<<<dim3((unsigned)loss_rows_blocks(p.M)), dim3(1024), 0, st>>>(p);
+            if (grad) loss_rows_kernel<true><<<dim3((unsigned)loss_rows_blocks(p.M)), dim3(1024), 0, st>>>(p);
+            else loss_rows_kernel<false><<<dim3((unsigned)loss_rows_blocks(p.M)), dim3(1024), 0, st>>>(p);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
         if (!grad) continue;
