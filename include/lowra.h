@@ -410,8 +410,8 @@ lowra_status lowra_rope_frequencies(int rot, double base, int scaling, double fa
  *   loss [M] fp32 dev (out, without the weight) | lse [M] fp32 dev (out) or null | dH [M,K] bf16 dev (out) or null: the loss alone
  *   workspace: dev, >= lowra_vocab_loss_workspace_bytes(M, V, K, dH wanted), 16-byte aligned; less than 512 MiB, as tokens are taken in
  *   pieces (but one of 256 tokens at least)
- * Products are bf16 with fp32 sums; the probabilities are rounded to bf16 before they meet W, but not the target's term, which is fp32 and
- * keeps its digits where the model is sure; a probability below 2^-94 of the largest may count as zero.  The order of all sums is fixed.  A NaN or an infinity in a row of h stays in its row.
+ * Products are bf16 with fp32 sums; the probabilities of the words but the target are rounded to bf16 before they meet W and brought back to their
+ * exact sum behind it; the target's term is fp32 and keeps its digits where the model is sure; a probability below 2^-94 of the largest may count as zero.  The order of all sums is fixed.  A NaN or an infinity in a row of h stays in its row.
  * M == 0 is a no-op.  INVALID_ARG: M < 0, V <= 0, K <= 0, a missing pointer, an output or the workspace that overlaps anything; UNSUPPORTED: K % 8
  * != 0, V above 2^21, K above 2^20, M above 2^30; MISALIGNED; WORKSPACE_TOO_SMALL. */
 size_t lowra_vocab_loss_workspace_bytes(int M, int V, int K, int grad);

@@ -10,13 +10,14 @@
 // first and brings a tile's exponentials to that scale on the way into the matrix unit, a subtraction from their exponents and exact; else its loop is without
 // (4096 x 32000 x 4096 by itself: 895 us with the subtraction, 818 without; a pass over the exponentials before it 90).  The token's factor
 // weight / sum meets the fp32 sums.  So a probability is rounded once, to bf16; the factor also takes the rounded exponentials' sum back to that of the exact ones, so
-// that a word's rounding counts by how far its row of W is from the others' mean, and not at all where one word has all that the target leaves.  The target's own term,
+// that a word's rounding counts by how far its row of W is from the others' mean, and not at all where one word has all that the target leaves (tokens sure of a wrong word,
+// 32000 words, K 1024: dH 2.03e-3 off in the norm without, 1.68e-3 so, all of it the outputs' own rounding; 777 tokens of 50265 words take 217.5 us for 215.5).  The target's own term,
 // weight (p_t - 1) W_t, is added in fp32: p_t is near one for most tokens of a trained model, and its rounding would be the gradient's error.  p_t - 1 and the loss come from
 // the sum without the target, so that they keep their digits there.
 // Tokens go in pieces whose exponentials fit kLossPiece bytes, so that neither the logits nor anything else of size M x V is ever there at once.
 // (Pieces of the vocabulary would have to form z a second time for the gradient: 6 M V K operations in place of 4.)
 // Graph replays: 4096 tokens of 32000 words, K 4096, 1636 to 1690 us by the card (1.27 to 1.31 PFLOP/s; the matrix unit busy for 76 % of the first product and 82 % of the
-// second), 777 of 50265, K 1024, 215; 333 of 32000, K 4096, without the gradient 112, 90 with W in a cache; 16 of 32000, K 4096, 95 and without 53 (W at 5.6 and 5.0 TB/s); 19 of 1003, K 512, 14.6, three launches' latencies.
+// second), 777 of 50265, K 1024, 217; 333 of 32000, K 4096, without the gradient 112, 90 with W in a cache; 16 of 32000, K 4096, 95 and without 53 (W at 5.6 and 5.0 TB/s); 19 of 1003, K 512, 15.1, three launches' latencies.
 #include <algorithm>
 
 #include "gemm_common.h"
