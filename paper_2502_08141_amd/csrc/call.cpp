@@ -577,6 +577,8 @@ PyObject* vocab_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t M = h->size(0), K = h->size(1), V = W->size(0);
         if (M > INT32_MAX || K > INT32_MAX || V > INT32_MAX || W->size(1) != K || targets->dim() != 1 || targets->size(0) != M) return none();
         if (weights && (weights->dim() != 1 || weights->size(0) != M)) return none();
+        for (const at::Tensor* t : {targets, weights})
+            if (t && (reinterpret_cast<uintptr_t>(t->data_ptr()) & 15u)) return none();      // lowra.py copies it
         for (const at::Tensor* t : {W, targets, ws, weights})
             if (t && t->device() != h->device()) return none();
         const bool want[3] = {true, true, a[4] == Py_True};

@@ -947,7 +947,7 @@ def lowra_vocab_loss_workspace_bytes(M: int, V: int, K: int, grad: bool = True) 
 def lowra_vocab_loss(h, W, targets, weights=None, grad: bool = True, loss=None, lse=None, dH=None, workspace=None):
     """Cross entropy of h [M,K] bf16 through the frozen head W [V,K] bf16 against targets [M] int32 (outside 0..V-1: no target, loss 0) ->
     (loss fp32 [M], lse fp32 [M], dH bf16 [M,K]): dH is the gradient of the sum of weights loss with respect to h (weights: [M] fp32, None: ones), None
-    without `grad`."""
+    without `grad`.  targets and weights may begin anywhere (`labels[1:]`): what is not 16-byte aligned is copied first."""
     if loss is None and lse is None and dH is None and workspace is not None and _lib is not None:
         res = _call.vocab_loss(h, W, targets, weights, grad, workspace)
         if res is not None:
@@ -959,6 +959,8 @@ def lowra_vocab_loss(h, W, targets, weights=None, grad: bool = True, loss=None, 
     if W.shape[1] != K or tuple(targets.shape) != (M,):
         raise ValueError("shape mismatch")
     _typed(weights, torch.float32, (M,), "weights", device)
+    # the library takes 16-byte aligned ones; labels[1:] beside h[:-1] are not
+    targets, weights = (t.clone() if t is not None and t.data_ptr() & 15 else t for t in (targets, weights))
     loss = torch.empty(M, dtype=torch.float32, device=device) if loss is None else loss
     lse = torch.empty(M, dtype=torch.float32, device=device) if lse is None else lse
     _typed(loss, torch.float32, (M,), "loss", device); _typed(lse, torch.float32, (M,), "lse", device)
