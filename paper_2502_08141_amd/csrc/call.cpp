@@ -522,7 +522,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
             !PyFloat_CheckExact(a[5]))
             return none();
         RopeTensor t[4];
-        at::Tensor out[4];
+        at::Tensor in[4], out[4];                                     // in: a list may lose its tensors while others have the interpreter's lock
         const int64_t M = positions->size(0);
         int64_t D = -1;
         for (Py_ssize_t i = 0; i < count; ++i) {
@@ -532,6 +532,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
             if (x.scalar_type() != at::kBFloat16 || !x.is_cuda() || x.dim() != 3 || (x.stride(2) != 1 && x.size(2) != 1) || x.size(0) != M || !here(x)) return none();
             if (D < 0) D = x.size(2);
             if (x.size(2) != D || x.size(1) > INT32_MAX) return none();
+            in[i] = x;
             t[i] = RopeTensor{x.data_ptr(), nullptr, (int)x.size(1), x.stride(0), x.stride(1), x.size(1) * D, D};
         }
         if (M > INT32_MAX || D > INT32_MAX || turns->size(0) > INT32_MAX / 2 || !here(*positions) || !here(*turns)) return none();

@@ -146,3 +146,23 @@ def test_what_is_left_to_python(native):
                 (h, W, t[1:], None, True, ws), (h, W, t[:M], f[1:], True, ws)):
         assert call.vocab_loss(*bad) is None
     assert lib.calls == 0
+
+
+def test_list_that_another_thread_empties(native):
+    """The interpreter's lock is given up while outputs are allocated: a list that loses its tensors meanwhile does not free what the library is about to read."""
+    call, lib, watch = native
+    _reset(lib, watch)
+    data = np.zeros((M, HEADS, D), np.int16)
+    gone = weakref.ref(data)
+    xs = [torch.from_numpy(data).view(torch.bfloat16), torch.zeros(M, KV, D, dtype=torch.bfloat16)]
+    del data
+    hook = HOOK(lambda: xs.clear())
+    watch["hook"].value = ctypes.cast(hook, ctypes.c_void_p).value
+    lib.look = lambda args: gone() is not None
+    res = call.rope(xs, torch.zeros(M, dtype=torch.int32), torch.zeros(ROT // 2, dtype=torch.int64), 0, False, 1.0)
+    watch["hook"].value, lib.look = 0, None
+    assert len(res) == 2 and lib.calls == 1 and not xs
+    assert lib.seen is True
+    del res
+    gc.collect()
+    assert gone() is None
