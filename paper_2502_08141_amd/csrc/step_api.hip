@@ -242,8 +242,10 @@ lowra_status lowra_adamw_batch_run(const lowra_adamw_batch* b, const lowra_adamw
     if (dev != b->device) return LOWRA_INVALID_ARG;
     // (1 - beta^t by expm1 and log: a beta next to one keeps its digits)
     auto over_bias = [&](double beta) { return beta > 0.0 ? (float)(-1.0 / std::expm1((double)s->step * std::log(beta))) : 1.0f; };
+    // (an eps that the kernel's reciprocal takes for zero would make NaN of 0 / (0 + eps), and is nothing beside any other root)
+    const float eps = s->eps > 0.0 ? std::max((float)s->eps, 0x1p-126f) : 0.0f;
     const lowra::AdamwStep a{(float)s->lr, (float)s->beta_one, (float)(1.0 - s->beta_one), (float)s->beta_two, (float)(1.0 - s->beta_two), over_bias(s->beta_one), over_bias(s->beta_two),
-                             (float)s->eps, (float)s->weight_decay, grad_scale};
+                             eps, (float)s->weight_decay, grad_scale};
     return launched(lowra::adamw_run(b->groups, a, static_cast<hipStream_t>(stream)));
 }
 
