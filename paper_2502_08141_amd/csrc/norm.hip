@@ -316,10 +316,8 @@ hipError_t launch_norm_bwd(const NormArgs& a, float* dweight, float* dbias, void
     float* sums = dweight || dbias ? static_cast<float*>(workspace) : nullptr;
     const hipError_t e = with_bwd_shape(a.M, a.N, [&](auto S_) {
         constexpr int W = decltype(S_)::W, C = decltype(S_)::C, G = decltype(S_)::G;
-        const int smem = G > 1 && sums ? G * a.N * (int)sizeof(float) : 0;
+        const int smem = G > 1 && sums ? G * a.N * (int)sizeof(float) : 0;          // (N G <= 8192 wherever G > 1: 32 KB at most)
         auto go = [&](auto kernel) {
-            const hipError_t e = smem > 65536 ? hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, smem) : hipSuccess;
-            if (e != hipSuccess) return e;
             kernel<<<dim3((unsigned)blocks), dim3(64 * W * G), smem, st>>>(a, sums);
             return hipGetLastError();
         };
