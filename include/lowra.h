@@ -374,7 +374,8 @@ lowra_status lowra_norm_bwd(int M, int N, int kind, const uint16_t* dY, const ui
  *   (the columns of a head are contiguous; 2-byte alignment is enough, 16-byte runs are fastest).  y may be x, with the same strides; otherwise no y
  *   overlaps another y or an x (heads of several tensors between each other in one row, at the same token stride, do not).
  *   positions [M] int32 dev (negative ones turn backwards) | turns [rot/2] uint64 dev, from lowra_rope_frequencies: the fraction of a full turn
- *   per position in units of 2^-64, so that the angle is exact at every position.  Sine and cosine are exact to fp32 rounding; outputs are rounded once.
+ *   per position in units of 2^-64, of which position times it is taken mod 2^64 without rounding and then to 2^-32 of a turn: the angle is 2^-30 off, and by
+ *   position f_j 2^-52 as the plan's f_j are of 64-bit arithmetic (2^-32 at position 2^20).  Sine and cosine of it are exact to fp32 rounding; outputs are rounded once.
  * INVALID_ARG: n <= 0, a non-positive size, rot > D, an unknown layout, a missing pointer, a negative stride, a y whose heads overlap, an
  * overlap as above; UNSUPPORTED: n > 4, odd rot, D above 2^20, M above 2^30, more than 2^32 elements or 2^20 heads; MISALIGNED (turns: 8 bytes, positions: 4, tensors: 2). */
 enum { LOWRA_ROPE_HALF = 0, LOWRA_ROPE_INTERLEAVED = 1 };
@@ -408,8 +409,10 @@ lowra_status lowra_rope_frequencies(int rot, double base, int scaling, double fa
  *   h [M,K], W [V,K] bf16 dev | targets [M] int32 dev: a token whose target is outside 0..V-1 (padding) has loss 0 and a gradient of zeros,
  *   whatever its h holds | weights [M] fp32 dev or null (one): of a token's loss in what is differentiated, e.g. 1 / number of targets
  *   loss [M] fp32 dev (out, without the weight) | lse [M] fp32 dev (out) or null | dH [M,K] bf16 dev (out) or null: the loss alone
- *   workspace: dev, >= lowra_vocab_loss_workspace_bytes(M, V, K, dH wanted), 16-byte aligned; less than 512 MiB, as tokens are taken in
- *   pieces (but one of 256 tokens at least)
+ *   (targets, weights, loss and lse are 16-byte aligned, too)
+ *   workspace: dev, >= lowra_vocab_loss_workspace_bytes(M, V, K, dH wanted), 16-byte aligned.  Tokens are taken in pieces, so that it is less than 512 MiB up
+ *   to V 2^19 and K 2^17; beyond, a piece is 256 tokens: 512 V bytes and 1024 K, and partial sums of up to 64 MiB (1.1 GiB at V 2^21).  Fewer tokens
+ *   may need more (other splits): a workspace that is kept for batches of several sizes is the largest of theirs
  * Products are bf16 with fp32 sums; the probabilities of the words but the target are rounded to bf16 before they meet W and brought back to their
  * exact sum behind it; the target's term is fp32 and keeps its digits where the model is sure; a probability below 2^-94 of the largest may count as zero.  The order of all sums is fixed.  A NaN or an infinity in a row of h stays in its row.
  * M == 0 is a no-op.  INVALID_ARG: M < 0, V <= 0, K <= 0, a missing pointer, an output or the workspace that overlaps anything; UNSUPPORTED: K % 8

@@ -244,7 +244,7 @@ hipError_t adamw_build(const std::vector<AdamwItem>& items, bool eight, AdamwGro
     if (items.empty()) return hipSuccess;
     long long total = 0;
     for (const AdamwItem& it : items) total += it.count;
-    // A batch of which the 256 MB behind the caches hold less than half of what it reads and writes goes past the caches, and a workgroup asks for AW_MOST rounds together: 32-bit
+    // A batch that reads and writes more than 128 MB, half of what the 256 MB behind the caches hold, goes past the caches, and a workgroup asks for AW_MOST rounds together: 32-bit
     // states of 201 MB 47 us through the caches and 43.5 in single rounds, 40.3 so; of 268 MB 57.6 in single rounds, 53.2 so; 8-bit states of 327 MB, two decodings with them, 98 and 91.
     // Below, workgroups of one round are as soon done or sooner (8-bit states of 82 MB 30.0 -> 27.4, 32-bit ones of 37 MB 8.4 -> 7.0).
     g.large = total * (eight ? 18 : 30) > (128ll << 20);

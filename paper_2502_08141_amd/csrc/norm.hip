@@ -6,8 +6,8 @@
 // Memory bound: every operand is read or written once, 16 bytes per lane.  A row stays in the registers of the threads that share it, so
 // that the deviations are squared about the mean itself; the backward pass forms mean and rstd again from the x that it reads
 // anyway, which costs it one reduction and saves the forward pass two arrays.  A thread keeps its columns from row to row and with them their
-// sums; workgroups meet in the workspace, added in a fixed order.  Graph replays: 4096 x 4096 forward 13.2 us (5.1 TB/s), rms backward with residual and dweight
-// 28.8 (4.7); layer backward with both sums 31.7; 777 x 1024 3.3 and 7.1, a launch each and one more for the sums.
+// sums; workgroups meet in the workspace, added in a fixed order.  Graph replays: 4096 x 4096 forward 13.1 us (5.1 TB/s), rms backward with residual and dweight
+// 28.4 (4.7), dX alone 19.6; layer backward with both sums 30.4 and with residual 35.4; 777 x 1024 3.3 and 6.9, a launch each and one more for the sums.
 #include <algorithm>
 
 #include "gemm_common.h"

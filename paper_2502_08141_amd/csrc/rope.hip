@@ -2,8 +2,9 @@
 // j and j + rot/2 (or 2 j and 2 j + 1) becomes (a cos - b sin, a sin + b cos), the angle being the token's position times f_j; the inverse
 // turns by the negative angle, which is the gradient's way back.
 //
-// Memory bound: 2 bytes in and 2 out per element.  The angle is position x turns mod 2^64 in whole numbers, 2^-64 of a full turn a unit: exact
-// at any position, where fp32 is off by 0.03 at 2^20 and a table of cosines would be read beside the data.  What is left is at most an eighth of a turn, where
+// Memory bound: 2 bytes in and 2 out per element.  The angle is position x turns mod 2^64 in whole numbers, 2^-64 of a full turn a unit, and then rounded to 2^-32 of a
+// turn (2^-30 radians): no product loses digits at far positions, where fp32 is off by 0.03 at 2^20 and a table of cosines would be read beside the data.  What the plan's
+// frequencies have lost (53 bits of each) grows with the position to 2^-32 at 2^20 and 2^-21 at 2^31.  What is left is at most an eighth of a turn, where
 // the Taylor polynomials of degree 9 and 10 are exact to fp32 rounding (remainders pi/4^11 / 11! = 2e-9 and pi/4^12 / 12! = 1e-10).  A thread keeps
 // the angles of its columns for several heads.  Graph replays: 4096 tokens of 32 + 32 heads of 128 columns 22.8 us (5.9 TB/s), 32 + 8 heads of neighbours 15.4,
 // four tokens of 32 + 8 heads 3.2.
