@@ -431,7 +431,7 @@ lowra_status lowra_vocab_loss(int M, int V, int K, const uint16_t* h, const uint
  * from m' and v' before they are coded.  Zeroed bytes are zero states.  What is not finite spoils its element with 32-bit states and its group with 8-bit ones.
  *   items: host array of n entries (read during create only); device pointers, 16-byte aligned (absmax: 4), that stay valid and in place for the
  *   life of the batch; m_out, v_out, m_absmax_out, v_absmax_out and weight_out may be the inputs of that name (in place), nothing else overlaps an output.
- *   grad_scale: one fp32 dev or null (one), e.g. the factor of a gradient clipping, without a wait for it.
+ *   grad_scale: one fp32 dev or null (one), e.g. the factor of a gradient clipping, without a wait for it; not in an output of the batch.
  * An eps between 0 and 2^-126 counts as 2^-126.  A run takes the scalars (a captured one repeats those it was captured with) and only launches.  create allocates device memory for the descriptors and
  * copies them synchronously; destroy frees.
  * create: INVALID_ARG (null / n <= 0 / count <= 0 / a missing pointer; absmax is needed with 8 bits and null with 32; an output that overlaps
